@@ -307,6 +307,65 @@ int lr_attention_gqa_bwd(const void* q, const void* k, const void* v, const void
                          int64_t ld, int64_t ldkv, int64_t B, int64_t S, int64_t H, int64_t Hkv,
                          int64_t hd, int causal, int dt, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- rotary tables and rotation at given positions ----------------------------------------- */
+/* cos_tab, sin_tab[n, rot / 2] (fp32): mscale * cos, mscale * sin of (first + p) * w_i, p < n, with the frequencies
+ * w_i = base^(-2 i / rot) scaled for contexts longer than the one trained on: context = 0 divides all of them by `factor`
+ * (1: none); context > 0 goes by t_i = context * w_i / (2 pi), the turns over the trained context: a frequency of t_i <= low is divided
+ * by factor, one of t_i >= high is kept, linearly in between.  Angles are formed in 64 bits, each entry is rounded once.
+ * rot even, at most 8192 (else LR_EUNSUPPORTED); first >= 0, first + n <= 2^31; base > 0, factor > 0, mscale finite, low < high.
+ * The tables serve lr_rope_at and lr_kv_append, and with rot = 128 lr_rope and the block (rope_cos, rope_sin).                 */
+int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_t first, double base, double factor,
+                  double context, double low, double high, double mscale, void* stream);
+/* out[T, ldo] = x[T, ldx] (H heads of hd columns from column 0) with the first rot columns of every head rotated by row pos[t] (DEVICE
+ * int32; NULL: t) of the tables [table_rows, rot / 2]: pairs (i, i + rot / 2), or (2i, 2i + 1) where interleaved != 0, become
+ * (a c - b s, b c + a s).  inverse != 0 uses -s: the transpose, which is its gradient.  Columns rot.. of a head are copied; a row of
+ * out whose position is outside the tables is left as it was, and so are columns past the heads.  out may be x with ldo = ldx (in
+ * place); any other overlap is not allowed.  LR_BF16: hd and the strides multiples of 8, rot of 16, all pointers 16-byte aligned but
+ * pos; LR_F32: rot even.  rot <= hd.  T may be 0.                                                                              */
+int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t* pos, const float* cos_tab,
+               const float* sin_tab, int64_t table_rows, int64_t T, int64_t H, int64_t hd, int64_t rot, int interleaved,
+               int inverse, int dt, void* stream);
+
+/* ---- a paged key / value cache ------------------------------------------------------------- */
+/* Keys and values of `batch` sequences (bf16), in pages of page_size tokens that a sequence collects in any order: key j of sequence b
+ * lies in page page_table[b, j / page_size], row j % page_size.  Token t of a call belongs to the sequence b with
+ * cu_q[b] <= t < cu_q[b + 1]; kv_len[b] counts b's keys including the new ones, so that its new tokens stand at positions
+ * kv_len[b] - (cu_q[b + 1] - cu_q[b]) and up.  The lists are DEVICE int32 and not read on the host: a captured call takes what they
+ * hold when it is replayed.  Tokens before cu_q[0] or from cu_q[batch] on belong to nobody (a padded batch): nothing is written for
+ * them.  Whatever the lists hold, nothing outside the cache and the other arguments is read or written: a page number
+ * outside [0, n_pages) is no page, keys past max_pages * page_size do not exist.
+ * page_size, head_dim and the strides (elements) are multiples of 8, k and v 16-byte aligned (LR_EALIGN); pages of both layouts
+ * [page_size, n_kv_heads, head_dim] and [n_kv_heads, page_size, head_dim] are a matter of the strides.  Limits (LR_EUNSUPPORTED):
+ * 2^35 elements from the first to the last of k, 2^31 - 1 keys of a sequence, 2^26 tokens of a call, token_stride < 2^26.       */
+typedef struct {
+  void *k, *v;
+  int64_t n_pages, page_size, n_kv_heads, head_dim;
+  int64_t page_stride, token_stride, head_stride;
+  const int32_t* page_table;   /* [batch, table_ld], max_pages columns of it */
+  int64_t batch, max_pages, table_ld;
+  const int32_t* cu_q;         /* [batch + 1] */
+  const int32_t* kv_len;       /* [batch] */
+} lr_kv_cache;                 /* a HOST struct */
+
+/* Writes the keys k[T, ldk] and values v[T, ldv] (n_kv_heads heads of head_dim columns) of the new tokens into their pages.  With tables
+ * (cos_tab, sin_tab, rot > 0: as lr_rope_at) keys are rotated by their position on the way; NULL tables with rot = 0: as they are.
+ * q (NULL: none; H heads, [T, ldq]) is rotated likewise into q_out[T, ldqo], which may be q with the same stride.  A token without a
+ * place (no page, no position below kv_len, no row in the tables) is left out: its row of q_out stays as it was.  Two tokens with one
+ * place (a page in two rows of page_table): either one's, or a mixture.  dt: LR_BF16.                                          */
+int lr_kv_append(const lr_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q,
+                 int64_t ldq, void* q_out, int64_t ldqo, int64_t T, int64_t H, const float* cos_tab, const float* sin_tab,
+                 int64_t table_rows, int64_t rot, int interleaved, int dt, void* stream);
+
+/* Causal attention of the new tokens over the cache, which holds their own keys and values already: o[T, ldo] (H heads) =
+ * softmax(scale * q . k) . v over the keys at positions up to the token's own, query head h on key / value head
+ * h / (H / n_kv_heads); lse[T, H] (fp32, NULL: not written) = log of the softmax's sum.  Any mixture of long and single-token sequences.
+ * A token that sees no key has o = 0 and lse = -infinity; a page number that is no page holds zeros.  H % n_kv_heads == 0, scale > 0.
+ * dt LR_BF16, head_dim 128, causal 1, otherwise LR_EUNSUPPORTED.  The workspace holds the parts of sequences whose keys are split over workgroups;
+ * its size depends on T, H and the cache's sizes, not on the lists.                                                            */
+size_t lr_attention_paged_workspace_bytes(const lr_kv_cache* cache, int64_t T, int64_t H);
+int lr_attention_paged_fwd(const lr_kv_cache* cache, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse,
+                           int64_t T, int64_t H, float scale, int causal, int dt, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- measurement aid (not on the compute path) ------------------------------------------ */
 /* Between begin and end every bf16 MFMA GEMM launch the library makes, and each attention forward /
  * backward call of the block, is bracketed by two HIP events on its stream.  end waits for the last one

@@ -56,6 +56,12 @@ class BlockLax(C.Structure):
     _fields_ = [(k + "_" + n, _vp) for k in ("h_prev", "dz_next", "dh_prev") for n in ("qkv", "o", "gu", "d")]
 
 
+class KvCache(C.Structure):
+    _fields_ = [("k", _vp), ("v", _vp)] + [(n, _i64) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "page_stride",
+                                                               "token_stride", "head_stride")] + \
+               [("page_table", _vp), ("batch", _i64), ("max_pages", _i64), ("table_ld", _i64), ("cu_q", _vp), ("kv_len", _vp)]
+
+
 PARAM_NAMES = tuple(n for n, _ in BlockParams._fields_)
 LAX_PARTS = ("qkv", "o", "gu", "d")
 
@@ -96,6 +102,12 @@ _SIGS = {
     "lr_attention_gqa_bwd_workspace_bytes": (_sz, [_i64, _i64, _i64, _i64, _i64]),
     "lr_attention_gqa_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _i64,
                                     _int, _int, _vp, _sz, _vp]),
+    "lr_rope_table": (_int, [_vp, _vp, _i64, _i64, _i64] + [C.c_double] * 6 + [_vp]),
+    "lr_rope_at": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _int, _int, _int, _vp]),
+    "lr_kv_append": (_int, [C.POINTER(KvCache), _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _i64, _int, _int,
+                            _vp]),
+    "lr_attention_paged_workspace_bytes": (_sz, [C.POINTER(KvCache), _i64, _i64]),
+    "lr_attention_paged_fwd": (_int, [C.POINTER(KvCache), _vp, _i64, _vp, _i64, _vp, _i64, _i64, _f32, _int, _int, _vp, _sz, _vp]),
     "lr_launch_timer_begin": (_int, [_int]),
     "lr_launch_timer_end": (_int, [_vp, _int, C.POINTER(_int)]),
     "lr_gemm_tile": (_int, [_int, _int, _int, _int, _int, _int, C.POINTER(_int), C.POINTER(_int)]),
@@ -175,6 +187,12 @@ def _dense(t):
 
 def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+# launches go to the current stream, which is one of the current device's
+def _on_current(device):
+    if device.type != "cuda" or device.index not in (None, torch.cuda.current_device()):
+        raise LrError(f"tensors on the current GPU expected, not on {device}")
 
 
 def _ws(nbytes: int, device):
@@ -456,6 +474,50 @@ def lr_attention_gqa_fwd(q, k, v, B, S, H, Hkv, hd, causal=True):
 
 def lr_attention_gqa_bwd(q, k, v, o, dout, lse, B, S, H, Hkv, hd, causal=True):
     return _native().attention_bwd(q, k, v, o, dout, lse, B, S, H, Hkv, hd, int(causal))
+
+
+# ---- rotary positions ------------------------------------------------------------------------
+def lr_rope_table(n, rot, base=10000.0, first=0, factor=1.0, ramp=None, mscale=1.0, device="cuda"):
+    """Returns (cos, sin) [n, rot / 2] fp32 of the positions first ..  factor > 1 stretches the context: all frequencies are divided by it,
+    or, with ramp = (trained context, low, high), those of at most `low` turns over the trained context, those of `high` and more are kept."""
+    context, low, high = (0.0, 0.0, 1.0) if ramp is None else ramp
+    if ramp is not None and not context > 0:
+        raise LrError("lr_rope_table: the trained context of a ramp is positive")
+    _on_current(torch.device(device))
+    cos, sin = (torch.empty((max(n, 0), max(rot, 0) // 2), dtype=torch.float32, device=device) for _ in range(2))
+    _check(lib().lr_rope_table(_dense(cos), _dense(sin), n, rot, first, base, factor, context, low, high, mscale, _stream()), "lr_rope_table")
+    return cos, sin
+
+
+def lr_rope_at(x, cos, sin, H, hd, pos=None, interleaved=False, inverse=False, out=None):
+    """x [T, >= H*hd] with the first 2 * cos.shape[1] columns of every head rotated by the table rows pos [T] int32 (None: 0, 1, ..);
+    returns out (None: a new tensor; x: in place)."""
+    return _native().rope_at(x, cos, sin, H, hd, pos, int(interleaved), int(inverse), out)
+
+
+# ---- paged key / value cache -------------------------------------------------------------------
+def lr_kv_append(k, v, k_cache, v_cache, page_table, cu_q, kv_len, rope=None, interleaved=False, q=None, H=0, q_out=None):
+    """Writes k, v [T, >= Hkv*hd] of the new tokens into their pages, keys rotated by their positions with rope = (cos, sin).  k_cache, v_cache
+    [pages, page size, Hkv, hd] (any strides, the same for both; hd contiguous), page_table [batch, columns], cu_q [batch + 1] and
+    kv_len [batch] int32.  q [T, >= H*hd]: rotated likewise; returns q_out (None: a new tensor; q: in place), or None without q."""
+    cos, sin = (None, None) if rope is None else rope
+    return _native().kv_append(k, v, k_cache, v_cache, page_table, cu_q, kv_len, cos, sin, int(interleaved), q, H, q_out)
+
+
+def lr_attention_paged_fwd(q, k_cache, v_cache, page_table, cu_q, kv_len, H, scale=None, causal=True, o=None, lse=None, ws=None):
+    """Returns (o like q, lse [T, H] fp32) of the new tokens' queries q [T, >= H*hd] over the cache (as lr_kv_append takes it, which comes
+    first).  scale: None = 1 / sqrt(hd).  Rows of o and lse that belong to no sequence are not written."""
+    return _native().attention_paged_fwd(q, k_cache, v_cache, page_table, cu_q, kv_len, H, k_cache.shape[-1] ** -0.5 if scale is None else scale,
+                                         int(causal), o, lse, ws)
+
+
+def lr_attention_paged_workspace_bytes(k_cache, page_table, T, H):
+    """Bytes of a workspace for calls of T tokens and H query heads on such a cache."""
+    pages, page_size, Hkv, hd = k_cache.shape
+    batch, cols = page_table.shape
+    c = KvCache(None, None, pages, page_size, Hkv, hd, k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), None, batch, cols,
+                page_table.stride(0), None, None)
+    return lib().lr_attention_paged_workspace_bytes(C.byref(c), T, H)
 
 
 # ---- measurement aid -----------------------------------------------------------------------

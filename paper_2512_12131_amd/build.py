@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "liblrboost.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.hip", "gemm_bf16.hip", "gemm_ring32.hip", "gemm_ring64.hip", "gemm_ring64x128.hip", "gemm_ring128.hip", "gemm_joint.hip", "gemm_rows16.hip",
-           "gemm_f32.hip", "stream_kernels.hip", "attention.hip", "probe.hip"]
+           "gemm_f32.hip", "stream_kernels.hip", "attention.hip", "attention_paged.hip", "rope.hip", "probe.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

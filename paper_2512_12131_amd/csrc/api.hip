@@ -3,6 +3,7 @@
 // Every entry point runs the same sequencing function twice over its lifetime: once "dry" (no
 // launches, only workspace carving) to answer *_workspace_bytes(), once for real.  That keeps the
 // size query and the actual use of the workspace from drifting apart.
+#include <cmath>
 #include <cstring>
 #include <mutex>
 
@@ -1429,6 +1430,122 @@ int lr_rope(void* x, int64_t ldx, const float* cos_tab, const float* sin_tab, in
   if (ldx % 8) return LR_EALIGN;
   hipError_t e = k_rope128_bf16(x, ldx, (int)H, nullptr, 0, 0, cos_tab, sin_tab, B * S, (int)S, inverse, (hipStream_t)stream);
   return e == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+// ---- rotary tables, rotation at positions, paged cache ---------------------------------------------
+int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_t first, double base, double factor, double context,
+                  double low, double high, double mscale, void* stream) {
+  if (n < 0 || rot <= 0 || rot % 2 || first < 0 || n > ((int64_t)1 << 31) || first > ((int64_t)1 << 31) - n) return LR_EINVAL;
+  if (!(base > 0) || !(factor > 0) || !(context >= 0) || !std::isfinite(base) || !std::isfinite(factor) || !std::isfinite(context) ||
+      !std::isfinite(mscale))
+    return LR_EINVAL;
+  if (context > 0 && (!(low < high) || !std::isfinite(low) || !std::isfinite(high))) return LR_EINVAL;
+  if (rot > 8192) return LR_EUNSUPPORTED;
+  if (n == 0) return LR_OK;
+  TRY(check_ptrs(LR_F32, {cos_tab, sin_tab}));
+  return k_rope_table(cos_tab, sin_tab, n, (int)(rot / 2), first, base, factor, context, low, high, mscale, (hipStream_t)stream) == hipSuccess
+             ? LR_OK : LR_ELAUNCH;
+}
+
+// what a rotation asks of heads, strides and tables
+static int check_rotation(int64_t hd, int64_t rot, const float* cos_tab, const float* sin_tab, int64_t table_rows, int dt) {
+  if (rot <= 0 || rot > hd || rot % 2 || table_rows <= 0) return LR_EINVAL;
+  if (table_rows > 0x7fffffffLL) return LR_EUNSUPPORTED;
+  if (dt == LR_BF16 && rot % 16) return LR_EALIGN;
+  return check_ptrs(dt, {cos_tab, sin_tab});
+}
+
+int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t* pos, const float* cos_tab, const float* sin_tab,
+               int64_t table_rows, int64_t T, int64_t H, int64_t hd, int64_t rot, int interleaved, int inverse, int dt, void* stream) {
+  TRY(check_dt(dt));
+  if (T < 0 || T > 0x7fffffffLL || H <= 0 || hd <= 0 || H > (1 << 24) || hd > (1 << 24) || H * hd > (1 << 24) || ldx < H * hd || ldo < H * hd)
+    return LR_EINVAL;
+  TRY(check_dims_bf16(dt, {hd, ldx, ldo}));
+  TRY(check_rotation(hd, rot, cos_tab, sin_tab, table_rows, dt));
+  if (!pos && T > table_rows) return LR_EINVAL;
+  if (x == out && ldx != ldo) return LR_EINVAL;
+  if ((uintptr_t)pos & 3) return LR_EALIGN;
+  if (T == 0) return LR_OK;
+  TRY(check_ptrs(dt, {x, out}));
+  return k_rope_at(x, ldx, out, ldo, pos, cos_tab, sin_tab, table_rows, T, (int)H, (int)hd, (int)rot, interleaved, inverse, dt,
+                   (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+static int check_cache(const lr_kv_cache* c, bool pointers, KvCache* out) {
+  if (!c) return LR_EINVAL;
+  const int64_t most = 0x7fffffffLL, far = (int64_t)1 << 35;
+  if (c->n_pages <= 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 || c->batch < 0 || c->max_pages <= 0 ||
+      c->table_ld < c->max_pages || c->page_stride <= 0 || c->token_stride <= 0 || c->head_stride <= 0)
+    return LR_EINVAL;
+  if (c->n_pages > most || c->page_size > most || c->max_pages > most / c->page_size || c->batch > (1 << 24) || c->n_kv_heads > (1 << 16) ||
+      c->head_dim > (1 << 16) || c->token_stride >= (1 << 26) || c->page_stride > far || c->head_stride > far ||
+      (c->n_pages > 1 && c->page_stride > far / (c->n_pages - 1)) || c->table_ld > far / (c->batch > 0 ? c->batch : 1))
+    return LR_EUNSUPPORTED;
+  if ((c->n_pages - 1) * c->page_stride + (c->page_size - 1) * c->token_stride + (c->n_kv_heads - 1) * c->head_stride + c->head_dim > far)
+    return LR_EUNSUPPORTED;
+  TRY(check_dims_bf16(LR_BF16, {c->page_size, c->head_dim, c->page_stride, c->token_stride, c->head_stride}));
+  if (pointers) {
+    TRY(check_ptrs(LR_BF16, {c->k, c->v}));
+    TRY(check_ptrs(LR_F32, {c->page_table, c->cu_q, c->kv_len}));
+  }
+  *out = KvCache{(uint16_t*)c->k, (uint16_t*)c->v, c->page_stride, c->token_stride, c->head_stride, c->table_ld, c->max_pages * c->page_size,
+                 c->page_table, c->cu_q, c->kv_len, (int)c->n_pages, (int)c->page_size, (int)c->n_kv_heads, (int)c->head_dim, (int)c->batch,
+                 FastDiv::of(c->page_size)};
+  return LR_OK;
+}
+constexpr int64_t PAGED_TOKENS = (int64_t)1 << 26;
+
+int lr_kv_append(const lr_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, void* q_out,
+                 int64_t ldqo, int64_t T, int64_t H, const float* cos_tab, const float* sin_tab, int64_t table_rows, int64_t rot,
+                 int interleaved, int dt, void* stream) {
+  KvCache c;
+  TRY(check_dt(dt));
+  if (dt != LR_BF16) return LR_EUNSUPPORTED;
+  TRY(check_cache(cache, true, &c));
+  const int64_t hd = c.head_dim, row = c.n_kv_heads * hd;
+  if (T < 0 || ldk < row || ldv < row || H < 0 || H > (1 << 16) || (H + c.n_kv_heads) * hd > (1 << 24) || (H > 0) != (q != nullptr) ||
+      (q != nullptr) != (q_out != nullptr))
+    return LR_EINVAL;
+  if (q && (ldq < H * hd || ldqo < H * hd || (q == q_out && ldq != ldqo))) return LR_EINVAL;
+  if (T > PAGED_TOKENS) return LR_EUNSUPPORTED;
+  TRY(check_dims_bf16(dt, {ldk, ldv, q ? ldq : 0, q ? ldqo : 0}));
+  if (rot == 0) {
+    if (cos_tab || sin_tab) return LR_EINVAL;
+  } else {
+    TRY(check_rotation(hd, rot, cos_tab, sin_tab, table_rows, dt));
+  }
+  if (T == 0 || c.batch == 0) return LR_OK;
+  TRY(check_ptrs(dt, {k, v}));
+  if (q) TRY(check_ptrs(dt, {q, q_out}));
+  return k_kv_append(c, k, ldk, v, ldv, q, ldq, q_out, ldqo, T, (int)H, cos_tab, sin_tab, table_rows, (int)rot, interleaved,
+                     (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+static int check_paged(const lr_kv_cache* cache, bool pointers, int64_t T, int64_t H, KvCache* c) {
+  TRY(check_cache(cache, pointers, c));
+  if (T < 0 || H <= 0 || H > (1 << 16) || H % c->n_kv_heads) return LR_EINVAL;
+  if (T > PAGED_TOKENS || T * H > 0x7fffffffLL || c->head_dim != 128) return LR_EUNSUPPORTED;
+  return LR_OK;
+}
+
+size_t lr_attention_paged_workspace_bytes(const lr_kv_cache* cache, int64_t T, int64_t H) {
+  KvCache c;
+  return check_paged(cache, false, T, H, &c) == LR_OK ? attention_paged_ws_bytes(T, (int)H, c.n_kv_heads, c.batch, c.capacity) : 0;
+}
+
+int lr_attention_paged_fwd(const lr_kv_cache* cache, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int64_t T, int64_t H,
+                           float scale, int causal, int dt, void* ws, size_t ws_bytes, void* stream) {
+  KvCache c;
+  TRY(check_dt(dt));
+  TRY(check_paged(cache, true, T, H, &c));
+  if (dt != LR_BF16 || causal != 1) return LR_EUNSUPPORTED;
+  if (ldq < H * 128 || ldo < H * 128 || !(scale > 0) || !std::isfinite(scale)) return LR_EINVAL;
+  TRY(check_dims_bf16(dt, {ldq, ldo}));
+  if (T == 0 || c.batch == 0) return LR_OK;
+  TRY(check_ptrs(dt, {q, o}));
+  if ((uintptr_t)lse & 3) return LR_EALIGN;
+  TRY(check_ws(ws, ws_bytes, attention_paged_ws_bytes(T, (int)H, c.n_kv_heads, c.batch, c.capacity)));
+  return attention_paged_bf16(c, q, ldq, o, ldo, lse, T, (int)H, scale, ws, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
 }
 
 // ---- measurement aid ---------------------------------------------------------------------------

@@ -217,6 +217,38 @@ hipError_t k_wgrad_finish_many(const FinishJob* jobs, int n, int accumulate, int
 hipError_t k_colsum_parts(const float* part, int64_t nparts, int64_t cols, void* out, int accumulate,
                           int out_dt, hipStream_t);
 
+// ---- rotary positions and the paged cache (rope.hip) -------------------------------------------
+// n / d for n < 2^31 as a product: mul = floor(2^(31 + s) / d) + 1 with 2^s >= d is off by less than 2^s / 2^(31 + s) per unit of n
+struct FastDiv {
+  uint32_t mul = 0, shift = 31;
+  static FastDiv of(int64_t d) {
+    uint32_t s = 0;
+    while (((int64_t)1 << s) < d) s++;
+    return FastDiv{(uint32_t)(((uint64_t)1 << (31 + s)) / (uint64_t)d + 1), 31 + s};
+  }
+  __host__ __device__ uint32_t div(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> shift); }
+};
+// lr_kv_cache as the kernels take it; strides in elements
+struct KvCache {
+  uint16_t *k, *v;
+  int64_t page_stride, token_stride, head_stride, table_ld, capacity;   // capacity: keys that a row of the page table holds
+  const int32_t *page_table, *cu_q, *kv_len;
+  int n_pages, page_size, n_kv_heads, head_dim, batch;
+  FastDiv by_page;
+};
+hipError_t k_rope_table(float* cs, float* sn, int64_t n, int half, int64_t first, double base, double factor, double context, double low,
+                        double high, double mscale, hipStream_t);
+hipError_t k_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t* pos, const float* cs, const float* sn,
+                     int64_t table_rows, int64_t T, int H, int hd, int rot, int interleaved, int inverse, int dt, hipStream_t);
+hipError_t k_kv_append(const KvCache& c, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, void* q_out,
+                       int64_t ldqo, int64_t T, int H, const float* cs, const float* sn, int64_t table_rows, int rot, int interleaved,
+                       hipStream_t);
+
+// ---- attention over the pages of a cache (attention_paged.hip) -----------------------------------
+size_t attention_paged_ws_bytes(int64_t T, int H, int Hkv, int batch, int64_t capacity);
+hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int64_t T, int H, float scale,
+                                void* ws, hipStream_t);
+
 // ---- attention (attention.hip) ---------------------------------------------------------------
 hipError_t attention_fwd_bf16(const void* q, const void* k, const void* v, void* o, float* lse, int64_t ld,
                               int B, int S, int H, int hd, int causal, hipStream_t);

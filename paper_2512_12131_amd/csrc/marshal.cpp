@@ -328,6 +328,137 @@ PyObject* swiglu_bwd(Args& a) {
   return tuple(dg, du);
 }
 
+// ---- rotary positions, paged cache -----------------------------------------------------------
+// Launches go to the current stream, which is one of the current device's: operands are there too.
+void on_current_device(std::initializer_list<const at::Tensor*> ts) {
+  for (const at::Tensor* t : ts)
+    if (t->defined() && (!t->is_cuda() || t->get_device() != c10::hip::current_device())) fail(g_lr_error, "tensors on the current GPU expected");
+}
+const int32_t* indices(const at::Tensor& t, int64_t n) {
+  if (t.defined() && t.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
+  if (t.defined() && (t.dim() != 1 || t.size(0) != n)) fail(PyExc_ValueError, "unexpected number of indices");
+  return (const int32_t*)dense(t);
+}
+void same_type(const at::Tensor& a, std::initializer_list<const at::Tensor*> others) {
+  for (const at::Tensor* t : others)
+    if (t->defined() && t->scalar_type() != a.scalar_type()) fail(g_lr_error, "operands of one type expected");
+}
+void rows_as_wide(const at::Tensor& t, int64_t T, int64_t width) {
+  if (t.dim() != 2 || t.size(0) != T || t.size(1) < width) fail(PyExc_ValueError, "unexpected shape");
+}
+// rows and pairs of the tables
+void tables_of(const at::Tensor& cos, const at::Tensor& sin, int64_t& rows, int64_t& half) {
+  if (cos.scalar_type() != at::kFloat || sin.scalar_type() != at::kFloat) fail(g_lr_error, "fp32 tables expected");
+  rows = rows_of(cos);
+  half = cos.size(1);
+  if (sin.sizes() != cos.sizes()) fail(PyExc_ValueError, "tables of the same shape expected");
+}
+
+PyObject* rope_at(Args& a) {
+  const at::Tensor &x = a.tensor(), &cos = a.tensor(), &sin = a.tensor();
+  const int64_t H = a.integer(), hd = a.integer();
+  const at::Tensor pos = a.optional();
+  const int inter = a.enumerator(), inverse = a.enumerator();
+  at::Tensor out = a.optional();
+  const int64_t T = rows_of(x), ldx = stride_of(x);
+  const int dt = dt_of(x);
+  int64_t rows, half;
+  tables_of(cos, sin, rows, half);
+  const int32_t* pp = indices(pos, T);
+  rows_as_wide(x, T, H * hd);
+  if (!out.defined()) out = fresh({T, H * hd}, x.scalar_type(), x);
+  same_type(x, {&out});
+  rows_as_wide(out, T, H * hd);
+  const int64_t ldo = stride_of(out);
+  on_current_device({&x, &cos, &sin, &pos, &out});
+  void *px = ptr(x), *pc = dense(cos), *ps = dense(sin), *po = ptr(out), *st = stream();
+  call("lr_rope_at", [&] { return lr_rope_at(px, ldx, po, ldo, pp, (float*)pc, (float*)ps, rows, T, H, hd, 2 * half, inter, inverse, dt, st); });
+  return wrap(out);
+}
+
+// k, v [pages, page size, heads, hd], page_table [batch, columns], cu_q [batch + 1], kv_len [batch]
+struct CacheTensors {
+  const at::Tensor &k, &v, &table, &cu, &len;
+  explicit CacheTensors(Args& a) : k(a.tensor()), v(a.tensor()), table(a.tensor()), cu(a.tensor()), len(a.tensor()) {}
+  lr_kv_cache view() const {
+    if (k.dim() != 4 || v.sizes() != k.sizes() || table.dim() != 2) fail(PyExc_ValueError, "unexpected shape of the cache or its page table");
+    if (k.scalar_type() != at::kBFloat16 || v.scalar_type() != at::kBFloat16) fail(g_lr_error, "a bf16 cache expected");
+    if (k.stride(3) != 1 || v.strides() != k.strides()) fail(PyExc_AssertionError, "caches with the same strides and contiguous heads expected");
+    if (table.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
+    if (table.size(1) > 1 && table.stride(1) != 1) fail(PyExc_AssertionError, "row-major page table expected");
+    const int64_t batch = table.size(0), cols = table.size(1);
+    lr_kv_cache c;
+    c.k = ptr(k); c.v = ptr(v);
+    c.n_pages = k.size(0); c.page_size = k.size(1); c.n_kv_heads = k.size(2); c.head_dim = k.size(3);
+    c.page_stride = k.stride(0); c.token_stride = k.stride(1); c.head_stride = k.stride(2);
+    c.page_table = (const int32_t*)ptr(table);
+    c.batch = batch; c.max_pages = cols;
+    c.table_ld = batch > 1 ? table.stride(0) : cols;
+    c.cu_q = indices(cu, batch + 1);
+    c.kv_len = indices(len, batch);
+    return c;
+  }
+};
+
+PyObject* kv_append(Args& a) {
+  const at::Tensor &k = a.tensor(), &v = a.tensor();
+  const CacheTensors ct(a);
+  const at::Tensor cos = a.optional(), sin = a.optional();
+  const int inter = a.enumerator();
+  const at::Tensor q = a.optional();
+  const int64_t H = a.integer();
+  at::Tensor q_out = a.optional();
+  const lr_kv_cache c = ct.view();
+  const int64_t T = rows_of(k), ldk = stride_of(k), ldv = stride_of(v);
+  const int dt = dt_of(k);
+  int64_t rows = 0, half = 0, ldq = 0, ldqo = 0;
+  if (cos.defined() != sin.defined()) fail(PyExc_ValueError, "both tables or neither expected");
+  if (cos.defined()) tables_of(cos, sin, rows, half);
+  if (cos.defined() && half == 0) fail(PyExc_ValueError, "tables without columns");
+  rows_as_wide(k, T, c.n_kv_heads * c.head_dim);
+  rows_as_wide(v, T, c.n_kv_heads * c.head_dim);
+  if (q.defined()) {
+    rows_as_wide(q, T, H * c.head_dim);
+    ldq = stride_of(q);
+    if (!q_out.defined()) q_out = fresh({T, H * c.head_dim}, q.scalar_type(), q);
+    rows_as_wide(q_out, T, H * c.head_dim);
+    ldqo = stride_of(q_out);
+  }
+  same_type(k, {&v, &q, &q_out});
+  on_current_device({&k, &v, &ct.k, &ct.v, &ct.table, &ct.cu, &ct.len, &cos, &sin, &q, &q_out});
+  void *pk = ptr(k), *pv = ptr(v), *pc = dense(cos), *ps = dense(sin), *pq = ptr(q), *po = ptr(q_out), *st = stream();
+  call("lr_kv_append", [&] {
+    return lr_kv_append(&c, pk, ldk, pv, ldv, pq, ldq, po, ldqo, T, H, (float*)pc, (float*)ps, rows, 2 * half, inter, dt, st);
+  });
+  if (!q_out.defined()) Py_RETURN_NONE;
+  return wrap(q_out);
+}
+
+PyObject* attention_paged_fwd(Args& a) {
+  const at::Tensor& q = a.tensor();
+  const CacheTensors ct(a);
+  const int64_t H = a.integer();
+  const float scale = a.real();
+  const int causal = a.enumerator();
+  at::Tensor o = a.optional(), lse = a.optional(), ws = a.optional();
+  const lr_kv_cache c = ct.view();
+  const int64_t T = rows_of(q), ldq = stride_of(q);
+  const int dt = dt_of(q);
+  rows_as_wide(q, T, H * c.head_dim);
+  if (!o.defined()) o = fresh({T, H * c.head_dim}, q.scalar_type(), q);
+  rows_as_wide(o, T, H * c.head_dim);
+  same_type(q, {&o});
+  const int64_t ldo = stride_of(o);
+  if (!lse.defined()) lse = fresh({T, H}, at::kFloat, q);
+  if (lse.scalar_type() != at::kFloat || lse.dim() != 2 || lse.size(0) != T || lse.size(1) != H) fail(PyExc_ValueError, "lse [T, H] fp32 expected");
+  on_current_device({&q, &ct.k, &ct.v, &ct.table, &ct.cu, &ct.len, &o, &lse, &ws});
+  if (!ws.defined()) ws = workspace(lr_attention_paged_workspace_bytes(&c, T, H), q);
+  const size_t nb = ws.numel() * ws.element_size();
+  void *pq = ptr(q), *po = ptr(o), *pl = dense(lse), *pw = dense(ws), *st = stream();
+  call("lr_attention_paged_fwd", [&] { return lr_attention_paged_fwd(&c, pq, ldq, po, ldo, (float*)pl, T, H, scale, causal, dt, pw, nb, st); });
+  return tuple(o, lse);
+}
+
 // No C++ exception leaves an entry; torch's own become the Python exceptions that they are elsewhere (out of memory, a device's error,
 // an interpreter's exception that crossed torch).
 template <PyObject* (*F)(Args&)>
@@ -351,7 +482,7 @@ PyObject* set_error(PyObject*, PyObject* type) {
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))(&entry<f>), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     ENTRY(linear_fwd), ENTRY(linear_fwd_static), ENTRY(linear_bwd), ENTRY(group_fwd), ENTRY(group_bwd), ENTRY(attention_fwd), ENTRY(attention_bwd),
-    ENTRY(rms_stat), ENTRY(rmsnorm_apply), ENTRY(rmsnorm_bwd), ENTRY(swiglu_fwd), ENTRY(swiglu_bwd),
+    ENTRY(rope_at), ENTRY(kv_append), ENTRY(attention_paged_fwd), ENTRY(rms_stat), ENTRY(rmsnorm_apply), ENTRY(rmsnorm_bwd), ENTRY(swiglu_fwd), ENTRY(swiglu_bwd),
     {"set_error", set_error, METH_O, "the exception type of failed calls"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
