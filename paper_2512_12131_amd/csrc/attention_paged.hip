@@ -1,90 +1,679 @@
-// Attention of each sequence's new tokens over its pages of a key / value cache, heads of 128, bf16 in / fp32 softmax.
-#include "common.h"
+// Causal attention of each sequence's new tokens over its pages of a key / value cache, heads of 128, bf16 in / fp32 softmax, for gfx950.
+//
+// Rows.  A sequence's n new tokens and the grp query heads that share a key / value head are n * grp rows against the same keys; row r is
+// token r / grp, head r % grp.  Up to 32 rows (decoding: single tokens, a few of them) are one narrow item of work, more are wide
+// items of 128 rows:
+//   narrow   a workgroup's four wavefronts take a quarter of the keys each, with all 32 rows, through LDS rings of their own and no barrier
+//            before the end, where they join their sums.  Bound by memory: every key and value is read once.
+//   wide     the four wavefronts take 32 rows each, keys and values pass through LDS in tiles of 64 for all of them.  Bound by the matrix
+//            and vector units.
+// Both compute S^T = K Q^T and O^T += V^T P^T on 32 x 32 x 16 MFMAs with the running maximum and sum of a softmax (one lane column per row),
+// as attention.hip does.
+//
+// Keys.  Nothing but the lists knows how long sequences are, and they stay on the device.  So every workgroup adds the work of all
+// sequences up by itself (64 of them at a time, one per lane), and sequences are cut into splits of equal length such that all of them
+// together are some rounds of the chip; a second kernel joins what was split, in the order of the splits.  No atomics: the same
+// lists give the same bits.
+//
+// Pages.  Eight keys that start at a multiple of eight lie in one page.  A lane looks one such group up and keeps its place in the cache in
+// units of 16 bytes; 64 groups (512 keys) are a window, the next one's page numbers are asked for while this one is worked on.  The place
+// becomes the base of a buffer descriptor that ends with the last key: rows past it, and pages that are none, arrive as zeros.
+#include "attn_tile.h"
 
 namespace lrb {
 namespace {
 
-constexpr int HD = 128;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr int R_NARROW = 32, R_WIDE = 128;
+constexpr int MIN_NARROW = 2, MIN_WIDE = 4;       // 64-key tiles of a split: 32 keys for each wavefront; what its fp32 sums cost
+constexpr int ROUNDS = 1024;                      // splits that all the work is cut into: two for each place on the chip
+constexpr int LDS_JOIN_LD = 132;                  // floats of a row of sums in LDS
+constexpr int LDS_BYTES = 4 * R_NARROW * LDS_JOIN_LD * 4 + 1024;
+static_assert(LDS_BYTES >= 4 * TILE_BYTES && LDS_BYTES <= 80 * 1024, "two workgroups share a CU");
+
+constexpr int AHEAD = 4;                          // MFMAs that their LDS operands are read ahead of
 
 struct PagedArgs {
   KvCache c;
   const uint16_t* q;
   uint16_t* o;
   float* lse;
-  int64_t ldq, ldo, T;
-  int H, grp;
+  float* part_o;          // [part_rows][128] unnormalised sums of splits
+  float2* part_ml;        // their maximum and sum
+  uint32_t part_rows;
+  int64_t ldq, ldo;
+  int T, H, grp, together;      // together: consecutive items on one XCD
+  FastDiv by_grp;
   float scale;
 };
+
+// The arguments once more, from where they are: what only the way in or out needs does not hold scalar registers in between (a hundred are too
+// few for everything, and those that do not fit would be read back lane by lane inside the loops).
+typedef const __attribute__((address_space(4))) PagedArgs* ArgPtr;
+__device__ __forceinline__ ArgPtr args_again() {
+  ArgPtr p = (ArgPtr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+__device__ __forceinline__ uint32_t div_by(uint32_t n, uint32_t mul, uint32_t shift) { return (uint32_t)(((uint64_t)n * mul) >> shift); }
 
 // The running maximum of a row that has seen no key: finite, so that no difference of two of them is undefined, and below any score whose
 // product with the exponent's factor c is finite.
 __device__ __forceinline__ float no_score(float c) { return -3.0e38f / fmaxf(c, 1.f); }
 
-// One wavefront per (token, head): 16 lanes hold a row's 128 columns, four keys at a time, each quarter with its own running
-// maximum and sum, joined at the end.
-__global__ __launch_bounds__(256) void paged_simple_kernel(PagedArgs a) {
+// ---- the split of the work ------------------------------------------------------------------------------
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t lo = __shfl_xor((uint32_t)x, d), hi = __shfl_xor((uint32_t)(x >> 32), d);
+    x += ((uint64_t)hi << 32) | lo;
+  }
+  return x;
+}
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {      // inclusive
   const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= a.T * a.H) return;
-  const int64_t t = item / a.H;
-  const int h = (int)(item % a.H), sub = lane & 15, quarter = lane >> 4;
-  int before = 0;
-  for (int i = 0; i < a.c.batch; i += 64) {
-    const bool in = i + lane < a.c.batch;
-    before += __popcll(__ballot(in && a.c.cu_q[in ? i + lane + 1 : 0] <= t));
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t y = __shfl_up(x, d);
+    x += lane >= d ? y : 0;
   }
-  if (before >= a.c.batch || a.c.cu_q[before] > t) return;
-  const int64_t end = a.c.cu_q[before + 1] < a.T ? a.c.cu_q[before + 1] : a.T;
-  int64_t keys = (int64_t)a.c.kv_len[before] - (end - t) + 1;
-  keys = keys < a.c.capacity ? keys : a.c.capacity;
-  const float c = a.scale * LOG2E;
-  float qv[8], m = no_score(c), l = 0.f, acc[8] = {};
-  unpack8(*reinterpret_cast<const uint4*>(a.q + t * a.ldq + h * HD + sub * 8), qv);
-  for (int64_t j = quarter; j < keys; j += 4) {
-    const int col = (int)a.c.by_page.div((uint32_t)j);
-    const int page = a.c.page_table[before * a.c.table_ld + col];
-    float kv[8] = {}, vv[8] = {};
-    if ((uint32_t)page < (uint32_t)a.c.n_pages) {
-      const int64_t at = page * a.c.page_stride + (j - (int64_t)col * a.c.page_size) * a.c.token_stride + h / a.grp * a.c.head_stride + sub * 8;
-      unpack8(*reinterpret_cast<const uint4*>(a.c.k + at), kv);
-      unpack8(*reinterpret_cast<const uint4*>(a.c.v + at), vv);
+  return x;
+}
+
+struct Seq {              // of one sequence
+  int tok0, n, kv;        // first token, new tokens, kv_len
+  int keys, tiles;        // keys that its last token sees, in 64-key tiles (at least one)
+  int rows, blocks;       // rows per key / value head and items of them
+};
+__device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
+  Seq s;
+  const int c0 = a.c.cu_q[b], c1 = a.c.cu_q[b + 1];
+  s.kv = a.c.kv_len[b];
+  s.tok0 = min(max(c0, 0), a.T);
+  s.n = max(min(max(c1, 0), a.T) - s.tok0, 0);
+  s.keys = (int)min((int64_t)max(s.kv, 0), a.c.capacity);
+  s.tiles = max((s.keys + KT - 1) / KT, 1);
+  s.rows = s.n * a.grp;                          // (below 2^31: T * H is)
+  s.blocks = s.rows <= R_NARROW ? (s.rows > 0) : (s.rows + R_WIDE - 1) / R_WIDE;
+  return s;
+}
+// 64-key tiles of a split
+struct SplitLen { uint32_t narrow, wide; };
+__device__ __forceinline__ SplitLen split_len(const PagedArgs& a) {
+  const int lane = threadIdx.x & 63;
+  uint64_t w = 0;
+  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    if (b0 + lane < a.c.batch) {
+      const Seq s = load_seq(a, b0 + lane);
+      w += (uint64_t)(uint32_t)s.blocks * (uint32_t)s.tiles;
     }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; i++) s = fmaf(qv[i], kv[i], s);
-    for (int d = 1; d < 16; d <<= 1) s += __shfl_xor(s, d);
-    const float mn = fmaxf(m, s), al = exp2f((m - mn) * c), p = exp2f((s - mn) * c);
-    l = l * al + p;
-#pragma unroll
-    for (int i = 0; i < 8; i++) acc[i] = acc[i] * al + p * vv[i];
-    m = mn;
   }
-  for (int d = 16; d < 64; d <<= 1) {
-    const float mo = __shfl_xor(m, d), lo = __shfl_xor(l, d), mn = fmaxf(m, mo);
-    const float al = exp2f((m - mn) * c), bl = exp2f((mo - mn) * c);
-    l = l * al + lo * bl;
+  w = wave_sum(w) * (uint32_t)a.c.n_kv_heads;
+  const uint32_t len = (uint32_t)uni((int)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu));
+  return SplitLen{max(len, (uint32_t)MIN_NARROW), max(len, (uint32_t)MIN_WIDE)};
+}
+__device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
+  const uint32_t len = s.rows <= R_NARROW ? l.narrow : l.wide;
+  return ((uint32_t)s.tiles + len - 1) / len;
+}
+// rows of sums that a sequence keeps: [key / value head][split][row]
+__device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& s, uint32_t splits) {
+  return splits > 1 ? (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.rows : 0;
+}
+
+// ---- pages ----------------------------------------------------------------------------------------------
+// The places of the 64 groups of one window and of the next.
+struct Pages {
+  uint32_t cur, nxt;
+  int raw;
+  int w;                  // index of the current window
+};
+struct PageSource {
+  const int32_t* row;     // of the page table
+  int keys;               // that are read at all
+  uint32_t head;          // of the key / value head, in units of 16 bytes
+};
+constexpr uint32_t NO_PLACE = 0xffffffffu;
+__device__ __forceinline__ int ask_pages(const PageSource& p, int w, int lane) {
+  const ArgPtr a = args_again();
+  const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u;
+  return key < (uint32_t)p.keys ? p.row[div_by(key, a->c.by_page.mul, a->c.by_page.shift)] : -1;
+}
+__device__ __forceinline__ uint32_t places(const PageSource& p, int w, int lane, int page) {
+  const ArgPtr a = args_again();
+  const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u;
+  const uint32_t in = key - div_by(key, a->c.by_page.mul, a->c.by_page.shift) * (uint32_t)a->c.page_size;
+  const uint64_t at = (uint64_t)(uint32_t)page * (uint64_t)(a->c.page_stride >> 3) + (uint64_t)in * (uint32_t)(a->c.token_stride >> 3) + p.head;
+  return (uint32_t)page < (uint32_t)a->c.n_pages ? (uint32_t)at : NO_PLACE;
+}
+// Descriptor of the keys of group g that are read, in K or V.
+__device__ __forceinline__ rsrc_t group_rsrc(uint32_t row_bytes, const uint16_t* base, const Pages& pg, int g, int end) {
+  const uint32_t c = __builtin_amdgcn_readlane(pg.cur, g & 63), n = __builtin_amdgcn_readlane(pg.nxt, g & 63);
+  const uint32_t at = (g >> 6) == pg.w ? c : n;
+  const int rows = min(end - g * 8, 8);
+  const uint64_t addr = (uint64_t)(uintptr_t)base + ((uint64_t)at << 4);
+  const uint32_t bytes = at != NO_PLACE && rows > 0 ? (uint32_t)(rows - 1) * row_bytes + 256u : 0u;
+  return rsrc_t{(uint32_t)addr, (uint32_t)(addr >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+
+// ---- one wavefront's share of a tile: 32 rows, NB blocks of 32 keys ------------------------------------------
+struct Rows {
+  f32x16 o[4];            // O^T: column = row of the wavefront
+  float m, l;             // running maximum; sum of this lane's keys
+};
+__device__ __forceinline__ void rows_init(Rows& s, float c) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) acc[i] = acc[i] * al + __shfl_xor(acc[i], d) * bl;
-    m = mn;
-  }
-  if (quarter == 0) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+  for (int hb = 0; hb < 4; hb++)
 #pragma unroll
-    for (int i = 0; i < 8; i++) acc[i] *= inv;
-    *reinterpret_cast<uint4*>(a.o + t * a.ldo + h * HD + sub * 8) = pack8(acc);
-    if (sub == 0 && a.lse) a.lse[t * a.H + h] = l > 0.f ? m * a.scale + logf(l) : -INFINITY;
+    for (int e = 0; e < 16; e++) s.o[hb][e] = 0.f;
+  s.m = no_score(c);
+  s.l = 0.f;
+}
+// queries: lane's row r in the B operand layout
+__device__ __forceinline__ void load_queries(bf16x8 (&qf)[8], const Seq& s, int kvh, int r, int lane) {
+  const ArgPtr a = args_again();
+  const bool ok = r < s.rows;
+  const int tok = ok ? (int)div_by((uint32_t)r, a->by_grp.mul, a->by_grp.shift) : 0, h = ok ? r - tok * a->grp : 0;
+  const uint16_t* p = a->q + (int64_t)(s.tok0 + tok) * a->ldq + (kvh * a->grp + h) * HD + (lane >> 5) * 8;
+#pragma unroll
+  for (int ks = 0; ks < 8; ks++)
+    qf[ks] = __builtin_bit_cast(bf16x8, ok ? *reinterpret_cast<const uint4*>(p + ks * 16) : make_uint4(0, 0, 0, 0));
+}
+// keys that row r sees
+__device__ __forceinline__ int row_limit(const Seq& s, int r) {
+  const ArgPtr a = args_again();
+  const int64_t lim = (int64_t)s.kv - s.n + (int)div_by((uint32_t)min(r, s.rows - 1), a->by_grp.mul, a->by_grp.shift) + 1;
+  return (int)min(max(lim, (int64_t)0), (int64_t)s.keys);
+}
+
+template <int NB>
+__device__ __forceinline__ void scores(f32x16 (&st)[NB], const bf16x8 (&qf)[8], const unsigned char* sK, int lane) {
+#pragma unroll
+  for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) st[nb][e] = 0.f;
+  bf16x8 fr[AHEAD];       // operands read ahead, slot i in fr[i % AHEAD]
+  auto read = [&](int i) { return swz_row_frag(sK, i % NB * 32, i / NB, lane); };
+#pragma unroll
+  for (int i = 0; i < AHEAD; i++) fr[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < 8 * NB; i++) {
+    st[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % AHEAD], qf[i / NB], st[i % NB], 0, 0, 0);
+    if (i + AHEAD < 8 * NB) fr[i % AHEAD] = read(i + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
   }
+}
+// Keys from the row's limit on: minus infinity.
+template <int NB>
+__device__ __forceinline__ void mask(f32x16 (&st)[NB], int lim, int lane) {
+#pragma unroll
+  for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) st[nb][e] = nb * 32 + acc_row(e, lane) >= lim ? -INFINITY : st[nb][e];
+}
+// Probabilities from scores, as bf16 operands (half a step, 2^-9 relative on average, is what their product with V on the matrix cores costs; the
+// sum adds them unrounded).
+template <int NB>
+__device__ __forceinline__ void softmax(Rows& s, f32x16 (&st)[NB], bf16x8 (&pf)[NB * 2], float c) {
+  float mx = st[0][0];
+#pragma unroll
+  for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) mx = fmaxf(mx, st[nb][e]);
+  const float mn = fmaxf(s.m, half_max(mx)), alpha = fast_exp2((s.m - mn) * c), mc = mn * c;
+  s.m = mn;
+  float sum = 0.f;
+#pragma unroll
+  for (int nb = 0; nb < NB; nb++)
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      st[nb][e] = fast_exp2(fmaf(st[nb][e], c, -mc));
+      sum += st[nb][e];
+    }
+  s.l = s.l * alpha + sum;
+#pragma unroll
+  for (int t = 0; t < NB * 2; t++) pf[t] = pack_acc_half(st[t >> 1], t & 1);
+  if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+    for (int hb = 0; hb < 4; hb++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) s.o[hb][e] *= alpha;
+  }
+}
+template <int NB>
+__device__ __forceinline__ void output(Rows& s, const bf16x8 (&pf)[NB * 2], const unsigned char* sV, int lane) {
+  bf16x8 fr[AHEAD];
+  auto read = [&](int i) { return swz_tr_frag(sV, (i >> 2) * 16, (i & 3) * 32, lane); };
+#pragma unroll
+  for (int i = 0; i < AHEAD; i++) fr[i] = read(i);
+#pragma unroll
+  for (int i = 0; i < 8 * NB; i++) {
+    s.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % AHEAD], pf[i >> 2], s.o[i & 3], 0, 0, 0);
+    if (i + AHEAD < 8 * NB) fr[i % AHEAD] = read(i + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+// A tile with keys that some rows must not see: there 0 * infinity and 0 * NaN would carry a later token's value into earlier rows.  Values
+// that are no numbers are taken out of the tile in LDS (16 bytes per lane and step, `bytes` of it from `at` on), and in the end added to the rows
+// that see them.
+__device__ __forceinline__ bool take_out(unsigned char* at, int bytes, int lane) {
+  uint32_t top = 0;
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  auto high = [&](uint32_t w) {
+    const u16x2 x = __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, w & 0x7fff7fffu));
+    top = __builtin_bit_cast(uint32_t, x);
+  };
+  for (int i = lane * 16; i < bytes; i += 1024) {
+    const uint4 q = *reinterpret_cast<const uint4*>(at + i);
+    high(q.x); high(q.y); high(q.z); high(q.w);
+  }
+  const bool bad = (top & 0xffffu) >= 0x7f80u || (top >> 16) >= 0x7f80u;
+  if (bad) {
+#pragma unroll 1
+    for (int i = lane * 16; i < bytes; i += 1024)
+#pragma unroll 1
+      for (int k = 0; k < 16; k += 2) {
+        uint16_t* x = reinterpret_cast<uint16_t*>(at + i + k);
+        if ((*x & 0x7f80u) == 0x7f80u) *x = 0;
+      }
+  }
+  return __builtin_amdgcn_ballot_w64(bad) != 0;
+}
+__device__ __forceinline__ void put_back(Rows& s, const int32_t* table, int kvh, int k0, int k1, int lim, int lane) {
+  const ArgPtr a = args_again();
+#pragma unroll 1
+  for (int k = k0; k < k1; k++) {
+    const int col = (int)div_by((uint32_t)k, a->c.by_page.mul, a->c.by_page.shift), page = table[col];
+    if ((uint32_t)page >= (uint32_t)a->c.n_pages) continue;
+    const uint16_t* p = a->c.v + page * a->c.page_stride + (int64_t)(k - col * a->c.page_size) * a->c.token_stride + kvh * a->c.head_stride + 4 * (lane >> 5);
+    auto seen = [&](uint32_t x) { return (x & 0x7f80u) == 0x7f80u && k < lim ? bf16_bits_to_f32(x) : 0.f; };
+#pragma unroll
+    for (int hb = 0; hb < 4; hb++)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; g4++) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p + hb * 32 + 8 * g4);
+        s.o[hb][g4 * 4] += seen(w.x & 0xffffu);
+        s.o[hb][g4 * 4 + 1] += seen(w.x >> 16);
+        s.o[hb][g4 * 4 + 2] += seen(w.y & 0xffffu);
+        s.o[hb][g4 * 4 + 3] += seen(w.y >> 16);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  }
+}
+
+// 4 consecutive columns of a row that is complete
+__device__ __forceinline__ void store4(uint16_t* p, float a, float b, float c, float d) {
+  uint2 w;
+  w.x = pack_bf16x2(a, b);
+  w.y = pack_bf16x2(c, d);
+  *reinterpret_cast<uint2*>(p) = w;
+}
+
+// All but the last N loads into LDS have landed; what was read from LDS is in registers.
+template <int N>
+__device__ __forceinline__ void landed() {
+  asm volatile("" ::: "memory");
+  wait_vm<N>();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void read_done() {
+  asm volatile("" ::: "memory");
+  wait_lgkm0();
+  asm volatile("" ::: "memory");
+}
+
+// ---- narrow items -----------------------------------------------------------------------------------------
+__device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, int kvh, int key_lo, int key_hi, bool whole,
+                                            uint32_t part0, unsigned char* smem) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6), r = lane & 31;
+  const ArgPtr in = args_again();
+  const uint16_t *cK = in->c.k, *cV = in->c.v;
+  const float c = in->scale * LOG2E;
+  const int blocks = (max(key_hi - key_lo, 0) + 31) / 32, share = (blocks + 3) / 4;
+  const int j0 = min(wave * share, blocks) + key_lo / 32, j1 = min((wave + 1) * share, blocks) + key_lo / 32;
+  const PageSource src = {table, key_hi, (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
+  unsigned char* sK = smem + wave * 16384;
+  unsigned char* sV = sK + 8192;
+  const uint32_t ldsK = (uint32_t)(uintptr_t)LRB_LDS_PTR(sK), ldsV = ldsK + 8192;
+  const int ts = (int)in->c.token_stride * 2, r4 = lane >> 4, pc = lane & 15;
+  uint32_t offK[4], offV[2];              // of load i: offK[i % 4], offV[i % 2]
+#pragma unroll
+  for (int i = 0; i < 4; i++) offK[i] = (uint32_t)(((i & 1) * 4 + r4) * ts + ((pc ^ (i * 4 + r4)) << 4));
+#pragma unroll
+  for (int i = 0; i < 2; i++) offV[i] = (uint32_t)((i * 4 + r4) * ts + ((pc ^ (r4 << 2)) << 4));
+
+  Rows st;
+  rows_init(st, c);
+  if (j0 < j1) {
+    bf16x8 qf[8];
+    load_queries(qf, s, kvh, r, lane);
+    const int lim = row_limit(s, r), lim0 = uni(row_limit(s, 0)), all = uni(row_limit(s, s.rows - 1));
+    Pages pg;
+    pg.w = j0 >> 4;
+    pg.raw = ask_pages(src, pg.w, lane);
+    const int raw1 = ask_pages(src, pg.w + 1, lane);
+    pg.cur = places(src, pg.w, lane, pg.raw);
+    pg.nxt = places(src, pg.w + 1, lane, raw1);
+    auto dma = [&](bool isV, int j) {     // 8 loads of 4 keys each; past the wavefront's keys: zeros, so that every block counts as many
+      const int end = j < j1 ? key_hi : 0;
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        const rsrc_t rs = group_rsrc((uint32_t)ts, isV ? cV : cK, pg, j * 4 + g, end);
+#pragma unroll
+        for (int i = g * 2; i < g * 2 + 2; i++) lds_dma_at(rs, (isV ? ldsV : ldsK) + i * 1024, isV ? offV[i & 1] : offK[i & 3]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    bool bad = false;
+    dma(false, j0);
+    dma(true, j0);
+    for (int j = j0; j < j1; j++) {
+      const int key0 = j * 32;
+      // windows of the next block's loads
+      if (((j + 1) & 15) == 0) {
+        pg.cur = pg.nxt;
+        pg.w++;
+        pg.raw = ask_pages(src, pg.w + 1, lane);
+      }
+      f32x16 x[1];
+      bf16x8 pf[2];
+      landed<8>();                        // K; behind it V
+      scores<1>(x, qf, sK, lane);
+      read_done();
+      dma(false, j + 1);
+      const bool masked = key0 + 32 > lim0;
+      if (masked) mask<1>(x, lim - key0, lane);
+      softmax<1>(st, x, pf, c);
+      if (((j + 1) & 15) == 0) pg.nxt = places(src, pg.w + 1, lane, pg.raw);
+      landed<8>();                        // V; behind it the next K
+      if (masked && lim0 < all) bad |= take_out(sV, 8192, lane);
+      output<1>(st, pf, sV, lane);
+      read_done();
+      dma(true, j + 1);
+    }
+    if (bad) put_back(st, table, kvh, max(j0 * 32, lim0 & ~31), min(min(j1 * 32, key_hi), all), lim, lane);
+  }
+  landed<0>();                            // no load is on its way into LDS
+  __syncthreads();
+  // the four wavefronts' sums, [wave][row][column]
+  float* sum = (float*)smem;
+  float2* ml = (float2*)(smem + 4 * R_NARROW * LDS_JOIN_LD * 4);
+  st.l = half_sum(st.l);
+  if (r < s.rows) {
+    float* p = sum + (wave * R_NARROW + r) * LDS_JOIN_LD;
+#pragma unroll
+    for (int hb = 0; hb < 4; hb++)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; g4++)
+        *reinterpret_cast<float4*>(p + hb * 32 + 8 * g4 + 4 * (lane >> 5)) =
+            make_float4(st.o[hb][g4 * 4], st.o[hb][g4 * 4 + 1], st.o[hb][g4 * 4 + 2], st.o[hb][g4 * 4 + 3]);
+    if (lane < 32) ml[wave * R_NARROW + r] = make_float2(st.m, st.l);
+  }
+  __syncthreads();
+  const ArgPtr a = args_again();
+  const int col = (tid & 31) * 4;
+  for (int row = tid >> 5; row < s.rows; row += 8) {
+    float2 w[4];
+    float m = no_score(c), l = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      w[i] = ml[i * R_NARROW + row];
+      m = fmaxf(m, w[i].x);
+    }
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const float f = fast_exp2((w[i].x - m) * c);
+      const float4 x = *reinterpret_cast<const float4*>(sum + (i * R_NARROW + row) * LDS_JOIN_LD + col);
+      l += w[i].y * f;
+      v[0] += x.x * f; v[1] += x.y * f; v[2] += x.z * f; v[3] += x.w * f;
+    }
+    if (whole) {
+      const int tok = (int)div_by((uint32_t)row, a->by_grp.mul, a->by_grp.shift), head = kvh * a->grp + row - tok * a->grp;
+      const int64_t t = s.tok0 + tok;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      store4(a->o + t * a->ldo + head * HD + col, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+      if (a->lse && col == 0) a->lse[t * a->H + head] = l == 0.f ? -INFINITY : m * a->scale + logf(l);
+    } else {
+      *reinterpret_cast<float4*>(a->part_o + (int64_t)(part0 + row) * HD + col) = make_float4(v[0], v[1], v[2], v[3]);
+      if (col == 0) a->part_ml[part0 + row] = make_float2(m, l);
+    }
+  }
+}
+
+// ---- wide items -------------------------------------------------------------------------------------------
+__device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, int kvh, int row0, int key_lo, int key_hi, bool whole,
+                                          uint32_t part0, unsigned char* smem) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
+  const ArgPtr in = args_again();
+  const uint16_t *cK = in->c.k, *cV = in->c.v;
+  const float c = in->scale * LOG2E;
+  const int wrow0 = row0 + wave * 32, r = wrow0 + (lane & 31);
+  const bool busy = wrow0 < s.rows;
+  const int lim = row_limit(s, r), lim0 = uni(row_limit(s, wrow0)), all = uni(row_limit(s, wrow0 + 31));
+  const int end = min(key_hi, uni(row_limit(s, row0 + R_WIDE - 1)));      // keys that any row of the item sees
+  const int first = uni(row_limit(s, row0));
+  const int t0 = key_lo / KT, t1 = max((end + KT - 1) / KT, t0);
+  const int tw = busy ? min(t1, max((min(all, end) + KT - 1) / KT, t0)) : t0;   // ... and of the wavefront
+  const PageSource src = {table, end, (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
+  const uint32_t lds0 = (uint32_t)(uintptr_t)LRB_LDS_PTR(smem) + (uint32_t)wave * 1024u;
+  const int ts = (int)in->c.token_stride * 2, r4 = lane >> 4, pc = lane & 15, rg = (wave & 1) * 4 + r4;
+  // load i of a tile: keys (i * 4 + wave) * 4 .., the same lane offset for every i
+  const uint32_t offK = (uint32_t)(rg * ts + ((pc ^ (wave * 4 + r4)) << 4)), offV = (uint32_t)(rg * ts + ((pc ^ (r4 << 2)) << 4));
+
+  Rows st;
+  rows_init(st, c);
+  bf16x8 qf[8];
+  load_queries(qf, s, kvh, r, lane);
+  Pages pg;
+  pg.w = t0 >> 3;
+  pg.raw = ask_pages(src, pg.w, lane);
+  const int raw1 = ask_pages(src, pg.w + 1, lane);
+  pg.cur = places(src, pg.w, lane, pg.raw);
+  pg.nxt = places(src, pg.w + 1, lane, raw1);
+  auto dma = [&](int t) {                 // K and V of tile t into the slots of its parity
+    const uint32_t slot = lds0 + (uint32_t)((t - t0) & 1) * TILE_BYTES;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int g = t * 8 + i * 2 + (wave >> 1);
+      lds_dma_at(group_rsrc((uint32_t)ts, cK, pg, g, end), slot + i * 4096, offK);
+      lds_dma_at(group_rsrc((uint32_t)ts, cV, pg, g, end), slot + 2 * TILE_BYTES + i * 4096, offV);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  bool bad = false;
+  if (t0 < t1) dma(t0);
+  for (int t = t0; t < t1; t++) {
+    landed<0>();
+    __syncthreads();                      // the tile has landed for everyone, and everyone has left the one before
+    if (((t + 1) & 7) == 0) {
+      pg.cur = pg.nxt;
+      pg.w++;
+      pg.raw = ask_pages(src, pg.w + 1, lane);
+    }
+    if (((t + 1) & 7) == 1 && t > t0) pg.nxt = places(src, pg.w + 1, lane, pg.raw);
+    if (t + 1 < t1) dma(t + 1);
+    unsigned char* sK = smem + ((t - t0) & 1) * TILE_BYTES;
+    unsigned char* sV = sK + 2 * TILE_BYTES;
+    const int key0 = t * KT;
+    if (key0 + KT > first && first < end) bad |= __syncthreads_or(take_out(sV + wave * 4096, 4096, lane)) != 0;
+    if (t >= tw) continue;
+    f32x16 x[2];
+    bf16x8 pf[4];
+    scores<2>(x, qf, sK, lane);
+    const bool masked = key0 + KT > lim0;
+    if (masked) mask<2>(x, lim - key0, lane);
+    softmax<2>(st, x, pf, c);
+    output<2>(st, pf, sV, lane);
+  }
+  wait_vm0();
+  if (bad && busy) put_back(st, table, kvh, max(t0 * KT, first & ~(KT - 1)), min(all, end), lim, lane);
+  const float l = half_sum(st.l);
+  if (r >= s.rows) return;
+  const ArgPtr a = args_again();
+  if (whole) {
+    const int tok = (int)div_by((uint32_t)r, a->by_grp.mul, a->by_grp.shift), head = kvh * a->grp + r - tok * a->grp;
+    const int64_t t = s.tok0 + tok;
+    store_acc_T(a->o + t * a->ldo + head * HD, st.o, l == 0.f ? 0.f : 1.f / l, lane);
+    if (a->lse && lane < 32) a->lse[t * a->H + head] = l == 0.f ? -INFINITY : st.m * a->scale + logf(l);
+  } else {
+    float* p = a->part_o + (int64_t)(part0 + r) * HD;
+#pragma unroll
+    for (int hb = 0; hb < 4; hb++)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; g4++)
+        *reinterpret_cast<float4*>(p + hb * 32 + 8 * g4 + 4 * (lane >> 5)) =
+            make_float4(st.o[hb][g4 * 4], st.o[hb][g4 * 4 + 1], st.o[hb][g4 * 4 + 2], st.o[hb][g4 * 4 + 3]);
+    if (lane < 32) a->part_ml[part0 + r] = make_float2(st.m, l);
+  }
+}
+
+// One workgroup per item: sequence, key / value head, split, block of rows (fastest, the last rows first).
+__global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int lane = threadIdx.x & 63;
+  const SplitLen len = split_len(a);
+  // the hardware deals workgroups to the 8 XCDs in rotation; `together` consecutive items stay on one
+  uint32_t v = blockIdx.x;
+  if (a.together > 1) {
+    const uint32_t x = v % 8, j = v / 8, n = (uint32_t)a.together;
+    v = (j / n * 8 + x) * n + j % n;
+  }
+  uint32_t item0 = 0, part0 = 0;
+  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    Seq s = {};
+    uint32_t splits = 0, items = 0, parts = 0;
+    if (b0 + lane < a.c.batch) {
+      s = load_seq(a, b0 + lane);
+      splits = splits_of(s, len);
+      items = (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.blocks;
+      parts = part_rows_of(a, s, splits);
+    }
+    const uint32_t item_end = item0 + wave_scan(items), part_end = part0 + wave_scan(parts);
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(v < item_end);
+    if (hit == 0) {
+      item0 = __builtin_amdgcn_readlane(item_end, 63);
+      part0 = __builtin_amdgcn_readlane(part_end, 63);
+      continue;
+    }
+    const int at = __builtin_ctzll(hit), b = b0 + at;
+    Seq q;
+    q.tok0 = __builtin_amdgcn_readlane(s.tok0, at); q.n = __builtin_amdgcn_readlane(s.n, at); q.kv = __builtin_amdgcn_readlane(s.kv, at);
+    q.keys = __builtin_amdgcn_readlane(s.keys, at); q.tiles = __builtin_amdgcn_readlane(s.tiles, at);
+    q.rows = __builtin_amdgcn_readlane(s.rows, at); q.blocks = __builtin_amdgcn_readlane(s.blocks, at);
+    splits = __builtin_amdgcn_readlane(splits, at);
+    items = __builtin_amdgcn_readlane(items, at);
+    parts = __builtin_amdgcn_readlane(parts, at);
+    const uint32_t local = v - (__builtin_amdgcn_readlane(item_end, at) - items), part = __builtin_amdgcn_readlane(part_end, at) - parts;
+    // (lists that are no batch's: nothing that has no room)
+    if (local >= items || part > a.part_rows || parts > a.part_rows - part) return;
+    const uint32_t per = splits * (uint32_t)q.blocks;
+    const int kvh = uni((int)(local / per));
+    const uint32_t rem = local - (uint32_t)kvh * per;
+    const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
+    const bool narrow = q.rows <= R_NARROW;
+    const int64_t l64 = (int64_t)(narrow ? len.narrow : len.wide) * KT;
+    const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
+    const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
+    const int32_t* table = a.c.page_table + (int64_t)b * a.c.table_ld;
+    if (narrow) narrow_item(q, table, kvh, lo, hi, splits == 1, p0, smem);
+    else wide_item(q, table, kvh, block * R_WIDE, lo, hi, splits == 1, p0, smem);
+    return;
+  }
+}
+
+// ---- joining the splits -------------------------------------------------------------------------------------
+// One wavefront per row (token and head), two columns per lane; a workgroup walks over the tokens.  Splits that a row's limit leaves
+// without keys have a sum of zero.
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
+  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+  const SplitLen len = split_len(a);
+  const float c = a.scale * LOG2E;
+  uint32_t part0 = 0;
+  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    Seq s = {};
+    uint32_t splits = 0, parts = 0;
+    if (b0 + lane < a.c.batch) {
+      s = load_seq(a, b0 + lane);
+      splits = splits_of(s, len);
+      parts = part_rows_of(a, s, splits);
+    }
+    const uint32_t part_end = part0 + wave_scan(parts);
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(parts > 0); todo; todo &= todo - 1) {
+      const int at = __builtin_ctzll(todo);
+      const int n = __builtin_amdgcn_readlane(s.n, at), tok0 = __builtin_amdgcn_readlane(s.tok0, at), rows = __builtin_amdgcn_readlane(s.rows, at);
+      const uint32_t sp = __builtin_amdgcn_readlane(splits, at), np = __builtin_amdgcn_readlane(parts, at),
+                     part = __builtin_amdgcn_readlane(part_end, at) - np;
+      if (part > a.part_rows || np > a.part_rows - part) continue;
+      for (int64_t i = (int64_t)blockIdx.x * 4 + wave; i < (int64_t)n * a.H; i += (int64_t)gridDim.x * 4) {
+        const int tok = uni((int)(i / a.H)), head = uni((int)(i % a.H)), kvh = uni((int)a.by_grp.div((uint32_t)head));
+        const uint32_t row = part + (uint32_t)kvh * sp * (uint32_t)rows + (uint32_t)(tok * a.grp + head - kvh * a.grp);
+        float m = no_score(c);
+        for (uint32_t k = lane; k < sp; k += 64) m = fmaxf(m, a.part_ml[row + k * (uint32_t)rows].x);
+        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+        float l = 0.f, x = 0.f, y = 0.f;
+#pragma unroll 4
+        for (uint32_t k = 0; k < sp; k++) {
+          const int64_t at_row = row + k * (uint32_t)rows;
+          const float2 w = a.part_ml[at_row];
+          const float2 v = *reinterpret_cast<const float2*>(a.part_o + at_row * HD + lane * 2);
+          const float f = w.y == 0.f ? 0.f : fast_exp2((w.x - m) * c);
+          l += w.y * f;
+          x += w.y == 0.f ? 0.f : v.x * f;
+          y += w.y == 0.f ? 0.f : v.y * f;
+        }
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const int64_t t = tok0 + tok;
+        *reinterpret_cast<uint32_t*>(a.o + t * a.ldo + head * HD + lane * 2) = pack_bf16x2(x * inv, y * inv);
+        if (a.lse && lane == 0) a.lse[t * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+      }
+    }
+    part0 = __builtin_amdgcn_readlane(part_end, 63);
+  }
+}
+
+// What can be said of a call without its lists.
+struct Bounds {
+  int64_t items, part_rows;
+  bool split;
+};
+Bounds bounds(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
+  const int64_t tiles = (capacity + KT - 1) / KT, rows = T * (H / Hkv);
+  const int64_t blocks = (batch < T ? batch : T) + rows / R_WIDE;      // of rows: a sequence's last one may be short
+  const int64_t most = (tiles + MIN_NARROW - 1) / MIN_NARROW;         // splits of a sequence
+  Bounds b;
+  b.split = most > 1;
+  b.items = Hkv * (most < 2 ? blocks : blocks * most < blocks + ROUNDS / Hkv + 1 ? blocks * most : blocks + ROUNDS / Hkv + 1);
+  // rows of sums: all rows in every split, or the splits there are at most (a sequence of several has no more than twice its share)
+  const int64_t all = T * H * most, some = 2 * (int64_t)ROUNDS * (rows < R_WIDE ? rows : R_WIDE);
+  b.part_rows = !b.split ? 0 : all < some ? all : some;
+  return b;
 }
 
 }  // namespace
 
-size_t attention_paged_ws_bytes(int64_t T, int H, int Hkv, int batch, int64_t capacity) { return 0; }
+size_t attention_paged_ws_bytes(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
+  return T == 0 || batch == 0 ? 0 : (size_t)bounds(T, H, Hkv, batch, capacity).part_rows * (HD * sizeof(float) + sizeof(float2));
+}
 
 hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int64_t T, int H, float scale,
                                 void* ws, hipStream_t st) {
-  PagedArgs a{c, (const uint16_t*)q, (uint16_t*)o, lse, ldq, ldo, T, H, H / c.n_kv_heads, scale};
-  hipLaunchKernelGGL(paged_simple_kernel, dim3((unsigned)((T * H + 3) / 4)), dim3(256), 0, st, a);
+  static const hipError_t attr_err = hipFuncSetAttribute((const void*)paged_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS_BYTES);
+  if (attr_err != hipSuccess) return attr_err;
+  const Bounds b = bounds(T, H, c.n_kv_heads, c.batch, c.capacity);
+  PagedArgs a;
+  a.c = c; a.q = (const uint16_t*)q; a.o = (uint16_t*)o; a.lse = lse;
+  a.part_rows = (uint32_t)b.part_rows;
+  a.part_o = (float*)ws;
+  a.part_ml = (float2*)((float*)ws + b.part_rows * HD);
+  a.ldq = ldq; a.ldo = ldo; a.T = (int)T; a.H = H; a.grp = H / c.n_kv_heads; a.scale = scale;
+  a.by_grp = FastDiv::of(a.grp);
+  a.together = T * a.grp >= 2 * (int64_t)R_WIDE * c.batch ? 16 : 1;
+  int64_t grid = b.items;
+  if (a.together > 1) grid = (grid + 8 * a.together - 1) / (8 * a.together) * (8 * a.together);
+  hipLaunchKernelGGL(paged_kernel, dim3((unsigned)grid), dim3(256), LDS_BYTES, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !b.split) return e;
+  const int64_t groups = (T * H + 3) / 4;
+  hipLaunchKernelGGL(paged_join_kernel, dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
