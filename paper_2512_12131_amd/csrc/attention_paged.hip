@@ -18,6 +18,8 @@
 // Pages.  Eight keys that start at a multiple of eight lie in one page.  A lane looks one such group up and keeps its place in the cache in
 // units of 16 bytes; 64 groups (512 keys) are a window, the next one's page numbers are asked for while this one is worked on.  The place
 // becomes the base of a buffer descriptor that ends with the last key: rows past it, and pages that are none, arrive as zeros.
+#include <algorithm>
+
 #include "attn_tile.h"
 
 namespace lrb {
@@ -62,21 +64,23 @@ __device__ __forceinline__ float no_score(float c) { return -3.0e38f / fmaxf(c, 
 
 // ---- the split of the work ------------------------------------------------------------------------------
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ uint64_t wave_sum(uint64_t x) {
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t lo = __shfl_xor((uint32_t)x, d), hi = __shfl_xor((uint32_t)(x >> 32), d);
-    x += ((uint64_t)hi << 32) | lo;
-  }
+// Inclusive sum over the lanes, in the vector unit's own lane moves (a shuffle goes through LDS: eighteen of them were 1.5 us on the way in).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  auto step = [&](auto Ctrl, auto Rows) {
+    constexpr int ctrl = decltype(Ctrl)::value, rows = decltype(Rows)::value;
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false);
+  };
+  using std::integral_constant;
+  using All = integral_constant<int, 0xf>;
+  step(integral_constant<int, 0x111>{}, All{});      // from 1, 2, 4, 8 lanes down within a row of 16
+  step(integral_constant<int, 0x112>{}, All{});
+  step(integral_constant<int, 0x114>{}, All{});
+  step(integral_constant<int, 0x118>{}, All{});
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // a row's last lane to the next row: rows 1 and 3
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // lane 31 to rows 2 and 3
   return x;
 }
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {      // inclusive
-  const int lane = threadIdx.x & 63;
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t y = __shfl_up(x, d);
-    x += lane >= d ? y : 0;
-  }
-  return x;
-}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return __builtin_amdgcn_readlane(x, 63); }
 
 struct Seq {              // of one sequence
   int tok0, n, kv;        // first token, new tokens, kv_len
@@ -101,13 +105,15 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a) {
   const int lane = threadIdx.x & 63;
   uint64_t w = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
+    uint64_t x = 0;
     if (b0 + lane < a.c.batch) {
       const Seq s = load_seq(a, b0 + lane);
-      w += (uint64_t)(uint32_t)s.blocks * (uint32_t)s.tiles;
+      x = min((uint64_t)(uint32_t)s.blocks * (uint32_t)s.tiles, (uint64_t)1 << 40);
     }
+    w += last_lane(wave_scan((uint32_t)x & 0xffffu)) + ((uint64_t)last_lane(wave_scan((uint32_t)(x >> 16))) << 16);
   }
-  w = wave_sum(w) * (uint32_t)a.c.n_kv_heads;
-  const uint32_t len = (uint32_t)uni((int)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu));
+  w *= (uint32_t)a.c.n_kv_heads;
+  const uint32_t len = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu);
   return SplitLen{max(len, (uint32_t)MIN_NARROW), max(len, (uint32_t)MIN_WIDE)};
 }
 __device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
@@ -550,8 +556,8 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
     const uint32_t item_end = item0 + wave_scan(items), part_end = part0 + wave_scan(parts);
     const uint64_t hit = __builtin_amdgcn_ballot_w64(v < item_end);
     if (hit == 0) {
-      item0 = __builtin_amdgcn_readlane(item_end, 63);
-      part0 = __builtin_amdgcn_readlane(part_end, 63);
+      item0 = last_lane(item_end);
+      part0 = last_lane(part_end);
       continue;
     }
     const int at = __builtin_ctzll(hit), b = b0 + at;
@@ -581,13 +587,19 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
 }
 
 // ---- joining the splits -------------------------------------------------------------------------------------
-// One wavefront per row (token and head), two columns per lane; a workgroup walks over the tokens.  Splits that a row's limit leaves
-// without keys have a sum of zero.
+// Rows (token and head) of the sequences that were split, numbered through; WAVES wavefronts per row share its splits out, two columns per
+// lane.  Splits that a row's limit leaves without keys have a sum of zero.
+constexpr int JOIN_BATCH = 8;      // splits whose sums are on their way at once
+
+template <int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
+  __shared__ float s_part[4][64 * 2 + 2];
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
   const SplitLen len = split_len(a);
   const float c = a.scale * LOG2E;
-  uint32_t part0 = 0;
+  uint32_t part0 = 0, row0 = 0;
+  uint32_t i = WAVES == 1 ? blockIdx.x * 4 + (uint32_t)wave : blockIdx.x;
+  const uint32_t stride = WAVES == 1 ? gridDim.x * 4 : gridDim.x;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
     Seq s = {};
     uint32_t splits = 0, parts = 0;
@@ -596,37 +608,68 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
       splits = splits_of(s, len);
       parts = part_rows_of(a, s, splits);
     }
-    const uint32_t part_end = part0 + wave_scan(parts);
-    for (uint64_t todo = __builtin_amdgcn_ballot_w64(parts > 0); todo; todo &= todo - 1) {
-      const int at = __builtin_ctzll(todo);
+    const uint32_t part_end = part0 + wave_scan(parts), row_end = row0 + wave_scan(parts > 0 ? (uint32_t)s.n * (uint32_t)a.H : 0);
+    part0 = last_lane(part_end);
+    row0 = last_lane(row_end);
+    for (; i < row0; i += stride) {
+      const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(i < row_end));
       const int n = __builtin_amdgcn_readlane(s.n, at), tok0 = __builtin_amdgcn_readlane(s.tok0, at), rows = __builtin_amdgcn_readlane(s.rows, at);
       const uint32_t sp = __builtin_amdgcn_readlane(splits, at), np = __builtin_amdgcn_readlane(parts, at),
                      part = __builtin_amdgcn_readlane(part_end, at) - np;
+      const uint32_t local = i - (__builtin_amdgcn_readlane(row_end, at) - (uint32_t)n * (uint32_t)a.H);
       if (part > a.part_rows || np > a.part_rows - part) continue;
-      for (int64_t i = (int64_t)blockIdx.x * 4 + wave; i < (int64_t)n * a.H; i += (int64_t)gridDim.x * 4) {
-        const int tok = uni((int)(i / a.H)), head = uni((int)(i % a.H)), kvh = uni((int)a.by_grp.div((uint32_t)head));
-        const uint32_t row = part + (uint32_t)kvh * sp * (uint32_t)rows + (uint32_t)(tok * a.grp + head - kvh * a.grp);
-        float m = no_score(c);
-        for (uint32_t k = lane; k < sp; k += 64) m = fmaxf(m, a.part_ml[row + k * (uint32_t)rows].x);
-        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-        float l = 0.f, x = 0.f, y = 0.f;
-#pragma unroll 4
-        for (uint32_t k = 0; k < sp; k++) {
-          const int64_t at_row = row + k * (uint32_t)rows;
-          const float2 w = a.part_ml[at_row];
-          const float2 v = *reinterpret_cast<const float2*>(a.part_o + at_row * HD + lane * 2);
-          const float f = w.y == 0.f ? 0.f : fast_exp2((w.x - m) * c);
-          l += w.y * f;
-          x += w.y == 0.f ? 0.f : v.x * f;
-          y += w.y == 0.f ? 0.f : v.y * f;
+      const int tok = uni((int)(local / (uint32_t)a.H)), head = uni((int)(local % (uint32_t)a.H)), kvh = uni((int)a.by_grp.div((uint32_t)head));
+      const uint32_t row = part + (uint32_t)kvh * sp * (uint32_t)rows + (uint32_t)(tok * a.grp + head - kvh * a.grp);
+      const uint32_t share = WAVES == 1 ? sp : (sp + WAVES - 1) / WAVES;
+      const uint32_t k0 = WAVES == 1 ? 0 : min((uint32_t)wave * share, sp), k1 = WAVES == 1 ? sp : min(k0 + share, sp);
+      float m = no_score(c), l = 0.f, x = 0.f, y = 0.f;
+      for (uint32_t k = k0; k < k1; k += JOIN_BATCH) {
+        float2 w[JOIN_BATCH], v[JOIN_BATCH];
+#pragma unroll
+        for (int j = 0; j < JOIN_BATCH; j++) {
+          const int64_t r = row + min(k + j, k1 - 1) * (uint32_t)rows;
+          w[j] = a.part_ml[r];
+          v[j] = *reinterpret_cast<const float2*>(a.part_o + r * HD + lane * 2);
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int64_t t = tok0 + tok;
-        *reinterpret_cast<uint32_t*>(a.o + t * a.ldo + head * HD + lane * 2) = pack_bf16x2(x * inv, y * inv);
-        if (a.lse && lane == 0) a.lse[t * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+        float mn = m;
+#pragma unroll
+        for (int j = 0; j < JOIN_BATCH; j++) mn = fmaxf(mn, w[j].x);
+        const float al = fast_exp2((m - mn) * c);
+        l *= al; x *= al; y *= al;
+        m = mn;
+#pragma unroll
+        for (int j = 0; j < JOIN_BATCH; j++) {
+          const float f = k + j < k1 && w[j].y != 0.f ? fast_exp2((w[j].x - m) * c) : 0.f;
+          l += f == 0.f ? 0.f : w[j].y * f;
+          x += f == 0.f ? 0.f : v[j].x * f;
+          y += f == 0.f ? 0.f : v[j].y * f;
+        }
       }
+      if constexpr (WAVES > 1) {
+        __syncthreads();                 // (the row before has been read)
+        s_part[wave][lane * 2] = x;
+        s_part[wave][lane * 2 + 1] = y;
+        if (lane == 0) { s_part[wave][128] = m; s_part[wave][129] = l; }
+        __syncthreads();
+        if (wave > 0) continue;
+        float mn = s_part[0][128];
+#pragma unroll
+        for (int j = 1; j < WAVES; j++) mn = fmaxf(mn, s_part[j][128]);
+        l = x = y = 0.f;
+#pragma unroll
+        for (int j = 0; j < WAVES; j++) {
+          const float f = fast_exp2((s_part[j][128] - mn) * c);
+          l += s_part[j][129] * f;
+          x += s_part[j][lane * 2] * f;
+          y += s_part[j][lane * 2 + 1] * f;
+        }
+        m = mn;
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const int64_t t = tok0 + tok;
+      *reinterpret_cast<uint32_t*>(a.o + t * a.ldo + head * HD + lane * 2) = pack_bf16x2(x * inv, y * inv);
+      if (a.lse && lane == 0) a.lse[t * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
     }
-    part0 = __builtin_amdgcn_readlane(part_end, 63);
   }
 }
 
@@ -672,8 +715,9 @@ hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, vo
   hipLaunchKernelGGL(paged_kernel, dim3((unsigned)grid), dim3(256), LDS_BYTES, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !b.split) return e;
-  const int64_t groups = (T * H + 3) / 4;
-  hipLaunchKernelGGL(paged_join_kernel, dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, a);
+  // four wavefronts per row where that leaves none without a place
+  if (T * H <= 2048) hipLaunchKernelGGL(paged_join_kernel<4>, dim3((unsigned)(T * H)), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(paged_join_kernel<1>, dim3((unsigned)std::min<int64_t>((T * H + 3) / 4, 2048)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
