@@ -19,6 +19,7 @@
 // units of 16 bytes; 64 groups (512 keys) are a window, the next one's page numbers are asked for while this one is worked on.  The place
 // becomes the base of a buffer descriptor that ends with the last key: rows past it, and pages that are none, arrive as zeros.
 #include <algorithm>
+#include <cmath>
 
 #include "attn_tile.h"
 
@@ -26,8 +27,8 @@ namespace lrb {
 namespace {
 
 constexpr int R_NARROW = 32, R_WIDE = 128;
-constexpr int MIN_NARROW = 2, MIN_WIDE = 4;       // 64-key tiles of a split: 32 keys for each wavefront; what its fp32 sums cost
-constexpr int ROUNDS = 1024;                      // splits that all the work is cut into: two for each place on the chip
+constexpr int MIN_SPLIT = 2;                      // 64-key tiles of a split: 32 keys for each wavefront of a narrow item
+constexpr int ROUNDS = 2048;                      // splits that all the work is cut into at most, four for each place on the chip
 constexpr int LDS_JOIN_LD = 132;                  // floats of a row of sums in LDS
 constexpr int LDS_BYTES = 4 * R_NARROW * LDS_JOIN_LD * 4 + 1024;
 static_assert(LDS_BYTES >= 4 * TILE_BYTES && LDS_BYTES <= 80 * 1024, "two workgroups share a CU");
@@ -99,9 +100,9 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
   s.blocks = s.rows <= R_NARROW ? (s.rows > 0) : (s.rows + R_WIDE - 1) / R_WIDE;
   return s;
 }
-// 64-key tiles of a split
-struct SplitLen { uint32_t narrow, wide; };
-__device__ __forceinline__ SplitLen split_len(const PagedArgs& a) {
+// 64-key tiles of a split, from the number w of them in all items: w / ROUNDS, but more than sqrt(w / 64).  A split's way in and out and its sums' way
+// through memory cost as much as some tiles, so of little work the splits are fewer: s splits save w (1 - 1 / s) and cost s.
+__device__ __forceinline__ uint32_t split_len(const PagedArgs& a) {
   const int lane = threadIdx.x & 63;
   uint64_t w = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
@@ -113,13 +114,10 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a) {
     w += last_lane(wave_scan((uint32_t)x & 0xffffu)) + ((uint64_t)last_lane(wave_scan((uint32_t)(x >> 16))) << 16);
   }
   w *= (uint32_t)a.c.n_kv_heads;
-  const uint32_t len = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu);
-  return SplitLen{max(len, (uint32_t)MIN_NARROW), max(len, (uint32_t)MIN_WIDE)};
+  const uint32_t even = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu), root = (uint32_t)uni((int)sqrtf((float)w * (1.f / 64.f))) + 1;
+  return max(max(even, root), (uint32_t)MIN_SPLIT);
 }
-__device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
-  const uint32_t len = s.rows <= R_NARROW ? l.narrow : l.wide;
-  return ((uint32_t)s.tiles + len - 1) / len;
-}
+__device__ __forceinline__ uint32_t splits_of(const Seq& s, uint32_t len) { return ((uint32_t)s.tiles + len - 1) / len; }
 // rows of sums that a sequence keeps: [key / value head][split][row]
 __device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& s, uint32_t splits) {
   return splits > 1 ? (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.rows : 0;
@@ -536,7 +534,7 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
 __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63;
-  const SplitLen len = split_len(a);
+  const uint32_t len = split_len(a);
   // the hardware deals workgroups to the 8 XCDs in rotation; `together` consecutive items stay on one
   uint32_t v = blockIdx.x;
   if (a.together > 1) {
@@ -575,12 +573,11 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
     const int kvh = uni((int)(local / per));
     const uint32_t rem = local - (uint32_t)kvh * per;
     const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
-    const bool narrow = q.rows <= R_NARROW;
-    const int64_t l64 = (int64_t)(narrow ? len.narrow : len.wide) * KT;
+    const int64_t l64 = (int64_t)len * KT;
     const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
     const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
     const int32_t* table = a.c.page_table + (int64_t)b * a.c.table_ld;
-    if (narrow) narrow_item(q, table, kvh, lo, hi, splits == 1, p0, smem);
+    if (q.rows <= R_NARROW) narrow_item(q, table, kvh, lo, hi, splits == 1, p0, smem);
     else wide_item(q, table, kvh, block * R_WIDE, lo, hi, splits == 1, p0, smem);
     return;
   }
@@ -595,7 +592,7 @@ template <int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
   __shared__ float s_part[4][64 * 2 + 2];
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
-  const SplitLen len = split_len(a);
+  const uint32_t len = split_len(a);
   const float c = a.scale * LOG2E;
   uint32_t part0 = 0, row0 = 0;
   uint32_t i = WAVES == 1 ? blockIdx.x * 4 + (uint32_t)wave : blockIdx.x;
@@ -681,13 +678,15 @@ struct Bounds {
 Bounds bounds(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
   const int64_t tiles = (capacity + KT - 1) / KT, rows = T * (H / Hkv);
   const int64_t blocks = (batch < T ? batch : T) + rows / R_WIDE;      // of rows: a sequence's last one may be short
-  const int64_t most = (tiles + MIN_NARROW - 1) / MIN_NARROW;         // splits of a sequence
+  const int64_t most = (tiles + MIN_SPLIT - 1) / MIN_SPLIT;           // splits of a sequence
+  // ... and of all: w / len, which grows with w, beside one for each item
+  const double w = (double)Hkv * (double)blocks * (double)tiles;
+  const int64_t cuts = std::min<int64_t>(ROUNDS, (int64_t)(8.0 * std::sqrt(w)) + 2);
   Bounds b;
   b.split = most > 1;
-  b.items = Hkv * (most < 2 ? blocks : blocks * most < blocks + ROUNDS / Hkv + 1 ? blocks * most : blocks + ROUNDS / Hkv + 1);
-  // rows of sums: all rows in every split, or the splits there are at most (a sequence of several has no more than twice its share)
-  const int64_t all = T * H * most, some = 2 * (int64_t)ROUNDS * (rows < R_WIDE ? rows : R_WIDE);
-  b.part_rows = !b.split ? 0 : all < some ? all : some;
+  b.items = std::min(Hkv * blocks * most, Hkv * blocks + cuts);
+  // rows of sums: all rows in every split, or those of the splits there are (a sequence of several has at most twice its share)
+  b.part_rows = b.split ? std::min(T * H * most, 2 * cuts * std::min<int64_t>(rows, R_WIDE)) : 0;
   return b;
 }
 
