@@ -124,38 +124,53 @@ __device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& 
 }
 
 // ---- pages ----------------------------------------------------------------------------------------------
-// The places of the 64 groups of one window and of the next.
+// Of the 64 groups of one window: place, bytes from there on that are read (0: none), and the next window's page numbers.
 struct Pages {
-  uint32_t cur, nxt;
+  uint32_t place, bytes;
   int raw;
-  int w;                  // index of the current window
 };
 struct PageSource {
   const int32_t* row;     // of the page table
-  int keys;               // that are read at all
+  int end;                // keys that are read end here
   uint32_t head;          // of the key / value head, in units of 16 bytes
 };
-constexpr uint32_t NO_PLACE = 0xffffffffu;
 __device__ __forceinline__ int ask_pages(const PageSource& p, int w, int lane) {
   const ArgPtr a = args_again();
   const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u;
-  return key < (uint32_t)p.keys ? p.row[div_by(key, a->c.by_page.mul, a->c.by_page.shift)] : -1;
+  return key < (uint32_t)p.end ? p.row[div_by(key, a->c.by_page.mul, a->c.by_page.shift)] : -1;
 }
-__device__ __forceinline__ uint32_t places(const PageSource& p, int w, int lane, int page) {
+__device__ __forceinline__ void places(Pages& pg, const PageSource& p, int w, int lane) {
   const ArgPtr a = args_again();
-  const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u;
+  const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u, row = (uint32_t)(a->c.token_stride >> 3);
   const uint32_t in = key - div_by(key, a->c.by_page.mul, a->c.by_page.shift) * (uint32_t)a->c.page_size;
-  const uint64_t at = (uint64_t)(uint32_t)page * (uint64_t)(a->c.page_stride >> 3) + (uint64_t)in * (uint32_t)(a->c.token_stride >> 3) + p.head;
-  return (uint32_t)page < (uint32_t)a->c.n_pages ? (uint32_t)at : NO_PLACE;
+  pg.place = (uint32_t)((uint64_t)(uint32_t)pg.raw * (uint64_t)(a->c.page_stride >> 3) + (uint64_t)in * row) + p.head;
+  const int rows = min(p.end - (int)key, 8);
+  pg.bytes = (uint32_t)pg.raw < (uint32_t)a->c.n_pages && rows > 0 ? (uint32_t)(rows - 1) * row * 16u + 256u : 0u;
 }
-// Descriptor of the keys of group g that are read, in K or V.
-__device__ __forceinline__ rsrc_t group_rsrc(uint32_t row_bytes, const uint16_t* base, const Pages& pg, int g, int end) {
-  const uint32_t c = __builtin_amdgcn_readlane(pg.cur, g & 63), n = __builtin_amdgcn_readlane(pg.nxt, g & 63);
-  const uint32_t at = (g >> 6) == pg.w ? c : n;
-  const int rows = min(end - g * 8, 8);
-  const uint64_t addr = (uint64_t)(uintptr_t)base + ((uint64_t)at << 4);
-  const uint32_t bytes = at != NO_PLACE && rows > 0 ? (uint32_t)(rows - 1) * row_bytes + 256u : 0u;
-  return rsrc_t{(uint32_t)addr, (uint32_t)(addr >> 32) & 0xffffu, bytes, 0x00020000u};
+// Before the loads of tile t, TILES of them to a window: the next window where t is its first one; its page numbers are asked for half a window ahead.
+template <int TILES>
+__device__ __forceinline__ void next_window(Pages& pg, const PageSource& p, int t, int lane) {
+  Pages n = pg;
+  if ((t & (TILES - 1)) == 0) places(n, p, t / TILES, lane);
+  else if ((t & (TILES - 1)) == TILES / 2) n.raw = ask_pages(p, t / TILES + 1, lane);
+  pg = n;
+}
+template <int TILES>
+__device__ __forceinline__ void first_window(Pages& pg, const PageSource& p, int t, int lane) {
+  pg.raw = ask_pages(p, t / TILES, lane);
+  const int next = ask_pages(p, t / TILES + 1, lane);
+  places(pg, p, t / TILES, lane);
+  pg.raw = next;
+}
+// Descriptors of a group's keys and values: the same place in both.
+struct Group { uint64_t at; uint32_t bytes; };
+__device__ __forceinline__ Group group(const Pages& pg, int g) {
+  const uint32_t place = __builtin_amdgcn_readlane(pg.place, g & 63), bytes = __builtin_amdgcn_readlane(pg.bytes, g & 63);
+  return Group{(uint64_t)place << 4, bytes};
+}
+__device__ __forceinline__ rsrc_t group_rsrc(const Group& g, const uint16_t* base) {
+  const uint64_t addr = (uint64_t)(uintptr_t)base + g.at;
+  return rsrc_t{(uint32_t)addr, (uint32_t)(addr >> 32), g.bytes, 0x00020000u};
 }
 
 // ---- one wavefront's share of a tile: 32 rows, NB blocks of 32 keys ------------------------------------------
@@ -190,17 +205,14 @@ __device__ __forceinline__ int row_limit(const Seq& s, int r) {
 
 template <int NB>
 __device__ __forceinline__ void scores(f32x16 (&st)[NB], const bf16x8 (&qf)[8], const unsigned char* sK, int lane) {
-#pragma unroll
-  for (int nb = 0; nb < NB; nb++)
-#pragma unroll
-    for (int e = 0; e < 16; e++) st[nb][e] = 0.f;
+  constexpr f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   bf16x8 fr[AHEAD];       // operands read ahead, slot i in fr[i % AHEAD]
   auto read = [&](int i) { return swz_row_frag(sK, i % NB * 32, i / NB, lane); };
 #pragma unroll
   for (int i = 0; i < AHEAD; i++) fr[i] = read(i);
 #pragma unroll
   for (int i = 0; i < 8 * NB; i++) {
-    st[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % AHEAD], qf[i / NB], st[i % NB], 0, 0, 0);
+    st[i % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[i % AHEAD], qf[i / NB], i < NB ? zero : st[i % NB], 0, 0, 0);
     if (i + AHEAD < 8 * NB) fr[i % AHEAD] = read(i + AHEAD);
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -208,10 +220,11 @@ __device__ __forceinline__ void scores(f32x16 (&st)[NB], const bf16x8 (&qf)[8], 
 // Keys from the row's limit on: minus infinity.
 template <int NB>
 __device__ __forceinline__ void mask(f32x16 (&st)[NB], int lim, int lane) {
+  lim -= 4 * (lane >> 5);
 #pragma unroll
   for (int nb = 0; nb < NB; nb++)
 #pragma unroll
-    for (int e = 0; e < 16; e++) st[nb][e] = nb * 32 + acc_row(e, lane) >= lim ? -INFINITY : st[nb][e];
+    for (int e = 0; e < 16; e++) st[nb][e] = nb * 32 + acc_row(e, 0) >= lim ? -INFINITY : st[nb][e];
 }
 // Probabilities from scores, as bf16 operands (half a step, 2^-9 relative on average, is what their product with V on the matrix cores costs; the
 // sum adds them unrounded).
@@ -333,7 +346,7 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
   const float c = in->scale * LOG2E;
   const int blocks = (max(key_hi - key_lo, 0) + 31) / 32, share = (blocks + 3) / 4;
   const int j0 = min(wave * share, blocks) + key_lo / 32, j1 = min((wave + 1) * share, blocks) + key_lo / 32;
-  const PageSource src = {table, key_hi, (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
+  const PageSource src = {table, min(key_hi, j1 * 32), (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
   unsigned char* sK = smem + wave * 16384;
   unsigned char* sV = sK + 8192;
   const uint32_t ldsK = (uint32_t)(uintptr_t)LRB_LDS_PTR(sK), ldsV = ldsK + 8192;
@@ -351,16 +364,11 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
     load_queries(qf, s, kvh, r, lane);
     const int lim = row_limit(s, r), lim0 = uni(row_limit(s, 0)), all = uni(row_limit(s, s.rows - 1));
     Pages pg;
-    pg.w = j0 >> 4;
-    pg.raw = ask_pages(src, pg.w, lane);
-    const int raw1 = ask_pages(src, pg.w + 1, lane);
-    pg.cur = places(src, pg.w, lane, pg.raw);
-    pg.nxt = places(src, pg.w + 1, lane, raw1);
+    first_window<16>(pg, src, j0, lane);
     auto dma = [&](bool isV, int j) {     // 8 loads of 4 keys each; past the wavefront's keys: zeros, so that every block counts as many
-      const int end = j < j1 ? key_hi : 0;
 #pragma unroll
       for (int g = 0; g < 4; g++) {
-        const rsrc_t rs = group_rsrc((uint32_t)ts, isV ? cV : cK, pg, j * 4 + g, end);
+        const rsrc_t rs = group_rsrc(group(pg, j * 4 + g), isV ? cV : cK);
 #pragma unroll
         for (int i = g * 2; i < g * 2 + 2; i++) lds_dma_at(rs, (isV ? ldsV : ldsK) + i * 1024, isV ? offV[i & 1] : offK[i & 3]);
         __builtin_amdgcn_sched_barrier(0);
@@ -371,22 +379,16 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
     dma(true, j0);
     for (int j = j0; j < j1; j++) {
       const int key0 = j * 32;
-      // windows of the next block's loads
-      if (((j + 1) & 15) == 0) {
-        pg.cur = pg.nxt;
-        pg.w++;
-        pg.raw = ask_pages(src, pg.w + 1, lane);
-      }
       f32x16 x[1];
       bf16x8 pf[2];
       landed<8>();                        // K; behind it V
       scores<1>(x, qf, sK, lane);
       read_done();
+      next_window<16>(pg, src, j + 1, lane);
       dma(false, j + 1);
       const bool masked = key0 + 32 > lim0;
       if (masked) mask<1>(x, lim - key0, lane);
       softmax<1>(st, x, pf, c);
-      if (((j + 1) & 15) == 0) pg.nxt = places(src, pg.w + 1, lane, pg.raw);
       landed<8>();                        // V; behind it the next K
       if (masked && lim0 < all) bad |= take_out(sV, 8192, lane);
       output<1>(st, pf, sV, lane);
@@ -444,6 +446,264 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
 }
 
 // ---- wide items -------------------------------------------------------------------------------------------
+struct WideTiles {
+  unsigned char* smem;
+  const uint16_t *cK, *cV;
+  uint32_t lds0, offK, offV;      // LDS address of the wavefront's first load; lane offsets in K and V, the same for every load
+  int t0, t1, tw;                 // 64-key tiles of the item, and the end of the wavefront's
+  int lim0, first, end;           // keys that the wavefront's and the item's first rows see, and that any row sees
+  int r, wave, lane;
+};
+// Takes what is no number out of V of tile t, if that has keys that some rows must not see.
+__device__ __forceinline__ bool careful(const WideTiles& w, int t) {
+  if (!(t * KT + KT > w.first && w.first < w.end)) return false;
+  return __syncthreads_or(take_out(w.smem + (2 + ((t - w.t0) & 1)) * TILE_BYTES + w.wave * 4096, 4096, w.lane)) != 0;
+}
+
+// A few tiles: one after the other.
+__device__ __forceinline__ bool wide_short(Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
+  Pages pg;
+  first_window<8>(pg, src, w.t0, w.lane);
+  auto dma = [&](int t) {                 // K and V of tile t into the slots of its parity
+    const uint32_t slot = w.lds0 + (uint32_t)((t - w.t0) & 1) * TILE_BYTES;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const Group g = group(pg, t * 8 + i * 2 + (w.wave >> 1));
+      lds_dma_at(group_rsrc(g, w.cK), slot + i * 4096, w.offK);
+      lds_dma_at(group_rsrc(g, w.cV), slot + 2 * TILE_BYTES + i * 4096, w.offV);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  bool bad = false;
+  if (w.t0 < w.t1) dma(w.t0);
+  for (int t = w.t0; t < w.t1; t++) {
+    landed<0>();
+    __syncthreads();                      // the tile has landed for everyone, and everyone has left the one before
+    if (t + 1 < w.t1) {
+      next_window<8>(pg, src, t + 1, w.lane);
+      dma(t + 1);
+    }
+    bad |= careful(w, t);
+    if (t >= w.tw) continue;
+    const unsigned char* sK = w.smem + ((t - w.t0) & 1) * TILE_BYTES;
+    f32x16 x[2];
+    bf16x8 pf[4];
+    scores<2>(x, qf, sK, w.lane);
+    if (t * KT + KT > w.lim0) mask<2>(x, row_limit(s, w.r) - t * KT, w.lane);
+    softmax<2>(st, x, pf, c);
+    output<2>(st, pf, sK + 2 * TILE_BYTES, w.lane);
+  }
+  return bad;
+}
+
+// An iteration works on two key tiles, as the dense forward's does: the scores of tile t + 1 and the output of tile t, with the softmax of tile t and
+// the maximum of the new scores threaded between their MFMAs, one barrier in the middle.
+constexpr int BARRIER = 12;
+constexpr int softmax_elems(int n) { return n < 0 ? 0 : n < 16 ? 5 * (n + 1) / 4 : n < 28 ? 5 + n : 32; }   // done by the end of slot n
+
+__device__ __forceinline__ bool wide_long(Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
+  unsigned char* const smem = w.smem;
+  const int t0 = w.t0, t1 = w.t1, tw = w.tw, lim0 = w.lim0, wave = w.wave, lane = w.lane;
+  Pages pk, pv;                           // windows of K's loads and of V's, which follow two tiles behind
+  first_window<8>(pk, src, t0, lane);
+  pv = pk;
+  auto dma = [&](bool isV, int t, int i) {      // load i of tile t into the slot of its parity; past the keys: zeros
+    lds_dma_at(group_rsrc(group(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), isV ? w.cV : w.cK),
+               w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096, isV ? w.offV : w.offK);
+  };
+  if (t0 < t1) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) dma(false, t0, i);
+#pragma unroll
+    for (int i = 0; i < 4; i++) dma(true, t0, i);
+    next_window<8>(pk, src, t0 + 1, lane);
+#pragma unroll
+    for (int i = 0; i < 4; i++) dma(false, t0 + 1, i);
+    next_window<8>(pk, src, t0 + 2, lane);
+  }
+  f32x16 sa[2], sb[2];                          // scores of the tile whose softmax comes next, and of the one after it
+  bf16x8 fr[AHEAD];                             // operands read ahead, slot n in fr[n % AHEAD]
+  float alpha = 1.f, mc = 0.f, sum = 0.f, plow = 0.f;
+  uint32_t pw[16];                              // probabilities as bf16 pairs
+  bool bad = false;
+  // operand of slot n: 0..15 scores (k16 step n / 2, key block n % 2), 16..31 output (16 keys each four slots)
+  auto read = [&](auto Nc, const unsigned char* sK, const unsigned char* sV) {
+    constexpr int n = decltype(Nc)::value;
+    if constexpr (n < 16) fr[n % AHEAD] = swz_row_frag(sK, (n & 1) * 32, n >> 1, lane);
+    else fr[n % AHEAD] = swz_tr_frag(sV, ((n - 16) >> 2) * 16, (n & 3) * 32, lane);
+  };
+  // maximum of a tile's scores from key0 on; mx where no key of it is hidden, else masked first
+  auto masked_max = [&](f32x16 (&x)[2], int key0, float mx) -> float {
+    if (key0 + KT > lim0) {
+      mask<2>(x, row_limit(s, w.r) - key0, lane);
+      mx = x[0][0];
+#pragma unroll
+      for (int nb = 0; nb < 2; nb++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) mx = fmaxf(mx, x[nb][e]);
+    }
+    return mx;
+  };
+  auto new_max = [&](float mx) {
+    const float mn = fmaxf(st.m, half_max(mx));
+    alpha = fast_exp2((st.m - mn) * c);
+    st.m = mn;
+    mc = mn * c;
+  };
+  auto rescale = [&] {
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+      for (int hb = 0; hb < 4; hb++)
+#pragma unroll
+        for (int e = 0; e < 16; e++) st.o[hb][e] *= alpha;
+    }
+  };
+  // everyone has read K of tile t + 1 and V of tile t - 1, and K of t + 2 and V of t have landed
+  auto turn = [&] {
+    read_done();
+    landed<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  auto next_loads = [&](int t, int i) {         // into the slots just left
+    if (i < 4) dma(true, t + 1, i);
+    else dma(false, t + 3, i - 4);
+  };
+  auto windows = [&](int t) {                   // of the loads of tile t's iteration
+    next_window<8>(pk, src, t + 3, lane);
+    const bool over = ((t + 1) & 7) == 0;
+    pv.place = over ? pk.place : pv.place;
+    pv.bytes = over ? pk.bytes : pv.bytes;
+  };
+  // elements F .. T - 1 of a tile's softmax
+  auto softmax_to = [&](const f32x16 (&x)[2], auto Fc, auto Tc) {
+    constexpr int f = decltype(Fc)::value, t = decltype(Tc)::value;
+    unroll_for<t - f>([&](auto I) {
+      constexpr int e = f + decltype(I)::value;
+      const float p = fast_exp2(fmaf(x[e >> 4][e & 15], c, -mc));
+      sum += p;
+      if constexpr (e & 1) pw[e >> 1] = pack_bf16x2(plow, p);
+      else plow = p;
+    });
+  };
+  auto out = [&](auto Nc) {
+    constexpr int n = decltype(Nc)::value, kk = (n - 16) >> 2;
+    const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[kk * 4], pw[kk * 4 + 1], pw[kk * 4 + 2], pw[kk * 4 + 3]));
+    st.o[n & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[n % AHEAD], pf, st.o[n & 3], 0, 0, 0);
+  };
+  // softmax and output of tile t (scores sc), scores of tile t + 1 (into sn).  LAST: near the end, where keys may be hidden
+  auto iteration = [&](int t, auto par, auto LAST, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
+    const unsigned char* sK1 = smem + (par ^ 1) * TILE_BYTES;             // K of tile t + 1
+    const unsigned char* sK2 = smem + par * TILE_BYTES;                   // K of tile t + 2
+    const unsigned char* sV = smem + (2 + par) * TILE_BYTES;              // V of tile t
+    windows(t);
+    rescale();
+    sum = 0.f;
+#pragma unroll
+    for (int nb = 0; nb < 2; nb++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) sn[nb][e] = 0.f;
+    float mx0 = -INFINITY, mx1 = -INFINITY;
+    unroll_for<32>([&](auto Nc) {
+      constexpr int n = decltype(Nc)::value;
+      if constexpr (n < 16) sn[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[n % AHEAD], qf[n >> 1], sn[n & 1], 0, 0, 0);
+      else out(Nc);
+      if constexpr (n == BARRIER) {
+        turn();
+        if constexpr (decltype(LAST)::value) bad |= careful(w, t);
+      }
+      // operands: V only from behind the barrier, then K of the tile after next
+      unroll_for<32>([&](auto I) {
+        constexpr int x = decltype(I)::value + AHEAD;               // slot that reads
+        constexpr int at = x - AHEAD < BARRIER && x >= 16 ? BARRIER : x - AHEAD;
+        if constexpr (at == n) {
+          if constexpr (x < 32) read(std::integral_constant<int, x>{}, sK1, sV);
+          else read(std::integral_constant<int, x - 32>{}, sK2, sV);
+        }
+      });
+      if constexpr (n > BARRIER && n <= BARRIER + 8) next_loads(t, n - BARRIER - 1);
+      softmax_to(sc, std::integral_constant<int, softmax_elems(n - 1)>{}, std::integral_constant<int, softmax_elems(n)>{});
+      if constexpr (n >= 18 && n < 26) {                            // maximum of the new scores
+        constexpr int e = (n - 18) * 2;
+        mx0 = fmaxf(fmaxf(mx0, sn[0][e]), sn[0][e + 1]);
+        mx1 = fmaxf(fmaxf(mx1, sn[1][e]), sn[1][e + 1]);
+      }
+      if constexpr (softmax_elems(n - 1) != softmax_elems(n)) asm volatile("" : "+v"(sum));
+      if constexpr (n == 25) asm volatile("" : "+v"(mx0), "+v"(mx1));
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    st.l = st.l * alpha + sum;
+    float mx = fmaxf(mx0, mx1);
+    if constexpr (decltype(LAST)::value) mx = masked_max(sn, (t + 1) * KT, mx);
+    new_max(mx);
+  };
+
+  landed<0>();
+  __syncthreads();
+  if (t0 < tw) {                                // scores of the first tile
+    scores<2>(sa, qf, smem, lane);
+    float mx = sa[0][0];
+#pragma unroll
+    for (int nb = 0; nb < 2; nb++)
+#pragma unroll
+      for (int e = 0; e < 16; e++) mx = fmaxf(mx, sa[nb][e]);
+    new_max(masked_max(sa, t0 * KT, mx));
+    if (t0 + 1 < tw) unroll_for<AHEAD>([&](auto I) { read(I, smem + TILE_BYTES, smem); });
+  }
+  read_done();
+  __builtin_amdgcn_s_barrier();                 // nobody reads K of the first tile any more
+  asm volatile("" ::: "memory");
+  if (t0 < t1) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) dma(false, t0 + 2, i);
+  }
+  const int plain = min(w.first / KT, tw);        // tiles without a hidden key
+  int t = t0;
+  for (; t + 2 < plain; t += 2) {
+    iteration(t, std::integral_constant<int, 0>{}, std::false_type{}, sa, sb);
+    iteration(t + 1, std::integral_constant<int, 1>{}, std::false_type{}, sb, sa);
+  }
+  for (; t + 1 < tw; t++) {
+    iteration(t, (t - t0) & 1, std::true_type{}, sa, sb);
+#pragma unroll
+    for (int nb = 0; nb < 2; nb++) sa[nb] = sb[nb];
+  }
+  if (t < tw) {                                 // this wavefront's last tile
+    const unsigned char* sV = smem + (2 + ((t - t0) & 1)) * TILE_BYTES;
+    windows(t);
+    rescale();
+    sum = 0.f;
+    turn();
+    bad |= careful(w, t);
+    unroll_for<AHEAD>([&](auto I) { read(std::integral_constant<int, 16 + decltype(I)::value>{}, smem, sV); });
+    if (t + 1 < t1) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) next_loads(t, i);
+    }
+    softmax_to(sa, std::integral_constant<int, 0>{}, std::integral_constant<int, 16>{});
+    unroll_for<16>([&](auto I) {
+      constexpr int n = 16 + decltype(I)::value;
+      out(std::integral_constant<int, n>{});
+      if constexpr (n + AHEAD < 32) read(std::integral_constant<int, n + AHEAD>{}, smem, sV);
+      if constexpr (n < 24) softmax_to(sa, std::integral_constant<int, 16 + (n - 16) * 2>{}, std::integral_constant<int, 18 + (n - 16) * 2>{});
+    });
+    st.l = st.l * alpha + sum;
+    t++;
+  }
+  for (; t < t1; t++) {                         // nothing left for this wavefront but its share of the loads
+    windows(t);
+    turn();
+    bad |= careful(w, t);
+    if (t + 1 < t1) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) next_loads(t, i);
+    }
+  }
+  return bad;
+}
+
+constexpr int LONG = 8;          // tiles from which on the long form is faster (its code and its way in are longer)
+
 __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, int kvh, int row0, int key_lo, int key_hi, bool whole,
                                           uint32_t part0, unsigned char* smem) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uni(tid >> 6);
@@ -452,7 +712,7 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   const float c = in->scale * LOG2E;
   const int wrow0 = row0 + wave * 32, r = wrow0 + (lane & 31);
   const bool busy = wrow0 < s.rows;
-  const int lim = row_limit(s, r), lim0 = uni(row_limit(s, wrow0)), all = uni(row_limit(s, wrow0 + 31));
+  const int lim0 = uni(row_limit(s, wrow0)), all = uni(row_limit(s, wrow0 + 31));
   const int end = min(key_hi, uni(row_limit(s, row0 + R_WIDE - 1)));      // keys that any row of the item sees
   const int first = uni(row_limit(s, row0));
   const int t0 = key_lo / KT, t1 = max((end + KT - 1) / KT, t0);
@@ -467,49 +727,10 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   rows_init(st, c);
   bf16x8 qf[8];
   load_queries(qf, s, kvh, r, lane);
-  Pages pg;
-  pg.w = t0 >> 3;
-  pg.raw = ask_pages(src, pg.w, lane);
-  const int raw1 = ask_pages(src, pg.w + 1, lane);
-  pg.cur = places(src, pg.w, lane, pg.raw);
-  pg.nxt = places(src, pg.w + 1, lane, raw1);
-  auto dma = [&](int t) {                 // K and V of tile t into the slots of its parity
-    const uint32_t slot = lds0 + (uint32_t)((t - t0) & 1) * TILE_BYTES;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const int g = t * 8 + i * 2 + (wave >> 1);
-      lds_dma_at(group_rsrc((uint32_t)ts, cK, pg, g, end), slot + i * 4096, offK);
-      lds_dma_at(group_rsrc((uint32_t)ts, cV, pg, g, end), slot + 2 * TILE_BYTES + i * 4096, offV);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-  bool bad = false;
-  if (t0 < t1) dma(t0);
-  for (int t = t0; t < t1; t++) {
-    landed<0>();
-    __syncthreads();                      // the tile has landed for everyone, and everyone has left the one before
-    if (((t + 1) & 7) == 0) {
-      pg.cur = pg.nxt;
-      pg.w++;
-      pg.raw = ask_pages(src, pg.w + 1, lane);
-    }
-    if (((t + 1) & 7) == 1 && t > t0) pg.nxt = places(src, pg.w + 1, lane, pg.raw);
-    if (t + 1 < t1) dma(t + 1);
-    unsigned char* sK = smem + ((t - t0) & 1) * TILE_BYTES;
-    unsigned char* sV = sK + 2 * TILE_BYTES;
-    const int key0 = t * KT;
-    if (key0 + KT > first && first < end) bad |= __syncthreads_or(take_out(sV + wave * 4096, 4096, lane)) != 0;
-    if (t >= tw) continue;
-    f32x16 x[2];
-    bf16x8 pf[4];
-    scores<2>(x, qf, sK, lane);
-    const bool masked = key0 + KT > lim0;
-    if (masked) mask<2>(x, lim - key0, lane);
-    softmax<2>(st, x, pf, c);
-    output<2>(st, pf, sV, lane);
-  }
-  wait_vm0();
-  if (bad && busy) put_back(st, table, kvh, max(t0 * KT, first & ~(KT - 1)), min(all, end), lim, lane);
+  const WideTiles w = {smem, cK, cV, lds0, offK, offV, t0, t1, tw, lim0, first, end, r, wave, lane};
+  const bool bad = t1 - t0 >= LONG ? wide_long(st, w, s, src, qf, c) : wide_short(st, w, s, src, qf, c);
+  landed<0>();
+  if (bad && busy) put_back(st, table, kvh, max(t0 * KT, first & ~(KT - 1)), min(all, end), row_limit(s, r), lane);
   const float l = half_sum(st.l);
   if (r >= s.rows) return;
   const ArgPtr a = args_again();
@@ -535,52 +756,55 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63;
   const uint32_t len = split_len(a);
-  // the hardware deals workgroups to the 8 XCDs in rotation; `together` consecutive items stay on one
+  // The hardware deals workgroups to the 8 XCDs in rotation; `together` consecutive items stay on one, not always the same one: the blocks of a
+  // prompt grow in work, and with eight such runs to a head one XCD had all the heaviest (4 x 4096 tokens: 1.04 ms).
   uint32_t v = blockIdx.x;
   if (a.together > 1) {
     const uint32_t x = v % 8, j = v / 8, n = (uint32_t)a.together;
-    v = (j / n * 8 + x) * n + j % n;
+    v = (j / n * 8 + (x + j / n) % 8) * n + j % n;
   }
-  uint32_t item0 = 0, part0 = 0;
-  for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    Seq s = {};
-    uint32_t splits = 0, items = 0, parts = 0;
+  uint32_t item0 = 0, part0 = 0, item_end, part_end, splits, items, parts;
+  uint64_t hit = 0;
+  int b0 = 0;
+  Seq s;
+  for (; b0 < a.c.batch; b0 += 64) {
+    s = Seq{};
+    splits = items = parts = 0;
     if (b0 + lane < a.c.batch) {
       s = load_seq(a, b0 + lane);
       splits = splits_of(s, len);
       items = (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.blocks;
       parts = part_rows_of(a, s, splits);
     }
-    const uint32_t item_end = item0 + wave_scan(items), part_end = part0 + wave_scan(parts);
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(v < item_end);
-    if (hit == 0) {
-      item0 = last_lane(item_end);
-      part0 = last_lane(part_end);
-      continue;
-    }
-    const int at = __builtin_ctzll(hit), b = b0 + at;
-    Seq q;
-    q.tok0 = __builtin_amdgcn_readlane(s.tok0, at); q.n = __builtin_amdgcn_readlane(s.n, at); q.kv = __builtin_amdgcn_readlane(s.kv, at);
-    q.keys = __builtin_amdgcn_readlane(s.keys, at); q.tiles = __builtin_amdgcn_readlane(s.tiles, at);
-    q.rows = __builtin_amdgcn_readlane(s.rows, at); q.blocks = __builtin_amdgcn_readlane(s.blocks, at);
-    splits = __builtin_amdgcn_readlane(splits, at);
-    items = __builtin_amdgcn_readlane(items, at);
-    parts = __builtin_amdgcn_readlane(parts, at);
-    const uint32_t local = v - (__builtin_amdgcn_readlane(item_end, at) - items), part = __builtin_amdgcn_readlane(part_end, at) - parts;
-    // (lists that are no batch's: nothing that has no room)
-    if (local >= items || part > a.part_rows || parts > a.part_rows - part) return;
-    const uint32_t per = splits * (uint32_t)q.blocks;
-    const int kvh = uni((int)(local / per));
-    const uint32_t rem = local - (uint32_t)kvh * per;
-    const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
-    const int64_t l64 = (int64_t)len * KT;
-    const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
-    const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
-    const int32_t* table = a.c.page_table + (int64_t)b * a.c.table_ld;
-    if (q.rows <= R_NARROW) narrow_item(q, table, kvh, lo, hi, splits == 1, p0, smem);
-    else wide_item(q, table, kvh, block * R_WIDE, lo, hi, splits == 1, p0, smem);
-    return;
+    item_end = item0 + wave_scan(items);
+    part_end = part0 + wave_scan(parts);
+    hit = __builtin_amdgcn_ballot_w64(v < item_end);
+    if (hit) break;
+    item0 = last_lane(item_end);
+    part0 = last_lane(part_end);
   }
+  if (hit == 0) return;
+  const int at = __builtin_ctzll(hit);
+  Seq q;
+  q.tok0 = __builtin_amdgcn_readlane(s.tok0, at); q.n = __builtin_amdgcn_readlane(s.n, at); q.kv = __builtin_amdgcn_readlane(s.kv, at);
+  q.keys = __builtin_amdgcn_readlane(s.keys, at); q.tiles = __builtin_amdgcn_readlane(s.tiles, at);
+  q.rows = __builtin_amdgcn_readlane(s.rows, at); q.blocks = __builtin_amdgcn_readlane(s.blocks, at);
+  splits = __builtin_amdgcn_readlane(splits, at);
+  items = __builtin_amdgcn_readlane(items, at);
+  parts = __builtin_amdgcn_readlane(parts, at);
+  const uint32_t local = v - (__builtin_amdgcn_readlane(item_end, at) - items), part = __builtin_amdgcn_readlane(part_end, at) - parts;
+  // (lists that are no batch's: nothing that has no room)
+  if (local >= items || part > a.part_rows || parts > a.part_rows - part) return;
+  const uint32_t per = splits * (uint32_t)q.blocks;
+  const int kvh = uni((int)(local / per));
+  const uint32_t rem = local - (uint32_t)kvh * per;
+  const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
+  const int64_t l64 = (int64_t)len * KT;
+  const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
+  const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
+  const int32_t* table = a.c.page_table + (int64_t)(b0 + at) * a.c.table_ld;
+  if (q.rows <= R_NARROW) narrow_item(q, table, kvh, lo, hi, splits == 1, p0, smem);
+  else wide_item(q, table, kvh, block * R_WIDE, lo, hi, splits == 1, p0, smem);
 }
 
 // ---- joining the splits -------------------------------------------------------------------------------------
