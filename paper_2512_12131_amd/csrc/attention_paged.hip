@@ -337,6 +337,12 @@ __device__ __forceinline__ void read_done() {
   asm volatile("" ::: "memory");
 }
 
+// lds_dma_at past the caches' retention: what is read once leaves room for nothing that is read again (decoding 64 sequences, 1.2 GB: 5.5 -> 6.1 TB/s;
+// a plain read of 4 GB reaches 6.3).
+__device__ __forceinline__ void lds_dma_once(rsrc_t rs, uint32_t lds, uint32_t voff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(voff), "s"(rs) : "m0", "memory");
+}
+
 // ---- narrow items -----------------------------------------------------------------------------------------
 __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, int kvh, int key_lo, int key_hi, bool whole,
                                             uint32_t part0, unsigned char* smem) {
@@ -370,7 +376,7 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
       for (int g = 0; g < 4; g++) {
         const rsrc_t rs = group_rsrc(group(pg, j * 4 + g), isV ? cV : cK);
 #pragma unroll
-        for (int i = g * 2; i < g * 2 + 2; i++) lds_dma_at(rs, (isV ? ldsV : ldsK) + i * 1024, isV ? offV[i & 1] : offK[i & 3]);
+        for (int i = g * 2; i < g * 2 + 2; i++) lds_dma_once(rs, (isV ? ldsV : ldsK) + i * 1024, isV ? offV[i & 1] : offK[i & 3]);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -799,7 +805,7 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   const int kvh = uni((int)(local / per));
   const uint32_t rem = local - (uint32_t)kvh * per;
   const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
-  const int64_t l64 = (int64_t)len * KT;
+  const int64_t l64 = (int64_t)(((uint32_t)q.tiles + splits - 1) / splits) * KT;      // (a sequence's splits are as even as they can be)
   const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
   const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
   const int32_t* table = a.c.page_table + (int64_t)(b0 + at) * a.c.table_ld;
@@ -808,18 +814,20 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
 }
 
 // ---- joining the splits -------------------------------------------------------------------------------------
-// Rows (token and head) of the sequences that were split, numbered through; WAVES wavefronts per row share its splits out, two columns per
-// lane.  Splits that a row's limit leaves without keys have a sum of zero.
-constexpr int JOIN_BATCH = 8;      // splits whose sums are on their way at once
+// Rows (token and head) of the sequences that were split, numbered through.  A row is half a wavefront's, four columns per lane, the halves on
+// neighbouring heads; WAVES wavefronts share a row's splits out.  Splits that a row's limit leaves without keys have a sum of zero.
+constexpr int JOIN_BATCH = 4;      // splits whose sums are on their way at once
 
 template <int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
-  __shared__ float s_part[4][64 * 2 + 2];
-  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6);
+  __shared__ float4 s_sum[4][64];
+  __shared__ float2 s_ml[4][2];
+  const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), half = lane >> 5, col = (lane & 31) * 4;
   const uint32_t len = split_len(a);
   const float c = a.scale * LOG2E;
-  uint32_t part0 = 0, row0 = 0;
-  uint32_t i = WAVES == 1 ? blockIdx.x * 4 + (uint32_t)wave : blockIdx.x;
+  const int pairs = (a.H + 1) / 2;
+  uint32_t part0 = 0, item0 = 0;
+  uint32_t i = WAVES == 1 ? blockIdx.x * 4 + (uint32_t)wave : blockIdx.x;      // (token, pair of heads)
   const uint32_t stride = WAVES == 1 ? gridDim.x * 4 : gridDim.x;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
     Seq s = {};
@@ -829,67 +837,78 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
       splits = splits_of(s, len);
       parts = part_rows_of(a, s, splits);
     }
-    const uint32_t part_end = part0 + wave_scan(parts), row_end = row0 + wave_scan(parts > 0 ? (uint32_t)s.n * (uint32_t)a.H : 0);
+    const uint32_t items = parts > 0 ? (uint32_t)s.n * (uint32_t)pairs : 0;
+    const uint32_t part_end = part0 + wave_scan(parts), item_end = item0 + wave_scan(items);
     part0 = last_lane(part_end);
-    row0 = last_lane(row_end);
-    for (; i < row0; i += stride) {
-      const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(i < row_end));
-      const int n = __builtin_amdgcn_readlane(s.n, at), tok0 = __builtin_amdgcn_readlane(s.tok0, at), rows = __builtin_amdgcn_readlane(s.rows, at);
-      const uint32_t sp = __builtin_amdgcn_readlane(splits, at), np = __builtin_amdgcn_readlane(parts, at),
-                     part = __builtin_amdgcn_readlane(part_end, at) - np;
-      const uint32_t local = i - (__builtin_amdgcn_readlane(row_end, at) - (uint32_t)n * (uint32_t)a.H);
+    item0 = last_lane(item_end);
+    for (; i < item0; i += stride) {
+      const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(i < item_end));
+      const int tok0 = __builtin_amdgcn_readlane(s.tok0, at);
+      const uint32_t rows = __builtin_amdgcn_readlane(s.rows, at), sp = __builtin_amdgcn_readlane(splits, at),
+                     np = __builtin_amdgcn_readlane(parts, at), part = __builtin_amdgcn_readlane(part_end, at) - np;
+      const uint32_t local = i - (__builtin_amdgcn_readlane(item_end, at) - __builtin_amdgcn_readlane(items, at));
       if (part > a.part_rows || np > a.part_rows - part) continue;
-      const int tok = uni((int)(local / (uint32_t)a.H)), head = uni((int)(local % (uint32_t)a.H)), kvh = uni((int)a.by_grp.div((uint32_t)head));
-      const uint32_t row = part + (uint32_t)kvh * sp * (uint32_t)rows + (uint32_t)(tok * a.grp + head - kvh * a.grp);
+      const int tok = uni((int)(local / (uint32_t)pairs)), head = uni((int)(local % (uint32_t)pairs)) * 2 + half;
+      const bool there = head < a.H;
+      const int kvh = (int)a.by_grp.div((uint32_t)(there ? head : a.H - 1)), in_grp = (there ? head : a.H - 1) - kvh * a.grp;
+      const int64_t row = part + (int64_t)((uint32_t)kvh * sp * rows) + (tok * a.grp + in_grp);
       const uint32_t share = WAVES == 1 ? sp : (sp + WAVES - 1) / WAVES;
       const uint32_t k0 = WAVES == 1 ? 0 : min((uint32_t)wave * share, sp), k1 = WAVES == 1 ? sp : min(k0 + share, sp);
-      float m = no_score(c), l = 0.f, x = 0.f, y = 0.f;
+      const float2* ml = a.part_ml + row;
+      const float* o = a.part_o + row * HD + col;
+      float m = no_score(c), l = 0.f;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
       for (uint32_t k = k0; k < k1; k += JOIN_BATCH) {
-        float2 w[JOIN_BATCH], v[JOIN_BATCH];
+        float2 w[JOIN_BATCH];
+        float4 v[JOIN_BATCH];
 #pragma unroll
         for (int j = 0; j < JOIN_BATCH; j++) {
-          const int64_t r = row + min(k + j, k1 - 1) * (uint32_t)rows;
-          w[j] = a.part_ml[r];
-          v[j] = *reinterpret_cast<const float2*>(a.part_o + r * HD + lane * 2);
+          w[j] = make_float2(m, 0.f);
+          if (k + j < k1) {
+            w[j] = ml[(k + j) * rows];
+            v[j] = *reinterpret_cast<const float4*>(o + (int64_t)((k + j) * rows) * HD);
+          }
         }
         float mn = m;
 #pragma unroll
         for (int j = 0; j < JOIN_BATCH; j++) mn = fmaxf(mn, w[j].x);
         const float al = fast_exp2((m - mn) * c);
-        l *= al; x *= al; y *= al;
+        l *= al; x.x *= al; x.y *= al; x.z *= al; x.w *= al;
         m = mn;
 #pragma unroll
         for (int j = 0; j < JOIN_BATCH; j++) {
-          const float f = k + j < k1 && w[j].y != 0.f ? fast_exp2((w[j].x - m) * c) : 0.f;
-          l += f == 0.f ? 0.f : w[j].y * f;
-          x += f == 0.f ? 0.f : v[j].x * f;
-          y += f == 0.f ? 0.f : v[j].y * f;
+          if (w[j].y == 0.f) continue;           // (nothing there, or no key: its sums were not formed)
+          const float f = fast_exp2((w[j].x - m) * c);
+          l += w[j].y * f;
+          x.x += v[j].x * f; x.y += v[j].y * f; x.z += v[j].z * f; x.w += v[j].w * f;
         }
       }
       if constexpr (WAVES > 1) {
         __syncthreads();                 // (the row before has been read)
-        s_part[wave][lane * 2] = x;
-        s_part[wave][lane * 2 + 1] = y;
-        if (lane == 0) { s_part[wave][128] = m; s_part[wave][129] = l; }
+        s_sum[wave][lane] = x;
+        if ((lane & 31) == 0) s_ml[wave][half] = make_float2(m, l);
         __syncthreads();
         if (wave > 0) continue;
-        float mn = s_part[0][128];
+        float mn = m;
 #pragma unroll
-        for (int j = 1; j < WAVES; j++) mn = fmaxf(mn, s_part[j][128]);
-        l = x = y = 0.f;
+        for (int j = 1; j < WAVES; j++) mn = fmaxf(mn, s_ml[j][half].x);
+        float f = fast_exp2((m - mn) * c);
+        l *= f; x.x *= f; x.y *= f; x.z *= f; x.w *= f;
 #pragma unroll
-        for (int j = 0; j < WAVES; j++) {
-          const float f = fast_exp2((s_part[j][128] - mn) * c);
-          l += s_part[j][129] * f;
-          x += s_part[j][lane * 2] * f;
-          y += s_part[j][lane * 2 + 1] * f;
+        for (int j = 1; j < WAVES; j++) {
+          const float2 w = s_ml[j][half];
+          const float4 v = s_sum[j][lane];
+          f = fast_exp2((w.x - mn) * c);
+          l += w.y * f;
+          x.x += v.x * f; x.y += v.y * f; x.z += v.z * f; x.w += v.w * f;
         }
         m = mn;
       }
+      if (!there) continue;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const int64_t t = tok0 + tok;
-      *reinterpret_cast<uint32_t*>(a.o + t * a.ldo + head * HD + lane * 2) = pack_bf16x2(x * inv, y * inv);
-      if (a.lse && lane == 0) a.lse[t * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
+      store4(a.o + t * a.ldo + head * HD + col, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+      if (a.lse && col == 0) a.lse[t * a.H + head] = l == 0.f ? -INFINITY : m * a.scale + logf(l);
     }
   }
 }
@@ -938,9 +957,10 @@ hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, vo
   hipLaunchKernelGGL(paged_kernel, dim3((unsigned)grid), dim3(256), LDS_BYTES, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !b.split) return e;
-  // four wavefronts per row where that leaves none without a place
-  if (T * H <= 2048) hipLaunchKernelGGL(paged_join_kernel<4>, dim3((unsigned)(T * H)), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(paged_join_kernel<1>, dim3((unsigned)std::min<int64_t>((T * H + 3) / 4, 2048)), dim3(256), 0, st, a);
+  // four wavefronts per pair of rows where the chip has places for all of them
+  const int64_t pairs = T * ((H + 1) / 2);
+  if (pairs <= 1024) hipLaunchKernelGGL(paged_join_kernel<4>, dim3((unsigned)pairs), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(paged_join_kernel<1>, dim3((unsigned)std::min<int64_t>((pairs + 3) / 4, 2048)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
