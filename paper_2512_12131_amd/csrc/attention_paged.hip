@@ -117,7 +117,8 @@ __device__ __forceinline__ uint32_t split_len(const PagedArgs& a) {
   const uint32_t even = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu), root = (uint32_t)uni((int)sqrtf((float)w * (1.f / 64.f))) + 1;
   return max(max(even, root), (uint32_t)MIN_SPLIT);
 }
-__device__ __forceinline__ uint32_t splits_of(const Seq& s, uint32_t len) { return ((uint32_t)s.tiles + len - 1) / len; }
+// (rounded to the nearer number, and as even as they can be)
+__device__ __forceinline__ uint32_t splits_of(const Seq& s, uint32_t len) { return max(((uint32_t)s.tiles + len / 2) / len, 1u); }
 // rows of sums that a sequence keeps: [key / value head][split][row]
 __device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& s, uint32_t splits) {
   return splits > 1 ? (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.rows : 0;
@@ -805,7 +806,7 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   const int kvh = uni((int)(local / per));
   const uint32_t rem = local - (uint32_t)kvh * per;
   const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
-  const int64_t l64 = (int64_t)(((uint32_t)q.tiles + splits - 1) / splits) * KT;      // (a sequence's splits are as even as they can be)
+  const int64_t l64 = (int64_t)(((uint32_t)q.tiles + splits - 1) / splits) * KT;
   const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
   const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
   const int32_t* table = a.c.page_table + (int64_t)(b0 + at) * a.c.table_ld;
