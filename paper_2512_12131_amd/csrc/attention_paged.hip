@@ -29,6 +29,7 @@ namespace {
 constexpr int R_NARROW = 32, R_WIDE = 128;
 constexpr int MIN_SPLIT = 2;                      // 64-key tiles of a split: 32 keys for each wavefront of a narrow item
 constexpr int ROUNDS = 2048;                      // splits that all the work is cut into at most, four for each place on the chip
+constexpr uint32_t RUN = 16;                      // blocks of rows that read the same keys on one XCD at a time
 constexpr int LDS_JOIN_LD = 132;                  // floats of a row of sums in LDS
 constexpr int LDS_BYTES = 4 * R_NARROW * LDS_JOIN_LD * 4 + 1024;
 static_assert(LDS_BYTES >= 4 * TILE_BYTES && LDS_BYTES <= 80 * 1024, "two workgroups share a CU");
@@ -44,7 +45,7 @@ struct PagedArgs {
   float2* part_ml;        // their maximum and sum
   uint32_t part_rows;
   int64_t ldq, ldo;
-  int T, H, grp, together;      // together: consecutive items on one XCD
+  int T, H, grp, runs;          // runs: consecutive items on one XCD
   FastDiv by_grp;
   float scale;
 };
@@ -102,13 +103,14 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
 }
 // 64-key tiles of a split, from the number w of them in all items: w / ROUNDS, but more than sqrt(w / 64).  A split's way in and out and its sums' way
 // through memory cost as much as some tiles, so of little work the splits are fewer: s splits save w (1 - 1 / s) and cost s.
-__device__ __forceinline__ uint32_t split_len(const PagedArgs& a) {
+// first: of the lane's sequence among the first 64, loaded already.
+__device__ __forceinline__ uint32_t split_len(const PagedArgs& a, const Seq& first) {
   const int lane = threadIdx.x & 63;
   uint64_t w = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
     uint64_t x = 0;
     if (b0 + lane < a.c.batch) {
-      const Seq s = load_seq(a, b0 + lane);
+      const Seq s = b0 == 0 ? first : load_seq(a, b0 + lane);
       x = min((uint64_t)(uint32_t)s.blocks * (uint32_t)s.tiles, (uint64_t)1 << 40);
     }
     w += last_lane(wave_scan((uint32_t)x & 0xffffu)) + ((uint64_t)last_lane(wave_scan((uint32_t)(x >> 16))) << 16);
@@ -135,13 +137,11 @@ struct PageSource {
   int end;                // keys that are read end here
   uint32_t head;          // of the key / value head, in units of 16 bytes
 };
-__device__ __forceinline__ int ask_pages(const PageSource& p, int w, int lane) {
-  const ArgPtr a = args_again();
+__device__ __forceinline__ int ask_pages(ArgPtr a, const PageSource& p, int w, int lane) {
   const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u;
   return key < (uint32_t)p.end ? p.row[div_by(key, a->c.by_page.mul, a->c.by_page.shift)] : -1;
 }
-__device__ __forceinline__ void places(Pages& pg, const PageSource& p, int w, int lane) {
-  const ArgPtr a = args_again();
+__device__ __forceinline__ void places(ArgPtr a, Pages& pg, const PageSource& p, int w, int lane) {
   const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u, row = (uint32_t)(a->c.token_stride >> 3);
   const uint32_t in = key - div_by(key, a->c.by_page.mul, a->c.by_page.shift) * (uint32_t)a->c.page_size;
   pg.place = (uint32_t)((uint64_t)(uint32_t)pg.raw * (uint64_t)(a->c.page_stride >> 3) + (uint64_t)in * row) + p.head;
@@ -152,15 +152,15 @@ __device__ __forceinline__ void places(Pages& pg, const PageSource& p, int w, in
 template <int TILES>
 __device__ __forceinline__ void next_window(Pages& pg, const PageSource& p, int t, int lane) {
   Pages n = pg;
-  if ((t & (TILES - 1)) == 0) places(n, p, t / TILES, lane);
-  else if ((t & (TILES - 1)) == TILES / 2) n.raw = ask_pages(p, t / TILES + 1, lane);
+  if ((t & (TILES - 1)) == 0) places(args_again(), n, p, t / TILES, lane);
+  else if ((t & (TILES - 1)) == TILES / 2) n.raw = ask_pages(args_again(), p, t / TILES + 1, lane);
   pg = n;
 }
 template <int TILES>
-__device__ __forceinline__ void first_window(Pages& pg, const PageSource& p, int t, int lane) {
-  pg.raw = ask_pages(p, t / TILES, lane);
-  const int next = ask_pages(p, t / TILES + 1, lane);
-  places(pg, p, t / TILES, lane);
+__device__ __forceinline__ void first_window(ArgPtr a, Pages& pg, const PageSource& p, int t, int lane) {
+  pg.raw = ask_pages(a, p, t / TILES, lane);
+  const int next = ask_pages(a, p, t / TILES + 1, lane);
+  places(a, pg, p, t / TILES, lane);
   pg.raw = next;
 }
 // Descriptors of a group's keys and values: the same place in both.
@@ -188,8 +188,7 @@ __device__ __forceinline__ void rows_init(Rows& s, float c) {
   s.l = 0.f;
 }
 // queries: lane's row r in the B operand layout
-__device__ __forceinline__ void load_queries(bf16x8 (&qf)[8], const Seq& s, int kvh, int r, int lane) {
-  const ArgPtr a = args_again();
+__device__ __forceinline__ void load_queries(ArgPtr a, bf16x8 (&qf)[8], const Seq& s, int kvh, int r, int lane) {
   const bool ok = r < s.rows;
   const int tok = ok ? (int)div_by((uint32_t)r, a->by_grp.mul, a->by_grp.shift) : 0, h = ok ? r - tok * a->grp : 0;
   const uint16_t* p = a->q + (int64_t)(s.tok0 + tok) * a->ldq + (kvh * a->grp + h) * HD + (lane >> 5) * 8;
@@ -198,8 +197,7 @@ __device__ __forceinline__ void load_queries(bf16x8 (&qf)[8], const Seq& s, int 
     qf[ks] = __builtin_bit_cast(bf16x8, ok ? *reinterpret_cast<const uint4*>(p + ks * 16) : make_uint4(0, 0, 0, 0));
 }
 // keys that row r sees
-__device__ __forceinline__ int row_limit(const Seq& s, int r) {
-  const ArgPtr a = args_again();
+__device__ __forceinline__ int row_limit(ArgPtr a, const Seq& s, int r) {
   const int64_t lim = (int64_t)s.kv - s.n + (int)div_by((uint32_t)min(r, s.rows - 1), a->by_grp.mul, a->by_grp.shift) + 1;
   return (int)min(max(lim, (int64_t)0), (int64_t)s.keys);
 }
@@ -368,10 +366,10 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
   rows_init(st, c);
   if (j0 < j1) {
     bf16x8 qf[8];
-    load_queries(qf, s, kvh, r, lane);
-    const int lim = row_limit(s, r), lim0 = uni(row_limit(s, 0)), all = uni(row_limit(s, s.rows - 1));
+    load_queries(in, qf, s, kvh, r, lane);
+    const int lim = row_limit(in, s, r), lim0 = uni(row_limit(in, s, 0)), all = uni(row_limit(in, s, s.rows - 1));
     Pages pg;
-    first_window<16>(pg, src, j0, lane);
+    first_window<16>(in, pg, src, j0, lane);
     auto dma = [&](bool isV, int j) {     // 8 loads of 4 keys each; past the wavefront's keys: zeros, so that every block counts as many
 #pragma unroll
       for (int g = 0; g < 4; g++) {
@@ -468,9 +466,9 @@ __device__ __forceinline__ bool careful(const WideTiles& w, int t) {
 }
 
 // A few tiles: one after the other.
-__device__ __forceinline__ bool wide_short(Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
+__device__ __forceinline__ bool wide_short(ArgPtr in, Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
   Pages pg;
-  first_window<8>(pg, src, w.t0, w.lane);
+  first_window<8>(in, pg, src, w.t0, w.lane);
   auto dma = [&](int t) {                 // K and V of tile t into the slots of its parity
     const uint32_t slot = w.lds0 + (uint32_t)((t - w.t0) & 1) * TILE_BYTES;
 #pragma unroll
@@ -496,7 +494,7 @@ __device__ __forceinline__ bool wide_short(Rows& st, const WideTiles& w, const S
     f32x16 x[2];
     bf16x8 pf[4];
     scores<2>(x, qf, sK, w.lane);
-    if (t * KT + KT > w.lim0) mask<2>(x, row_limit(s, w.r) - t * KT, w.lane);
+    if (t * KT + KT > w.lim0) mask<2>(x, row_limit(args_again(), s, w.r) - t * KT, w.lane);
     softmax<2>(st, x, pf, c);
     output<2>(st, pf, sK + 2 * TILE_BYTES, w.lane);
   }
@@ -508,11 +506,11 @@ __device__ __forceinline__ bool wide_short(Rows& st, const WideTiles& w, const S
 constexpr int BARRIER = 12;
 constexpr int softmax_elems(int n) { return n < 0 ? 0 : n < 16 ? 5 * (n + 1) / 4 : n < 28 ? 5 + n : 32; }   // done by the end of slot n
 
-__device__ __forceinline__ bool wide_long(Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
+__device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
   unsigned char* const smem = w.smem;
   const int t0 = w.t0, t1 = w.t1, tw = w.tw, lim0 = w.lim0, wave = w.wave, lane = w.lane;
   Pages pk, pv;                           // windows of K's loads and of V's, which follow two tiles behind
-  first_window<8>(pk, src, t0, lane);
+  first_window<8>(in, pk, src, t0, lane);
   pv = pk;
   auto dma = [&](bool isV, int t, int i) {      // load i of tile t into the slot of its parity; past the keys: zeros
     lds_dma_at(group_rsrc(group(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), isV ? w.cV : w.cK),
@@ -542,7 +540,7 @@ __device__ __forceinline__ bool wide_long(Rows& st, const WideTiles& w, const Se
   // maximum of a tile's scores from key0 on; mx where no key of it is hidden, else masked first
   auto masked_max = [&](f32x16 (&x)[2], int key0, float mx) -> float {
     if (key0 + KT > lim0) {
-      mask<2>(x, row_limit(s, w.r) - key0, lane);
+      mask<2>(x, row_limit(args_again(), s, w.r) - key0, lane);
       mx = x[0][0];
 #pragma unroll
       for (int nb = 0; nb < 2; nb++)
@@ -719,9 +717,9 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   const float c = in->scale * LOG2E;
   const int wrow0 = row0 + wave * 32, r = wrow0 + (lane & 31);
   const bool busy = wrow0 < s.rows;
-  const int lim0 = uni(row_limit(s, wrow0)), all = uni(row_limit(s, wrow0 + 31));
-  const int end = min(key_hi, uni(row_limit(s, row0 + R_WIDE - 1)));      // keys that any row of the item sees
-  const int first = uni(row_limit(s, row0));
+  const int lim0 = uni(row_limit(in, s, wrow0)), all = uni(row_limit(in, s, wrow0 + 31));
+  const int end = min(key_hi, uni(row_limit(in, s, row0 + R_WIDE - 1)));      // keys that any row of the item sees
+  const int first = uni(row_limit(in, s, row0));
   const int t0 = key_lo / KT, t1 = max((end + KT - 1) / KT, t0);
   const int tw = busy ? min(t1, max((min(all, end) + KT - 1) / KT, t0)) : t0;   // ... and of the wavefront
   const PageSource src = {table, end, (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
@@ -733,11 +731,11 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   Rows st;
   rows_init(st, c);
   bf16x8 qf[8];
-  load_queries(qf, s, kvh, r, lane);
+  load_queries(in, qf, s, kvh, r, lane);
   const WideTiles w = {smem, cK, cV, lds0, offK, offV, t0, t1, tw, lim0, first, end, r, wave, lane};
-  const bool bad = t1 - t0 >= LONG ? wide_long(st, w, s, src, qf, c) : wide_short(st, w, s, src, qf, c);
+  const bool bad = t1 - t0 >= LONG ? wide_long(in, st, w, s, src, qf, c) : wide_short(in, st, w, s, src, qf, c);
   landed<0>();
-  if (bad && busy) put_back(st, table, kvh, max(t0 * KT, first & ~(KT - 1)), min(all, end), row_limit(s, r), lane);
+  if (bad && busy) put_back(st, table, kvh, max(t0 * KT, first & ~(KT - 1)), min(all, end), row_limit(args_again(), s, r), lane);
   const float l = half_sum(st.l);
   if (r >= s.rows) return;
   const ArgPtr a = args_again();
@@ -758,27 +756,27 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   }
 }
 
-// One workgroup per item: sequence, key / value head, split, block of rows (fastest, the last rows first).
+// One workgroup per item: sequence, run of blocks, key / value head, split, block of rows in the run.
 __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int lane = threadIdx.x & 63;
-  const uint32_t len = split_len(a);
-  // The hardware deals workgroups to the 8 XCDs in rotation; `together` consecutive items stay on one, not always the same one: the blocks of a
-  // prompt grow in work, and with eight such runs to a head one XCD had all the heaviest (4 x 4096 tokens: 1.04 ms).
+  Seq s = {};
+  if (lane < a.c.batch) s = load_seq(a, lane);
+  const uint32_t len = split_len(a, s);
+  // The hardware deals workgroups to the 8 XCDs in rotation; a run, which reads the same keys, stays on one.  Back and forth over the XCDs: a
+  // prompt's runs shrink, and dealt in one direction the first XCD had the longest of every eight (4 x 4096 tokens: 1.04 ms).
   uint32_t v = blockIdx.x;
-  if (a.together > 1) {
-    const uint32_t x = v % 8, j = v / 8, n = (uint32_t)a.together;
-    v = (j / n * 8 + (x + j / n) % 8) * n + j % n;
+  if (a.runs) {
+    const uint32_t x = v % 8, j = v / 8, round = j / RUN;
+    v = (round * 8 + (round & 1 ? 7 - x : x)) * RUN + j % RUN;
   }
   uint32_t item0 = 0, part0 = 0, item_end, part_end, splits, items, parts;
   uint64_t hit = 0;
   int b0 = 0;
-  Seq s;
   for (; b0 < a.c.batch; b0 += 64) {
-    s = Seq{};
     splits = items = parts = 0;
     if (b0 + lane < a.c.batch) {
-      s = load_seq(a, b0 + lane);
+      if (b0 > 0) s = load_seq(a, b0 + lane);
       splits = splits_of(s, len);
       items = (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.blocks;
       parts = part_rows_of(a, s, splits);
@@ -802,10 +800,13 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   const uint32_t local = v - (__builtin_amdgcn_readlane(item_end, at) - items), part = __builtin_amdgcn_readlane(part_end, at) - parts;
   // (lists that are no batch's: nothing that has no room)
   if (local >= items || part > a.part_rows || parts > a.part_rows - part) return;
-  const uint32_t per = splits * (uint32_t)q.blocks;
-  const int kvh = uni((int)(local / per));
-  const uint32_t rem = local - (uint32_t)kvh * per;
-  const int split = uni((int)(rem / (uint32_t)q.blocks)), block = q.blocks - 1 - uni((int)(rem % (uint32_t)q.blocks));
+  // blocks in runs, the last (longest) ones of all heads first
+  const uint32_t runs = ((uint32_t)q.blocks + RUN - 1) / RUN, run = (uint32_t)uni((int)min(local / (RUN * (uint32_t)a.c.n_kv_heads * splits), runs - 1));
+  const uint32_t size = min((uint32_t)q.blocks - run * RUN, RUN), of_head = size * splits;
+  uint32_t rem = local - run * (RUN * (uint32_t)a.c.n_kv_heads * splits);
+  const int kvh = uni((int)(rem / of_head));
+  rem -= (uint32_t)kvh * of_head;
+  const int split = uni((int)(rem / size)), block = q.blocks - 1 - (int)(run * RUN + rem - (uint32_t)split * size);
   const int64_t l64 = (int64_t)(((uint32_t)q.tiles + splits - 1) / splits) * KT;
   const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
   const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
@@ -824,17 +825,18 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
   __shared__ float4 s_sum[4][64];
   __shared__ float2 s_ml[4][2];
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), half = lane >> 5, col = (lane & 31) * 4;
-  const uint32_t len = split_len(a);
+  Seq s = {};
+  if (lane < a.c.batch) s = load_seq(a, lane);
+  const uint32_t len = split_len(a, s);
   const float c = a.scale * LOG2E;
   const int pairs = (a.H + 1) / 2;
   uint32_t part0 = 0, item0 = 0;
   uint32_t i = WAVES == 1 ? blockIdx.x * 4 + (uint32_t)wave : blockIdx.x;      // (token, pair of heads)
   const uint32_t stride = WAVES == 1 ? gridDim.x * 4 : gridDim.x;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    Seq s = {};
     uint32_t splits = 0, parts = 0;
     if (b0 + lane < a.c.batch) {
-      s = load_seq(a, b0 + lane);
+      if (b0 > 0) s = load_seq(a, b0 + lane);
       splits = splits_of(s, len);
       parts = part_rows_of(a, s, splits);
     }
@@ -952,9 +954,9 @@ hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, vo
   a.part_ml = (float2*)((float*)ws + b.part_rows * HD);
   a.ldq = ldq; a.ldo = ldo; a.T = (int)T; a.H = H; a.grp = H / c.n_kv_heads; a.scale = scale;
   a.by_grp = FastDiv::of(a.grp);
-  a.together = T * a.grp >= 2 * (int64_t)R_WIDE * c.batch ? 16 : 1;
+  a.runs = T * a.grp >= 2 * (int64_t)R_WIDE * c.batch;
   int64_t grid = b.items;
-  if (a.together > 1) grid = (grid + 8 * a.together - 1) / (8 * a.together) * (8 * a.together);
+  if (a.runs) grid = (grid + 8 * RUN - 1) / (8 * RUN) * (8 * RUN);
   hipLaunchKernelGGL(paged_kernel, dim3((unsigned)grid), dim3(256), LDS_BYTES, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !b.split) return e;
