@@ -28,6 +28,7 @@ namespace {
 
 constexpr int R_NARROW = 32, R_WIDE = 128;
 constexpr int MIN_SPLIT = 2;                      // 64-key tiles of a split: 32 keys for each wavefront of a narrow item
+constexpr uint32_t PLACES = 512;                  // workgroups that the chip holds at once
 constexpr int ROUNDS = 2048;                      // splits that all the work is cut into at most, four for each place on the chip
 constexpr uint32_t RUN = 16;                      // blocks of rows that read the same keys on one XCD at a time
 constexpr int LDS_JOIN_LD = 132;                  // floats of a row of sums in LDS
@@ -101,10 +102,13 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
   s.blocks = s.rows <= R_NARROW ? (s.rows > 0) : (s.rows + R_WIDE - 1) / R_WIDE;
   return s;
 }
-// 64-key tiles of a split, from the number w of them in all items: w / ROUNDS, but more than sqrt(w / 64).  A split's way in and out and its sums' way
-// through memory cost as much as some tiles, so of little work the splits are fewer: s splits save w (1 - 1 / s) and cost s.
+// 64-key tiles of a split, from the number w of them in all items: w / ROUNDS, but more than sqrt(w / 64): a split's way in and out and its sums' way
+// through memory cost as much as some tiles, so splits should grow with the work: s splits save w (1 - 1 / s) and cost s.  Narrow items' sums are small:
+// while w is few times PLACES, w / PLACES tiles, so that every item finds a place on the chip at once (one sequence of 4096 keys 12.4 -> 10.6 us,
+// 8 of 2000 20.4 -> 16.8, one of 16384 20.1 -> 18.0).
+struct SplitLen { uint32_t narrow, wide; };
 // first: of the lane's sequence among the first 64, loaded already.
-__device__ __forceinline__ uint32_t split_len(const PagedArgs& a, const Seq& first) {
+__device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& first) {
   const int lane = threadIdx.x & 63;
   uint64_t w = 0;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
@@ -117,10 +121,14 @@ __device__ __forceinline__ uint32_t split_len(const PagedArgs& a, const Seq& fir
   }
   w *= (uint32_t)a.c.n_kv_heads;
   const uint32_t even = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu), root = (uint32_t)uni((int)sqrtf((float)w * (1.f / 64.f))) + 1;
-  return max(max(even, root), (uint32_t)MIN_SPLIT);
+  const uint32_t wide = max(max(even, root), (uint32_t)MIN_SPLIT), fill = ((uint32_t)min(w, (uint64_t)4 * PLACES) + PLACES - 1) / PLACES;
+  return SplitLen{w <= 4 * PLACES ? max(fill, (uint32_t)MIN_SPLIT) : wide, wide};
 }
 // (rounded to the nearer number, and as even as they can be)
-__device__ __forceinline__ uint32_t splits_of(const Seq& s, uint32_t len) { return max(((uint32_t)s.tiles + len / 2) / len, 1u); }
+__device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
+  const uint32_t len = s.rows <= R_NARROW ? l.narrow : l.wide;
+  return max(((uint32_t)s.tiles + len / 2) / len, 1u);
+}
 // rows of sums that a sequence keeps: [key / value head][split][row]
 __device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& s, uint32_t splits) {
   return splits > 1 ? (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.rows : 0;
@@ -762,7 +770,7 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   const int lane = threadIdx.x & 63;
   Seq s = {};
   if (lane < a.c.batch) s = load_seq(a, lane);
-  const uint32_t len = split_len(a, s);
+  const SplitLen len = split_len(a, s);
   // The hardware deals workgroups to the 8 XCDs in rotation; a run, which reads the same keys, stays on one.  Back and forth over the XCDs: a
   // prompt's runs shrink, and dealt in one direction the first XCD had the longest of every eight (4 x 4096 tokens: 1.04 ms).
   uint32_t v = blockIdx.x;
@@ -827,7 +835,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
   const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), half = lane >> 5, col = (lane & 31) * 4;
   Seq s = {};
   if (lane < a.c.batch) s = load_seq(a, lane);
-  const uint32_t len = split_len(a, s);
+  const SplitLen len = split_len(a, s);
   const float c = a.scale * LOG2E;
   const int pairs = (a.H + 1) / 2;
   uint32_t part0 = 0, item0 = 0;
@@ -927,7 +935,7 @@ Bounds bounds(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
   const int64_t most = (tiles + MIN_SPLIT - 1) / MIN_SPLIT;           // splits of a sequence
   // ... and of all: w / len, which grows with w, beside one for each item
   const double w = (double)Hkv * (double)blocks * (double)tiles;
-  const int64_t cuts = std::min<int64_t>(ROUNDS, (int64_t)(8.0 * std::sqrt(w)) + 2);
+  const int64_t cuts = std::min<int64_t>(ROUNDS, std::max<int64_t>((int64_t)(8.0 * std::sqrt(w)) + 2, PLACES));
   Bounds b;
   b.split = most > 1;
   b.items = std::min(Hkv * blocks * most, Hkv * blocks + cuts);
