@@ -321,7 +321,8 @@ int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_
  * (a c - b s, b c + a s).  inverse != 0 uses -s: the transpose, which is its gradient.  Columns rot.. of a head are copied; a row of
  * out whose position is outside the tables is left as it was, and so are columns past the heads.  out may be x with ldo = ldx (in
  * place); any other overlap is not allowed.  LR_BF16: hd and the strides multiples of 8, rot of 16, all pointers 16-byte aligned but
- * pos; LR_F32: rot even.  rot <= hd.  T may be 0.                                                                              */
+ * pos; LR_F32: rot even.  rot <= hd.  T may be 0, and is at most 2^24; LR_EUNSUPPORTED above 2^32 lanes (units of 16 bytes, of a pair where
+ * fp32 rows do not start on 16 bytes).                                                                                         */
 int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t* pos, const float* cos_tab,
                const float* sin_tab, int64_t table_rows, int64_t T, int64_t H, int64_t hd, int64_t rot, int interleaved,
                int inverse, int dt, void* stream);

@@ -191,6 +191,7 @@ def _stream():
 
 # launches go to the current stream, which is one of the current device's
 def _on_current(device):
+    device = torch.device(device)
     if device.type != "cuda" or device.index not in (None, torch.cuda.current_device()):
         raise LrError(f"tensors on the current GPU expected, not on {device}")
 
@@ -483,10 +484,8 @@ def lr_rope_table(n, rot, base=10000.0, first=0, factor=1.0, ramp=None, mscale=1
     context, low, high = (0.0, 0.0, 1.0) if ramp is None else ramp
     if ramp is not None and not context > 0:
         raise LrError("lr_rope_table: the trained context of a ramp is positive")
-    _on_current(torch.device(device))
-    cos, sin = (torch.empty((max(n, 0), max(rot, 0) // 2), dtype=torch.float32, device=device) for _ in range(2))
-    _check(lib().lr_rope_table(_dense(cos), _dense(sin), n, rot, first, base, factor, context, low, high, mscale, _stream()), "lr_rope_table")
-    return cos, sin
+    _on_current(device)
+    return _native().rope_table(n, rot, first, base, factor, context, low, high, mscale)
 
 
 def lr_rope_at(x, cos, sin, H, hd, pos=None, interleaved=False, inverse=False, out=None):

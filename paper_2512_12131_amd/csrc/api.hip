@@ -1458,7 +1458,7 @@ static int check_rotation(int64_t hd, int64_t rot, const float* cos_tab, const f
 int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t* pos, const float* cos_tab, const float* sin_tab,
                int64_t table_rows, int64_t T, int64_t H, int64_t hd, int64_t rot, int interleaved, int inverse, int dt, void* stream) {
   TRY(check_dt(dt));
-  if (T < 0 || T > 0x7fffffffLL || H <= 0 || hd <= 0 || H > (1 << 24) || hd > (1 << 24) || H * hd > (1 << 24) || ldx < H * hd || ldo < H * hd)
+  if (T < 0 || T > ((int64_t)1 << 24) || H <= 0 || hd <= 0 || H > (1 << 24) || hd > (1 << 24) || H * hd > (1 << 24) || ldx < H * hd || ldo < H * hd)
     return LR_EINVAL;
   TRY(check_dims_bf16(dt, {hd, ldx, ldo}));
   TRY(check_rotation(hd, rot, cos_tab, sin_tab, table_rows, dt));
@@ -1467,8 +1467,9 @@ int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t
   if ((uintptr_t)pos & 3) return LR_EALIGN;
   if (T == 0) return LR_OK;
   TRY(check_ptrs(dt, {x, out}));
-  return k_rope_at(x, ldx, out, ldo, pos, cos_tab, sin_tab, table_rows, T, (int)H, (int)hd, (int)rot, interleaved, inverse, dt,
-                   (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+  const hipError_t e = k_rope_at(x, ldx, out, ldo, pos, cos_tab, sin_tab, table_rows, T, (int)H, (int)hd, (int)rot, interleaved, inverse, dt,
+                                 (hipStream_t)stream);
+  return e == hipSuccess ? LR_OK : e == hipErrorNotSupported ? LR_EUNSUPPORTED : LR_ELAUNCH;
 }
 
 static int check_cache(const lr_kv_cache* c, bool pointers, KvCache* out) {

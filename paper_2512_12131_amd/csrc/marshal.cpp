@@ -354,6 +354,21 @@ void tables_of(const at::Tensor& cos, const at::Tensor& sin, int64_t& rows, int6
   if (sin.sizes() != cos.sizes()) fail(PyExc_ValueError, "tables of the same shape expected");
 }
 
+PyObject* rope_table(Args& a) {
+  const int64_t n = a.integer(), rot = a.integer(), first = a.integer();
+  double x[6];
+  for (double& v : x) {
+    v = PyFloat_AsDouble(a.next());
+    if (v == -1.0 && PyErr_Occurred()) throw PyError{};
+  }
+  const auto options = at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, c10::hip::current_device());
+  const int64_t sizes[] = {n < 0 ? 0 : n, rot < 0 ? 0 : rot / 2};
+  const at::Tensor cos = at::empty(sizes, options), sin = at::empty(sizes, options);
+  void *pc = ptr(cos), *ps = ptr(sin), *st = stream();
+  call("lr_rope_table", [&] { return lr_rope_table((float*)pc, (float*)ps, n, rot, first, x[0], x[1], x[2], x[3], x[4], x[5], st); });
+  return tuple(cos, sin);
+}
+
 PyObject* rope_at(Args& a) {
   const at::Tensor &x = a.tensor(), &cos = a.tensor(), &sin = a.tensor();
   const int64_t H = a.integer(), hd = a.integer();
@@ -482,7 +497,7 @@ PyObject* set_error(PyObject*, PyObject* type) {
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))(&entry<f>), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     ENTRY(linear_fwd), ENTRY(linear_fwd_static), ENTRY(linear_bwd), ENTRY(group_fwd), ENTRY(group_bwd), ENTRY(attention_fwd), ENTRY(attention_bwd),
-    ENTRY(rope_at), ENTRY(kv_append), ENTRY(attention_paged_fwd), ENTRY(rms_stat), ENTRY(rmsnorm_apply), ENTRY(rmsnorm_bwd), ENTRY(swiglu_fwd), ENTRY(swiglu_bwd),
+    ENTRY(rope_table), ENTRY(rope_at), ENTRY(kv_append), ENTRY(attention_paged_fwd), ENTRY(rms_stat), ENTRY(rmsnorm_apply), ENTRY(rmsnorm_bwd), ENTRY(swiglu_fwd), ENTRY(swiglu_bwd),
     {"set_error", set_error, METH_O, "the exception type of failed calls"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

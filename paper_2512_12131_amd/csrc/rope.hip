@@ -39,52 +39,101 @@ __device__ __forceinline__ void sincos_f64(double a, double* sn, double* cs) {
   *cs = ((q + 1) & 2) ? -v : v;
 }
 
-// A workgroup writes `rows` rows; its columns' frequencies are formed once, in LDS.
+// A lane stays in one column and walks down a workgroup's rows, `step` at a time: the first angle is formed as above, the next ones by turning it by
+// step * w (four products of 64 bits; 16 of them are off by some 2^-49).  Bound: the writes.  131072 rows of 64 (67 MB), a call: 20 us with an
+// angle of its own for every entry, now 12.
 __global__ __launch_bounds__(256) void rope_table_kernel(float* __restrict__ cs, float* __restrict__ sn, int64_t n, int half, int rows,
-                                                         FastDiv by_half, int64_t first, double log2_base, double inv_factor,
-                                                         double turns, double low, double inv_span, double mscale) {
-  extern __shared__ double freq[];
-  for (int i = threadIdx.x; i < half; i += 256) {
-    const double w = exp2(-log2_base * (double)i / (double)half);
+                                                         int64_t first, double log2_base, double inv_factor, double turns, double low,
+                                                         double inv_span, double mscale) {
+  const int wide = half < 256 ? half : 256, step = 256 / wide, row = (int)threadIdx.x / wide;
+  if (row >= step) return;
+  const int64_t row0 = (int64_t)blockIdx.x * rows, end = row0 + rows < n ? row0 + rows : n;
+  for (int i = (int)threadIdx.x % wide; i < half; i += 256) {
+    double w = exp2(-log2_base * (double)i / (double)half);
     const double keep = turns > 0.0 ? fmin(1.0, fmax(0.0, (turns * w - low) * inv_span)) : 0.0;
-    freq[i] = w * (keep + (1.0 - keep) * inv_factor);
-  }
-  __syncthreads();
-  const int64_t row0 = (int64_t)blockIdx.x * rows;
-  const int count = (int)(n - row0 < rows ? n - row0 : rows) * half;
-  for (int e = threadIdx.x; e < count; e += 256) {
-    const int p = (int)by_half.div((uint32_t)e), i = e - p * half;
-    double s, c;
-    sincos_f64((double)(first + row0 + p) * freq[i], &s, &c);
-    cs[row0 * half + e] = (float)(c * mscale);
-    sn[row0 * half + e] = (float)(s * mscale);
+    w *= keep + (1.0 - keep) * inv_factor;
+    double s, c, ds = 0.0, dc = 1.0;
+    sincos_f64((double)(first + row0 + row) * w, &s, &c);
+    if (rows > step) sincos_f64((double)step * w, &ds, &dc);
+    s *= mscale;
+    c *= mscale;
+    for (int64_t p = row0 + row; p < end; p += step) {
+      cs[p * half + i] = (float)c;
+      sn[p * half + i] = (float)s;
+      const double t = c * dc - s * ds;
+      s = s * dc + c * ds;
+      c = t;
+    }
   }
 }
 
 // ---- rotation ----------------------------------------------------------------------------------------
-// One lane's share of a head, a unit: 8 pairs of bf16 (two 16-byte vectors: i and i + rot / 2, or neighbours), or one vector of the
-// columns that are copied.  fp32: one pair or one column, since rows may start anywhere.
-template <bool INTER>
-__device__ __forceinline__ void turn8(const float* a, const float* b, const float* c, const float* s, float* oa, float* ob) {
-  if constexpr (INTER) {      // a: pairs 0..3, b: pairs 4..7
+// One lane's share of a head, a unit: as many pairs as 16 bytes hold elements (two vectors, i and i + rot / 2 or neighbours), or one
+// vector of the columns that are copied.  fp32 rows that may start anywhere: one pair or one column.
+template <typename E, int VEC> struct Vec;
+template <> struct Vec<uint16_t, 8> {
+  typedef uint4 T;
+  static __device__ __forceinline__ void get(const T& q, float* v) { unpack8(q, v); }
+  static __device__ __forceinline__ T put(const float* v) { return pack8(v); }
+};
+template <> struct Vec<float, 4> {
+  typedef float4 T;
+  static __device__ __forceinline__ void get(const T& q, float* v) { v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w; }
+  static __device__ __forceinline__ T put(const float* v) { return make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <> struct Vec<float, 1> {
+  typedef float T;
+  static __device__ __forceinline__ void get(const T& q, float* v) { v[0] = q; }
+  static __device__ __forceinline__ T put(const float* v) { return v[0]; }
+};
+// a and b: the first and second elements of VEC pairs, or, interleaved, the first and second half of them
+template <int VEC, bool INTER>
+__device__ __forceinline__ void turn(const float* a, const float* b, const float* c, const float* s, float* oa, float* ob) {
+  if constexpr (INTER && VEC > 1) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < VEC / 2; i++) {
       oa[2 * i] = a[2 * i] * c[i] - a[2 * i + 1] * s[i];
       oa[2 * i + 1] = a[2 * i + 1] * c[i] + a[2 * i] * s[i];
-      ob[2 * i] = b[2 * i] * c[4 + i] - b[2 * i + 1] * s[4 + i];
-      ob[2 * i + 1] = b[2 * i + 1] * c[4 + i] + b[2 * i] * s[4 + i];
+      ob[2 * i] = b[2 * i] * c[VEC / 2 + i] - b[2 * i + 1] * s[VEC / 2 + i];
+      ob[2 * i + 1] = b[2 * i + 1] * c[VEC / 2 + i] + b[2 * i] * s[VEC / 2 + i];
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
+    for (int i = 0; i < VEC; i++) {
       oa[i] = a[i] * c[i] - b[i] * s[i];
       ob[i] = b[i] * c[i] + a[i] * s[i];
     }
   }
 }
-__device__ __forceinline__ void load8f(const float* p, float* v) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+template <int VEC>
+__device__ __forceinline__ void table_entries(const float* p, float* v) {
+  if constexpr (VEC == 1) {
+    v[0] = *p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(p + i);
+      v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+    }
+  }
+}
+// Unit u of a head, x to out.  A lane does one: two heads or four per lane, sharing the table's entries, were slower (16384 tokens of 32 heads 42 us ->
+// 51 and 53: the entries are in the nearest cache, and the lanes are fewer).
+template <typename E, int VEC, bool INTER>
+__device__ __forceinline__ void turn_unit(int u, int rot, const float* cs, const float* sn, float sgn, const E* x, E* out) {
+  using V = Vec<E, VEC>;
+  const int at = INTER ? u * 2 * VEC : u * VEC, other = INTER ? VEC : rot / 2;
+  const typename V::T qa = *reinterpret_cast<const typename V::T*>(x + at), qb = *reinterpret_cast<const typename V::T*>(x + at + other);
+  float c[VEC], s[VEC], va[VEC], vb[VEC], oa[VEC], ob[VEC];
+  table_entries<VEC>(cs + u * VEC, c);
+  table_entries<VEC>(sn + u * VEC, s);
+#pragma unroll
+  for (int i = 0; i < VEC; i++) s[i] *= sgn;
+  V::get(qa, va);
+  V::get(qb, vb);
+  turn<VEC, INTER>(va, vb, c, s, oa, ob);
+  *reinterpret_cast<typename V::T*>(out + at) = V::put(oa);
+  *reinterpret_cast<typename V::T*>(out + at + other) = V::put(ob);
 }
 
 struct RopeArgs {
@@ -95,82 +144,27 @@ struct RopeArgs {
   const float *cs, *sn;
   int H, hd, rot;
   int nrot, units;        // units of a head that turn, and all of them
-  int groups, rows;       // head groups of a row (a lane works on heads g, g + groups, ...); rows of a workgroup
-  FastDiv by_units, by_row;
+  int rows, parts;        // rows of a workgroup, or workgroups of a row
+  FastDiv by_units, by_row, by_parts;
   float sgn;
 };
 
-template <typename E, bool INTER, int HPT>
+template <typename E, int VEC, bool INTER>
 __global__ __launch_bounds__(256) void rope_at_kernel(RopeArgs a) {
-  constexpr bool BF = sizeof(E) == 2;
-  const int per_row = a.groups * a.units, half = a.rot / 2;
-  const int64_t row0 = (int64_t)blockIdx.x * a.rows;
-  const int count = (int)(a.T - row0 < a.rows ? a.T - row0 : a.rows) * per_row;
-  for (int idx = threadIdx.x; idx < count; idx += 256) {
-    const int r = (int)a.by_row.div((uint32_t)idx), rem = idx - r * per_row;
-    const int g = (int)a.by_units.div((uint32_t)rem), u = rem - g * a.units;
-    const int64_t row = row0 + r;
-    const int64_t p = a.pos ? (int64_t)a.pos[row] : row;
-    if (p < 0 || p >= a.table_rows) continue;
-    const E* x = (const E*)a.x + row * a.ldx;
-    E* out = (E*)a.out + row * a.ldo;
-    if constexpr (BF) {
-      if (u < a.nrot) {
-        const int at = INTER ? u * 16 : u * 8, other = INTER ? 8 : half;
-        float c[8], s[8];
-        load8f(a.cs + p * half + u * 8, c);
-        load8f(a.sn + p * half + u * 8, s);
-#pragma unroll
-        for (int i = 0; i < 8; i++) s[i] *= a.sgn;
-        uint4 qa[HPT], qb[HPT];
-#pragma unroll
-        for (int j = 0; j < HPT; j++) {
-          const int h = g + j * a.groups;
-          if (h < a.H) {
-            qa[j] = *reinterpret_cast<const uint4*>(x + h * a.hd + at);
-            qb[j] = *reinterpret_cast<const uint4*>(x + h * a.hd + at + other);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < HPT; j++) {
-          const int h = g + j * a.groups;
-          if (h < a.H) {
-            float va[8], vb[8], oa[8], ob[8];
-            unpack8(qa[j], va);
-            unpack8(qb[j], vb);
-            turn8<INTER>(va, vb, c, s, oa, ob);
-            *reinterpret_cast<uint4*>(out + h * a.hd + at) = pack8(oa);
-            *reinterpret_cast<uint4*>(out + h * a.hd + at + other) = pack8(ob);
-          }
-        }
-      } else {
-        const int at = a.rot + (u - a.nrot) * 8;
-        for (int h = g; h < a.H; h += a.groups)
-          *reinterpret_cast<uint4*>(out + h * a.hd + at) = *reinterpret_cast<const uint4*>(x + h * a.hd + at);
-      }
-    } else {
-      if (u < a.nrot) {
-        const int i0 = INTER ? 2 * u : u, i1 = INTER ? i0 + 1 : u + half;
-        const float c = a.cs[p * half + u], s = a.sn[p * half + u] * a.sgn;
-        float va[HPT], vb[HPT];
-#pragma unroll
-        for (int j = 0; j < HPT; j++) {
-          const int h = g + j * a.groups;
-          if (h < a.H) { va[j] = x[h * a.hd + i0]; vb[j] = x[h * a.hd + i1]; }
-        }
-#pragma unroll
-        for (int j = 0; j < HPT; j++) {
-          const int h = g + j * a.groups;
-          if (h < a.H) {
-            out[h * a.hd + i0] = va[j] * c - vb[j] * s;
-            out[h * a.hd + i1] = vb[j] * c + va[j] * s;
-          }
-        }
-      } else {
-        const int at = a.rot + u - a.nrot;
-        for (int h = g; h < a.H; h += a.groups) out[h * a.hd + at] = x[h * a.hd + at];
-      }
-    }
+  const uint32_t group = a.by_parts.div(blockIdx.x), idx = (blockIdx.x - group * a.parts) * 256 + threadIdx.x;
+  const uint32_t r = a.by_row.div(idx), rem = idx - r * (uint32_t)(a.H * a.units);
+  const int64_t row = (int64_t)group * a.rows + r;
+  if (r >= (uint32_t)a.rows || row >= a.T) return;
+  const int64_t p = a.pos ? (int64_t)a.pos[row] : row;
+  if (p < 0 || p >= a.table_rows) return;
+  const int h = (int)a.by_units.div(rem), u = (int)rem - h * a.units;
+  const E* x = (const E*)a.x + row * a.ldx + h * a.hd;
+  E* out = (E*)a.out + row * a.ldo + h * a.hd;
+  if (u < a.nrot) {
+    turn_unit<E, VEC, INTER>(u, a.rot, a.cs + p * (a.rot / 2), a.sn + p * (a.rot / 2), a.sgn, x, out);
+  } else {
+    const int at = a.rot + (u - a.nrot) * VEC;
+    *reinterpret_cast<typename Vec<E, VEC>::T*>(out + at) = *reinterpret_cast<const typename Vec<E, VEC>::T*>(x + at);
   }
 }
 
@@ -182,23 +176,23 @@ struct AppendArgs {
   int64_t ldk, ldv, ldq, ldqo, T, table_rows;
   const float *cs, *sn;
   int H, rot;
-  int nrot, units;          // of a key or query head, as above
-  int groups, vunits, vgroups;    // head groups (keys' and queries' heads in one row of them); vectors of a value head, its groups
-  FastDiv by_units, by_vunits, by_tok;
+  int nrot, units, vunits;  // units of a key or query head, as above; vectors of a value head
+  int parts;                // workgroups that share a token's units out
+  FastDiv by_units, by_vunits, by_tok, by_parts;
 };
 
-constexpr int APPEND_TOKENS = 4;       // a workgroup's: one for each wavefront to look up
-
-// Where the workgroup's tokens go is found once, a token per wavefront: its sequence is the number of boundaries at or before it, 64 of them
-// compared at a time.  Then the lanes share out the units of all of them.
-template <bool INTER, int HPT>
+// Where a workgroup's tokens go is found once, a token per wavefront: its sequence is the number of boundaries at or before it, 64 of them compared
+// at a time.  Then the lanes share out the units of all of them.  Bound: memory, 16384 tokens of 32 heads, each with keys and values of its own,
+// 164 us (0.81 GB in and out, 4.9 TB/s; a copy of 1 GB 5.1).
+template <bool INTER, int TOKENS>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
-  __shared__ int s_pos[APPEND_TOKENS];
-  __shared__ int64_t s_row[APPEND_TOKENS];     // element offset of the token's row in the cache
+  __shared__ int s_pos[TOKENS];
+  __shared__ int64_t s_row[TOKENS];            // element offset of the token's row in the cache
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t tok0 = (int64_t)blockIdx.x * APPEND_TOKENS;
+  const uint32_t group = a.by_parts.div(blockIdx.x), part = blockIdx.x - group * a.parts;
+  const int64_t tok0 = (int64_t)group * TOKENS;
   const int Hkv = a.c.n_kv_heads, hd = a.c.head_dim;
-  {
+  if (wave < TOKENS) {
     const int64_t t = tok0 + wave;
     int pos = -1;
     int64_t at = 0;
@@ -224,64 +218,26 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     if (lane == 0) { s_pos[wave] = pos; s_row[wave] = at; }
   }
   __syncthreads();
-  const int heads = Hkv + a.H, half = a.rot / 2;
-  const int nqk = a.groups * a.units, per_tok = nqk + a.vgroups * a.vunits;
-  for (int idx = tid; idx < APPEND_TOKENS * per_tok; idx += 256) {
-    const int tl = (int)a.by_tok.div((uint32_t)idx);
-    int rem = idx - tl * per_tok;
-    const int pos = s_pos[tl];
+  const int nqk = (Hkv + a.H) * a.units, per_tok = nqk + Hkv * a.vunits;
+  for (int idx = (int)part * 256 + tid; idx < TOKENS * per_tok; idx += a.parts * 256) {
+    const int tl = TOKENS == 1 ? 0 : (int)a.by_tok.div((uint32_t)idx);
+    const int rem = idx - tl * per_tok, pos = s_pos[tl];
     if (pos < 0) continue;                     // (also where the call has no such token)
     const int64_t t = tok0 + tl, row = s_row[tl];
-    if (rem >= nqk) {                          // values
-      rem -= nqk;
-      const int g = (int)a.by_vunits.div((uint32_t)rem), at = (rem - g * a.vunits) * 8;
-      uint4 w[HPT];
-#pragma unroll
-      for (int j = 0; j < HPT; j++) {
-        const int h = g + j * a.vgroups;
-        if (h < Hkv) w[j] = *reinterpret_cast<const uint4*>(a.v + t * a.ldv + h * hd + at);
+    if (rem < nqk) {
+      const int h = (int)a.by_units.div((uint32_t)rem), u = rem - h * a.units;
+      const uint16_t* x = h < Hkv ? a.k + t * a.ldk + h * hd : a.q + t * a.ldq + (h - Hkv) * hd;
+      uint16_t* out = h < Hkv ? a.c.k + row + h * a.c.head_stride : a.q_out + t * a.ldqo + (h - Hkv) * hd;
+      if (u < a.nrot) {
+        const int64_t at = (int64_t)pos * (a.rot / 2);
+        turn_unit<uint16_t, 8, INTER>(u, a.rot, a.cs + at, a.sn + at, 1.f, x, out);
+      } else {
+        const int at = a.rot + (u - a.nrot) * 8;
+        *reinterpret_cast<uint4*>(out + at) = *reinterpret_cast<const uint4*>(x + at);
       }
-#pragma unroll
-      for (int j = 0; j < HPT; j++) {
-        const int h = g + j * a.vgroups;
-        if (h < Hkv) *reinterpret_cast<uint4*>(a.c.v + row + h * a.c.head_stride + at) = w[j];
-      }
-      continue;
-    }
-    const int g = (int)a.by_units.div((uint32_t)rem), u = rem - g * a.units;
-    auto src = [&](int h) { return h < Hkv ? a.k + t * a.ldk + h * hd : a.q + t * a.ldq + (h - Hkv) * hd; };
-    auto dst = [&](int h) { return h < Hkv ? a.c.k + row + h * a.c.head_stride : a.q_out + t * a.ldqo + (h - Hkv) * hd; };
-    if (u < a.nrot) {
-      const int at = INTER ? u * 16 : u * 8, other = INTER ? 8 : half;
-      float c[8], s[8];
-      load8f(a.cs + (int64_t)pos * half + u * 8, c);
-      load8f(a.sn + (int64_t)pos * half + u * 8, s);
-      uint4 qa[HPT], qb[HPT];
-#pragma unroll
-      for (int j = 0; j < HPT; j++) {
-        const int h = g + j * a.groups;
-        if (h < heads) {
-          const uint16_t* p = src(h) + at;
-          qa[j] = *reinterpret_cast<const uint4*>(p);
-          qb[j] = *reinterpret_cast<const uint4*>(p + other);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < HPT; j++) {
-        const int h = g + j * a.groups;
-        if (h < heads) {
-          float va[8], vb[8], oa[8], ob[8];
-          unpack8(qa[j], va);
-          unpack8(qb[j], vb);
-          turn8<INTER>(va, vb, c, s, oa, ob);
-          uint16_t* p = dst(h) + at;
-          *reinterpret_cast<uint4*>(p) = pack8(oa);
-          *reinterpret_cast<uint4*>(p + other) = pack8(ob);
-        }
-      }
-    } else {
-      const int at = a.rot + (u - a.nrot) * 8;
-      for (int h = g; h < heads; h += a.groups) *reinterpret_cast<uint4*>(dst(h) + at) = *reinterpret_cast<const uint4*>(src(h) + at);
+    } else {                                   // values
+      const int h = (int)a.by_vunits.div((uint32_t)(rem - nqk)), at = (rem - nqk - h * a.vunits) * 8;
+      *reinterpret_cast<uint4*>(a.c.v + row + h * a.c.head_stride + at) = *reinterpret_cast<const uint4*>(a.v + t * a.ldv + h * hd + at);
     }
   }
 }
@@ -292,11 +248,13 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 hipError_t k_rope_table(float* cs, float* sn, int64_t n, int half, int64_t first, double base, double factor, double context, double low,
                         double high, double mscale, hipStream_t st) {
-  int64_t rows = 4096 / half < 1 ? 1 : 4096 / half;
-  if ((n + rows - 1) / rows < 1024) rows = n / 1024 < 1 ? 1 : n / 1024;
-  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3(256), half * sizeof(double), st, cs, sn, n, half,
-                     (int)rows, FastDiv::of(half), first, log2(base), 1.0 / factor, context / 6.283185307179586477, low, 1.0 / (high - low),
-                     mscale);
+  const int wide = half < 256 ? half : 256, step = 256 / wide;
+  // 2048 workgroups, of 16 steps at most while that is a grid
+  int64_t rows = (n + 2047) / 2048;
+  rows = (rows + step - 1) / step * step;
+  if (rows > 16 * step && (n + 16 * step - 1) / (16 * step) < (1 << 22)) rows = 16 * step;
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3(256), 0, st, cs, sn, n, half, (int)rows, first, log2(base),
+                     1.0 / factor, context / 6.283185307179586477, low, 1.0 / (high - low), mscale);
   return hipGetLastError();
 }
 
@@ -305,24 +263,27 @@ hipError_t k_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const i
   RopeArgs a;
   a.x = x; a.out = out; a.ldx = ldx; a.ldo = ldo; a.T = T; a.table_rows = table_rows; a.pos = pos; a.cs = cs; a.sn = sn;
   a.H = H; a.hd = hd; a.rot = rot; a.sgn = inverse ? -1.f : 1.f;
-  const int vec = dt == LR_BF16 ? 8 : 1;
+  // fp32 in vectors of four where rows, heads and the two halves of the pairs start on 16 bytes
+  const bool whole = (((uintptr_t)x | (uintptr_t)out | (uintptr_t)cs | (uintptr_t)sn) & 15) == 0 && (ldx | ldo | hd) % 4 == 0 && rot % 8 == 0;
+  const int vec = dt == LR_BF16 ? 8 : whole ? 4 : 1;
   a.nrot = rot / 2 / vec;
   a.units = a.nrot + (x == out ? 0 : (hd - rot) / vec);
-  auto launch = [&](auto HPTc) {
-    constexpr int HPT = decltype(HPTc)::value;
-    a.groups = ceil_div(H, HPT);
-    const int per_row = a.groups * a.units;
-    a.rows = per_row >= 256 ? 1 : 256 / per_row;
-    a.by_units = FastDiv::of(a.units);
-    a.by_row = FastDiv::of(per_row);
-    const dim3 grid((unsigned)((T + a.rows - 1) / a.rows)), block(256);
-    if (dt == LR_BF16 && interleaved) hipLaunchKernelGGL((rope_at_kernel<uint16_t, true, HPT>), grid, block, 0, st, a);
-    else if (dt == LR_BF16) hipLaunchKernelGGL((rope_at_kernel<uint16_t, false, HPT>), grid, block, 0, st, a);
-    else if (interleaved) hipLaunchKernelGGL((rope_at_kernel<float, true, HPT>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((rope_at_kernel<float, false, HPT>), grid, block, 0, st, a);
-    return hipGetLastError();
-  };
-  return launch(std::integral_constant<int, 1>{});
+  const int per_row = H * a.units;
+  a.rows = per_row >= 256 ? 1 : 256 / per_row;
+  a.parts = ceil_div(per_row, 256);
+  a.by_units = FastDiv::of(a.units);
+  a.by_row = FastDiv::of(per_row);
+  a.by_parts = FastDiv::of(a.parts);
+  const int64_t groups = (T + a.rows - 1) / a.rows * a.parts;
+  if (groups >= (int64_t)1 << 24) return hipErrorNotSupported;      // 2^32 lanes
+  const dim3 grid((unsigned)groups), block(256);
+  if (dt == LR_BF16 && interleaved) hipLaunchKernelGGL((rope_at_kernel<uint16_t, 8, true>), grid, block, 0, st, a);
+  else if (dt == LR_BF16) hipLaunchKernelGGL((rope_at_kernel<uint16_t, 8, false>), grid, block, 0, st, a);
+  else if (whole && interleaved) hipLaunchKernelGGL((rope_at_kernel<float, 4, true>), grid, block, 0, st, a);
+  else if (whole) hipLaunchKernelGGL((rope_at_kernel<float, 4, false>), grid, block, 0, st, a);
+  else if (interleaved) hipLaunchKernelGGL((rope_at_kernel<float, 1, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((rope_at_kernel<float, 1, false>), grid, block, 0, st, a);
+  return hipGetLastError();
 }
 
 hipError_t k_kv_append(const KvCache& c, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, void* q_out,
@@ -334,15 +295,19 @@ hipError_t k_kv_append(const KvCache& c, const void* k, int64_t ldk, const void*
   a.nrot = rot / 16;
   a.units = a.nrot + (c.head_dim - rot) / 8;
   a.vunits = c.head_dim / 8;
-  constexpr int HPT = 1;
-  a.groups = ceil_div(c.n_kv_heads + H, HPT);
-  a.vgroups = ceil_div(c.n_kv_heads, HPT);
+  const int per_tok = (c.n_kv_heads + H) * a.units + c.n_kv_heads * a.vunits;
+  // Few tokens: as many workgroups to each as its units fill, so that a lane has one; else four tokens to a workgroup, found side by side.
+  const bool few = T * per_tok <= 256 * 1024;
+  a.parts = few ? ceil_div(per_tok, 256) : 1;
   a.by_units = FastDiv::of(a.units);
   a.by_vunits = FastDiv::of(a.vunits);
-  a.by_tok = FastDiv::of(a.groups * a.units + a.vgroups * a.vunits);
-  const dim3 grid((unsigned)((T + APPEND_TOKENS - 1) / APPEND_TOKENS)), block(256);
-  if (interleaved) hipLaunchKernelGGL((kv_append_kernel<true, HPT>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((kv_append_kernel<false, HPT>), grid, block, 0, st, a);
+  a.by_tok = FastDiv::of(per_tok);
+  a.by_parts = FastDiv::of(a.parts);
+  const dim3 grid((unsigned)(few ? T * a.parts : (T + 3) / 4)), block(256);
+  if (few && interleaved) hipLaunchKernelGGL((kv_append_kernel<true, 1>), grid, block, 0, st, a);
+  else if (few) hipLaunchKernelGGL((kv_append_kernel<false, 1>), grid, block, 0, st, a);
+  else if (interleaved) hipLaunchKernelGGL((kv_append_kernel<true, 4>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((kv_append_kernel<false, 4>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
