@@ -233,6 +233,12 @@ __device__ __forceinline__ void mask(f32x16 (&st)[NB], int lim, int lane) {
 #pragma unroll
     for (int e = 0; e < 16; e++) st[nb][e] = nb * 32 + acc_row(e, 0) >= lim ? -INFINITY : st[nb][e];
 }
+// The maximum that exponents refer to moves up only where it would by more than 8 powers of two: up to there probabilities stay below 2^8, and the
+// sums need no rescaling (64 products a tile, needed for one row in 32 they are done for all; with scores in no order that was half of the tiles).
+__device__ __forceinline__ float next_max(float m, float mx, float c) {
+  const float mn = fmaxf(m, mx);
+  return (mn - m) * c > 8.f ? mn : m;
+}
 // Probabilities from scores, as bf16 operands (half a step, 2^-9 relative on average, is what their product with V on the matrix cores costs; the
 // sum adds them unrounded).
 template <int NB>
@@ -242,7 +248,7 @@ __device__ __forceinline__ void softmax(Rows& s, f32x16 (&st)[NB], bf16x8 (&pf)[
   for (int nb = 0; nb < NB; nb++)
 #pragma unroll
     for (int e = 0; e < 16; e++) mx = fmaxf(mx, st[nb][e]);
-  const float mn = fmaxf(s.m, half_max(mx)), alpha = fast_exp2((s.m - mn) * c), mc = mn * c;
+  const float mn = next_max(s.m, half_max(mx), c), alpha = fast_exp2((s.m - mn) * c), mc = mn * c;
   s.m = mn;
   float sum = 0.f;
 #pragma unroll
@@ -558,7 +564,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     return mx;
   };
   auto new_max = [&](float mx) {
-    const float mn = fmaxf(st.m, half_max(mx));
+    const float mn = next_max(st.m, half_max(mx), c);
     alpha = fast_exp2((st.m - mn) * c);
     st.m = mn;
     mc = mn * c;
