@@ -120,7 +120,7 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& fir
     w += last_lane(wave_scan((uint32_t)x & 0xffffu)) + ((uint64_t)last_lane(wave_scan((uint32_t)(x >> 16))) << 16);
   }
   w *= (uint32_t)a.c.n_kv_heads;
-  const uint32_t even = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu), root = (uint32_t)uni((int)sqrtf((float)w * (1.f / 64.f))) + 1;
+  const uint32_t even = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu), root = (uint32_t)uni((int)__builtin_amdgcn_sqrtf((float)w * (1.f / 64.f))) + 1;
   const uint32_t wide = max(max(even, root), (uint32_t)MIN_SPLIT), fill = ((uint32_t)min(w, (uint64_t)4 * PLACES) + PLACES - 1) / PLACES;
   return SplitLen{w <= 4 * PLACES ? max(fill, (uint32_t)MIN_SPLIT) : wide, wide};
 }
@@ -384,7 +384,7 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
     const int lim = row_limit(in, s, r), lim0 = uni(row_limit(in, s, 0)), all = uni(row_limit(in, s, s.rows - 1));
     Pages pg;
     first_window<16>(in, pg, src, j0, lane);
-    auto dma = [&](bool isV, int j) {     // 8 loads of 4 keys each; past the wavefront's keys: zeros, so that every block counts as many
+    auto dma = [&](bool isV, int j) {     // 8 loads of 4 keys each
 #pragma unroll
       for (int g = 0; g < 4; g++) {
         const rsrc_t rs = group_rsrc(group(pg, j * 4 + g), isV ? cV : cK);
@@ -403,16 +403,22 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
       landed<8>();                        // K; behind it V
       scores<1>(x, qf, sK, lane);
       read_done();
-      next_window<16>(pg, src, j + 1, lane);
-      dma(false, j + 1);
+      const bool more = j + 1 < j1;       // (a load that asks for nothing still takes 95 cycles to issue)
+      if (more) {
+        next_window<16>(pg, src, j + 1, lane);
+        dma(false, j + 1);
+      }
       const bool masked = key0 + 32 > lim0;
       if (masked) mask<1>(x, lim - key0, lane);
       softmax<1>(st, x, pf, c);
-      landed<8>();                        // V; behind it the next K
+      if (more) landed<8>();              // V; behind it the next K
+      else landed<0>();
       if (masked && lim0 < all) bad |= take_out(sV, 8192, lane);
       output<1>(st, pf, sV, lane);
-      read_done();
-      dma(true, j + 1);
+      if (more) {
+        read_done();
+        dma(true, j + 1);
+      }
     }
     if (bad) put_back(st, table, kvh, max(j0 * 32, lim0 & ~31), min(min(j1 * 32, key_hi), all), lim, lane);
   }
@@ -815,12 +821,20 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   // (lists that are no batch's: nothing that has no room)
   if (local >= items || part > a.part_rows || parts > a.part_rows - part) return;
   // blocks in runs, the last (longest) ones of all heads first
-  const uint32_t runs = ((uint32_t)q.blocks + RUN - 1) / RUN, run = (uint32_t)uni((int)min(local / (RUN * (uint32_t)a.c.n_kv_heads * splits), runs - 1));
-  const uint32_t size = min((uint32_t)q.blocks - run * RUN, RUN), of_head = size * splits;
-  uint32_t rem = local - run * (RUN * (uint32_t)a.c.n_kv_heads * splits);
-  const int kvh = uni((int)(rem / of_head));
-  rem -= (uint32_t)kvh * of_head;
-  const int split = uni((int)(rem / size)), block = q.blocks - 1 - (int)(run * RUN + rem - (uint32_t)split * size);
+  int kvh, split, block = 0;
+  if (q.blocks == 1) {
+    kvh = uni((int)(local / splits));
+    split = (int)(local - (uint32_t)kvh * splits);
+  } else {
+    const uint32_t runs = ((uint32_t)q.blocks + RUN - 1) / RUN, of_run = RUN * (uint32_t)a.c.n_kv_heads * splits,
+                   run = (uint32_t)uni((int)min(local / of_run, runs - 1));
+    const uint32_t size = min((uint32_t)q.blocks - run * RUN, RUN), of_head = size * splits;
+    uint32_t rem = local - run * of_run;
+    kvh = uni((int)(rem / of_head));
+    rem -= (uint32_t)kvh * of_head;
+    split = uni((int)(rem / size));
+    block = q.blocks - 1 - (int)(run * RUN + rem - (uint32_t)split * size);
+  }
   const int64_t l64 = (int64_t)(((uint32_t)q.tiles + splits - 1) / splits) * KT;
   const int lo = (int)min(split * l64, (int64_t)q.keys), hi = (int)min((split + 1) * l64, (int64_t)q.keys);
   const uint32_t p0 = part + ((uint32_t)kvh * splits + (uint32_t)split) * (uint32_t)q.rows;
