@@ -67,12 +67,9 @@ __device__ __forceinline__ float no_score(float c) { return -3.0e38f / fmaxf(c, 
 
 // ---- the split of the work ------------------------------------------------------------------------------
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
-// Inclusive sum over the lanes, in the vector unit's own lane moves (a shuffle goes through LDS: eighteen of them were 1.5 us on the way in).
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-  auto step = [&](auto Ctrl, auto Rows) {
-    constexpr int ctrl = decltype(Ctrl)::value, rows = decltype(Rows)::value;
-    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl, rows, 0xf, false);
-  };
+// The lane moves of an inclusive scan in the vector unit (a shuffle goes through LDS: eighteen of them were 1.5 us on the way in).
+template <class F>
+__device__ __forceinline__ void down_the_lanes(F&& step) {
   using std::integral_constant;
   using All = integral_constant<int, 0xf>;
   step(integral_constant<int, 0x111>{}, All{});      // from 1, 2, 4, 8 lanes down within a row of 16
@@ -81,6 +78,12 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
   step(integral_constant<int, 0x118>{}, All{});
   step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // a row's last lane to the next row: rows 1 and 3
   step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // lane 31 to rows 2 and 3
+}
+// Inclusive sum over the lanes.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  down_the_lanes([&](auto Ctrl, auto Rows) {
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(Ctrl)::value, decltype(Rows)::value, 0xf, false);
+  });
   return x;
 }
 __device__ __forceinline__ uint32_t last_lane(uint32_t x) { return __builtin_amdgcn_readlane(x, 63); }
@@ -102,32 +105,52 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
   s.blocks = s.rows <= R_NARROW ? (s.rows > 0) : (s.rows + R_WIDE - 1) / R_WIDE;
   return s;
 }
-// 64-key tiles of a split, from the number w of them in all items: w / ROUNDS, but more than sqrt(w / 64): a split's way in and out and its sums' way
-// through memory cost as much as some tiles, so splits should grow with the work: s splits save w (1 - 1 / s) and cost s.  Narrow items' sums are small:
-// while w is few times PLACES, w / PLACES tiles, so that every item finds a place on the chip at once (one sequence of 4096 keys 12.4 -> 10.6 us,
-// 8 of 2000 20.4 -> 16.8, one of 16384 20.1 -> 18.0).
-struct SplitLen { uint32_t narrow, wide; };
+// 64-key tiles of a split, from w, the number of them in all items.
+//   narrow  w / ROUNDS, but more than sqrt(w / 64): a split's way in and out costs as much as some tiles, so splits should grow with the work: s
+//           splits save w (1 - 1 / s) and cost s.  While w is few times PLACES, w / PLACES, so that every item finds a place on the chip at
+//           once (one sequence of 4096 keys 12.4 -> 10.6 us, 8 of 2000 20.4 -> 16.8, one of 16384 20.1 -> 18.0).
+//   wide    w / PLACES (of little work half of the places, a CU each): more splits than places save nothing.  And no less than sqrt(x / 6150), x the tiles times their rows: len tiles take len * 1.6
+//           us, and x / len rows of sums 0.26 ns each on their way through memory.  A sequence of two of the latter is not split, since the join
+//           takes some us by itself.  (us, against the narrow rule for both: a prompt of 777 tokens 31.2 -> 25.9, of 2048 70 -> 56, 512
+//           tokens over 8192 keys 93 -> 83, over 32768 301 -> 268, the mixed batch 101 -> 93.)
+struct SplitLen { uint32_t narrow, wide, whole; };      // whole: wide sequences of up to so many tiles are not split
+// Sum over the lanes, in an order of its own: both kernels get the same bits.  (Products and sums are rounded one by one wherever this is inlined.)
+__device__ __forceinline__ float lanes_sum(float x) {
+  auto step = [&](auto Ctrl, auto Rows) {
+    constexpr int ctrl = decltype(Ctrl)::value, rows = decltype(Rows)::value;
+    x = __fadd_rn(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), ctrl, rows, 0xf, false)));
+  };
+  down_the_lanes(step);
+  return __uint_as_float(last_lane(__float_as_uint(x)));
+}
 // first: of the lane's sequence among the first 64, loaded already.
 __device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& first) {
   const int lane = threadIdx.x & 63;
-  uint64_t w = 0;
+  float w = 0.f, x = 0.f;
   for (int b0 = 0; b0 < a.c.batch; b0 += 64) {
-    uint64_t x = 0;
+    float tiles = 0.f, rows = 0.f;
     if (b0 + lane < a.c.batch) {
       const Seq s = b0 == 0 ? first : load_seq(a, b0 + lane);
-      x = min((uint64_t)(uint32_t)s.blocks * (uint32_t)s.tiles, (uint64_t)1 << 40);
+      tiles = __fmul_rn((float)s.blocks, (float)s.tiles);
+      rows = s.rows > R_NARROW ? __fmul_rn((float)s.rows, (float)s.tiles) : 0.f;
     }
-    w += last_lane(wave_scan((uint32_t)x & 0xffffu)) + ((uint64_t)last_lane(wave_scan((uint32_t)(x >> 16))) << 16);
+    w = __fadd_rn(w, lanes_sum(tiles));
+    if (__builtin_amdgcn_ballot_w64(rows > 0.f)) x = __fadd_rn(x, lanes_sum(rows));
   }
-  w *= (uint32_t)a.c.n_kv_heads;
-  const uint32_t even = (uint32_t)min((w + ROUNDS - 1) / ROUNDS, (uint64_t)0x7fffffffu), root = (uint32_t)uni((int)__builtin_amdgcn_sqrtf((float)w * (1.f / 64.f))) + 1;
-  const uint32_t wide = max(max(even, root), (uint32_t)MIN_SPLIT), fill = ((uint32_t)min(w, (uint64_t)4 * PLACES) + PLACES - 1) / PLACES;
-  return SplitLen{w <= 4 * PLACES ? max(fill, (uint32_t)MIN_SPLIT) : wide, wide};
+  w = __fmul_rn(w, (float)a.c.n_kv_heads);
+  x = __fmul_rn(x, (float)a.c.n_kv_heads);
+  auto part = [&](float n) { return (uint32_t)uni((int)ceilf(fminf(__fmul_rn(w, 1.f / n), 1e9f))); };      // (n: a power of two)
+  auto root = [&](float y, float f) { return (uint32_t)uni((int)__builtin_amdgcn_sqrtf(__fmul_rn(y, f))) + 1; };
+  const float places = PLACES;
+  const uint32_t narrow = w <= 4.f * places ? part(places) : max(part(ROUNDS), root(w, 1.f / 64.f));
+  const uint32_t traffic = max(root(x, 1.f / 6150.f), (uint32_t)MIN_SPLIT), fill = max(part(places), min(part(places / 2), 8u));
+  return SplitLen{max(narrow, (uint32_t)MIN_SPLIT), max(fill, traffic), 2 * traffic};
 }
 // (rounded to the nearer number, and as even as they can be)
 __device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
-  const uint32_t len = s.rows <= R_NARROW ? l.narrow : l.wide;
-  return max(((uint32_t)s.tiles + len / 2) / len, 1u);
+  const bool wide = s.rows > R_NARROW;
+  const uint32_t len = wide ? l.wide : l.narrow, n = ((uint32_t)s.tiles + len / 2) / len;
+  return wide && (uint32_t)s.tiles <= l.whole ? 1u : max(n, 1u);
 }
 // rows of sums that a sequence keeps: [key / value head][split][row]
 __device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& s, uint32_t splits) {
@@ -953,14 +976,14 @@ Bounds bounds(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
   const int64_t tiles = (capacity + KT - 1) / KT, rows = T * (H / Hkv);
   const int64_t blocks = (batch < T ? batch : T) + rows / R_WIDE;      // of rows: a sequence's last one may be short
   const int64_t most = (tiles + MIN_SPLIT - 1) / MIN_SPLIT;           // splits of a sequence
-  // ... and of all: w / len, which grows with w, beside one for each item
+  // ... and of all beside one for each item: w / len, which grows with w; wide ones at most PLACES
   const double w = (double)Hkv * (double)blocks * (double)tiles;
-  const int64_t cuts = std::min<int64_t>(ROUNDS, std::max<int64_t>((int64_t)(8.0 * std::sqrt(w)) + 2, PLACES));
+  const int64_t cuts = std::min<int64_t>(ROUNDS, std::max<int64_t>((int64_t)(8.0 * std::sqrt(w)) + 2, PLACES)), wide = rows > R_NARROW ? PLACES : 0;
   Bounds b;
   b.split = most > 1;
-  b.items = std::min(Hkv * blocks * most, Hkv * blocks + cuts);
-  // rows of sums: all rows in every split, or those of the splits there are (a sequence of several has at most twice its share)
-  b.part_rows = b.split ? std::min(T * H * most, 2 * cuts * std::min<int64_t>(rows, R_WIDE)) : 0;
+  b.items = std::min(Hkv * blocks * most, Hkv * blocks + cuts + wide);
+  // rows of sums: all rows in every split, or those of the splits there are (narrow: of several at most twice a sequence's share, wide: 5 / 4)
+  b.part_rows = b.split ? std::min(T * H * most, 2 * cuts * std::min<int64_t>(rows, R_NARROW) + wide * R_WIDE * 5 / 4) : 0;
   return b;
 }
 
