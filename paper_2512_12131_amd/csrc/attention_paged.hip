@@ -196,8 +196,13 @@ __device__ __forceinline__ void first_window(ArgPtr a, Pages& pg, const PageSour
 }
 // Descriptors of a group's keys and values: the same place in both.
 struct Group { uint64_t at; uint32_t bytes; };
+// A vector write of a scalar needs five wait states before a load's descriptor has it, and the compiler does not see the loads: asked for right before
+// them, the group waits (SETTLE); asked for a slot of other work earlier, it does not have to (the machine code is checked for either).
+template <bool SETTLE = true>
 __device__ __forceinline__ Group group(const Pages& pg, int g) {
-  const uint32_t place = __builtin_amdgcn_readlane(pg.place, g & 63), bytes = __builtin_amdgcn_readlane(pg.bytes, g & 63);
+  const uint32_t place = __builtin_amdgcn_readlane(pg.place, g & 63);
+  uint32_t bytes = __builtin_amdgcn_readlane(pg.bytes, g & 63);
+  if constexpr (SETTLE) asm volatile("s_nop 4" : "+s"(bytes));
   return Group{(uint64_t)place << 4, bytes};
 }
 __device__ __forceinline__ rsrc_t group_rsrc(const Group& g, const uint16_t* base) {
@@ -555,10 +560,10 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
   Pages pk, pv;                           // windows of K's loads and of V's, which follow two tiles behind
   first_window<8>(in, pk, src, t0, lane);
   pv = pk;
-  auto dma = [&](bool isV, int t, int i) {      // load i of tile t into the slot of its parity; past the keys: zeros
-    lds_dma_at(group_rsrc(group(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), isV ? w.cV : w.cK),
-               w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096, isV ? w.offV : w.offK);
+  auto load = [&](const Group& g, bool isV, int t, int i) {     // load i of tile t into the slot of its parity; past the keys: zeros
+    lds_dma_at(group_rsrc(g, isV ? w.cV : w.cK), w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096, isV ? w.offV : w.offK);
   };
+  auto dma = [&](bool isV, int t, int i) { load(group(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), isV, t, i); };
   if (t0 < t1) {
 #pragma unroll
     for (int i = 0; i < 4; i++) dma(false, t0, i);
@@ -613,10 +618,9 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  auto next_loads = [&](int t, int i) {         // into the slots just left
-    if (i < 4) dma(true, t + 1, i);
-    else dma(false, t + 3, i - 4);
-  };
+  // loads 0 .. 7 of tile t's iteration, into the slots just left: V of t + 1, K of t + 3
+  auto next_load = [&](int t, int i) { dma(i < 4, t + (i < 4 ? 1 : 3), i & 3); };
+  auto next_group = [&](int t, int i) { return group<false>(i < 4 ? pv : pk, (t + (i < 4 ? 1 : 3)) * 8 + (i & 3) * 2 + (wave >> 1)); };
   auto windows = [&](int t) {                   // of the loads of tile t's iteration
     next_window<8>(pk, src, t + 3, lane);
     const bool over = ((t + 1) & 7) == 0;
@@ -652,6 +656,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
 #pragma unroll
       for (int e = 0; e < 16; e++) sn[nb][e] = 0.f;
     float mx0 = -INFINITY, mx1 = -INFINITY;
+    Group ahead = {};
     unroll_for<32>([&](auto Nc) {
       constexpr int n = decltype(Nc)::value;
       if constexpr (n < 16) sn[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[n % AHEAD], qf[n >> 1], sn[n & 1], 0, 0, 0);
@@ -669,7 +674,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
           else read(std::integral_constant<int, x - 32>{}, sK2, sV);
         }
       });
-      if constexpr (n > BARRIER && n <= BARRIER + 8) next_loads(t, n - BARRIER - 1);
+      if constexpr (n > BARRIER && n <= BARRIER + 8) load(ahead, n - BARRIER <= 4, t + (n - BARRIER <= 4 ? 1 : 3), (n - BARRIER - 1) & 3);
       softmax_to(sc, std::integral_constant<int, softmax_elems(n - 1)>{}, std::integral_constant<int, softmax_elems(n)>{});
       if constexpr (n >= 18 && n < 26) {                            // maximum of the new scores
         constexpr int e = (n - 18) * 2;
@@ -677,6 +682,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
         mx1 = fmaxf(fmaxf(mx1, sn[1][e]), sn[1][e + 1]);
       }
       if constexpr (softmax_elems(n - 1) != softmax_elems(n)) asm volatile("" : "+v"(sum));
+      if constexpr (n >= BARRIER && n < BARRIER + 8) ahead = next_group(t, n - BARRIER);
       if constexpr (n == 25) asm volatile("" : "+v"(mx0), "+v"(mx1));
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -726,7 +732,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     unroll_for<AHEAD>([&](auto I) { read(std::integral_constant<int, 16 + decltype(I)::value>{}, smem, sV); });
     if (t + 1 < t1) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) next_loads(t, i);
+      for (int i = 0; i < 8; i++) next_load(t, i);
     }
     softmax_to(sa, std::integral_constant<int, 0>{}, std::integral_constant<int, 16>{});
     unroll_for<16>([&](auto I) {
@@ -744,7 +750,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     bad |= careful(w, t);
     if (t + 1 < t1) {
 #pragma unroll
-      for (int i = 0; i < 8; i++) next_loads(t, i);
+      for (int i = 0; i < 8; i++) next_load(t, i);
     }
   }
   return bad;
@@ -788,6 +794,8 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
     store_acc_T(a->o + t * a->ldo + head * HD, st.o, l == 0.f ? 0.f : 1.f / l, lane);
     if (a->lse && lane < 32) a->lse[t * a->H + head] = l == 0.f ? -INFINITY : st.m * a->scale + logf(l);
   } else {
+    if (lane < 32) a->part_ml[part0 + r] = make_float2(st.m, l);
+    if (t0 >= t1) return;               // (a split behind all of the block's keys: its sums are not read)
     float* p = a->part_o + (int64_t)(part0 + r) * HD;
 #pragma unroll
     for (int hb = 0; hb < 4; hb++)
@@ -795,7 +803,6 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
       for (int g4 = 0; g4 < 4; g4++)
         *reinterpret_cast<float4*>(p + hb * 32 + 8 * g4 + 4 * (lane >> 5)) =
             make_float4(st.o[hb][g4 * 4], st.o[hb][g4 * 4 + 1], st.o[hb][g4 * 4 + 2], st.o[hb][g4 * 4 + 3]);
-    if (lane < 32) a->part_ml[part0 + r] = make_float2(st.m, l);
   }
 }
 

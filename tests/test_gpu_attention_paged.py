@@ -65,6 +65,9 @@ CASES = [
     ([(130, 1500)], 16, 16, 24, "token", 0, 0),
     ([(200, 5)], 4, 2, 16, "token", 0, 0), ([(3, 1), (2, 0), (5, -4)], 4, 1, 16, "token", 0, 0),    # rows that see nothing
     ([(2, 70)], 40, 1, 16, "token", 0, 0), ([(1, 70)], 64, 1, 16, "token", 0, 0),                   # more heads in a group than a tile has rows
+    ([(1, 400), (2, 517), (1, 64)] * 24, 2, 2, 16, "head", 0, 1),                 # split, and more sequences than lanes
+    ([(60, 1200), (1, 900), (40, 70)], 3, 1, 32, "token", 1, 0),                  # split, an odd number of heads
+    ([(140, 260), (30, 1100)], 4, 2, 8, "wide", 0, 2),                            # splits behind all keys of the first blocks
 ]
 
 
@@ -281,6 +284,74 @@ def test_on_a_stream_of_its_own():
         o2, lse2 = B.lr_attention_paged_fwd(q, H=8, **c)
     s.synchronize()
     assert torch.equal(o[:, :8 * HD], o2) and torch.equal(lse, lse2)
+
+
+# Real sizes, in the long form of an item and with keys in many splits: (new tokens, keys) of the sequences, H, Hkv, page
+@pytest.mark.parametrize("seqs,H,Hkv,page", [([(512, 8192)], 32, 8, 16), ([(1, 16384), (1, 300)], 32, 8, 48), ([(2047, 2047), (130, 900)], 8, 8, 64),
+                                             ([(1, 4096)] * 6 + [(200, 4096), (77, 3000)], 32, 8, 16), ([(600, 5000)], 6, 1, 24)])
+def test_real_sizes(seqs, H, Hkv, page):
+    """Against 64 bits on the GPU, every element; bounds as above."""
+    print(f"paged attention {seqs} H={H} Hkv={Hkv} page={page}", flush=True)
+    c, T = make(seqs, Hkv, HD, page, seed=11)
+    q, o, lse = call(c, T, H)
+    t0, grp = 0, H // Hkv
+    for b, (n, kv) in enumerate(seqs):
+        k, v = (x.double().view(kv, Hkv, HD) for x in _dense(c, b, kv))
+        hidden = torch.arange(kv, device=DEV)[None] > torch.arange(kv - n, kv, device=DEV)[:, None]
+        for h in range(H):
+            qq, kk, vv = q[t0:t0 + n, h * HD:(h + 1) * HD].double(), k[:, h // grp].contiguous(), v[:, h // grp].contiguous()
+            s = (qq @ kk.t().contiguous()) * HD ** -0.5
+            d = 128 * 2.0 ** -24 * (qq.abs() @ kk.abs().t().contiguous() * HD ** -0.5).masked_fill(hidden, 0).amax(1)
+            s = s.masked_fill(hidden, float("-inf"))
+            l = torch.logsumexp(s, 1)
+            w = torch.exp(s - l[:, None])
+            ref, mag = w @ vv, w @ vv.abs()
+            err = (o[t0:t0 + n, h * HD:(h + 1) * HD].double() - ref).abs()
+            assert bool((err <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * d + 2.0 ** -18)[:, None] * mag).all()), (b, h)
+            lerr = (lse[t0:t0 + n, h].double() - l).abs()
+            assert bool((lerr <= d + 2.0 ** -20 * (1 + l.abs()) + kv * 2.0 ** -24).all()), (b, h, float(lerr.max()))
+        t0 += n
+    again = call(c, T, H)
+    assert torch.equal(o, again[1]) and torch.equal(lse, again[2])
+
+
+def test_sequences_that_share_pages():
+    """A common beginning in the same pages, and a page twice in one row: as with copies of them."""
+    H, Hkv, page = 8, 2, 16
+    c, T = make([(1, 100), (40, 130), (3, 64)], Hkv, HD, page, seed=12, extra_pages=30)
+    table = c["page_table"].clone()
+    table[1, :4], table[2, :4], table[1, 6] = table[0, :4], table[0, :4], table[1, 5]
+    q, o, lse = call({**c, "page_table": table}, T, H)
+    compare(o, lse, q, {**c, "page_table": table}, H)
+    copies, free = table.clone(), [i for i in range(c["k_cache"].shape[0]) if i not in table.flatten().tolist()]
+    for at in [(1, j) for j in range(4)] + [(2, j) for j in range(4)] + [(1, 6)]:
+        to = free.pop()
+        for x in (c["k_cache"], c["v_cache"]):
+            x[to] = x[int(table[at])]
+        copies[at] = to
+    _, o2, lse2 = call({**c, "page_table": copies}, T, H)
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_two_graphs_on_one_workspace():
+    """Replayed in turn: what the other left in the workspace is not read."""
+    H, Hkv = 8, 2
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    runs = []
+    for seqs, seed in (([(1, 3000), (1, 500)], 13), ([(70, 1500), (2, 900)], 14)):
+        c, T = make(seqs, Hkv, HD, 16, seed=seed)
+        q, o, lse = call(c, T, H)
+        out, out_lse = torch.zeros_like(o), torch.zeros_like(lse)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.lr_attention_paged_fwd(q, H=H, o=out, lse=out_lse, ws=ws, **c)
+        runs.append((graph, out, out_lse, o, lse, c, q))
+    for k in (0, 1, 0, 0, 1, 1, 0):
+        graph, out, out_lse, o, lse, _, _ = runs[k]
+        out.zero_(), out_lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, o) and torch.equal(out_lse, lse), k
 
 
 def test_a_workspace_of_the_size_asked_for_is_enough():

@@ -145,3 +145,26 @@ def test_far_pages():
     for t, (pg, row) in enumerate([(n_pages - 1, 255), (3, 0), (3, 1), (8200, 142), (8200, 143)]):
         assert torch.equal(cache[pg, row].flatten(), k[t]) and torch.equal(vc[pg, row].flatten(), v[t])
     assert int((cache.flatten(1).abs().amax(1) > 0).sum()) == 3
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [0, 64, 128])
+def test_many_tokens(rot, interleaved):
+    """More tokens than find a workgroup each: the bits of lr_rope_at, in their places."""
+    H, Hkv, hd, page = 6, 3, 128, 24
+    c, T = make([(1500, 1501), (1, 800), (0, 5), (2333, 2333), (31, 40)], Hkv, hd, page, "head", seed=3, lead=1, tail=2)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    q, k, v = (torch.randn((T, w * hd), generator=g, device=DEV).to(BF) for w in (H, Hkv, Hkv))
+    cu, kv_len, table = lists(c)
+    placed = np.array(po.places(cu, kv_len, table, page, c["k_cache"].shape[0], T))
+    t, pos, pg, row = (torch.from_numpy(placed[:, i].copy()).to(DEV) for i in (0, 2, 3, 4))
+    tables = B.lr_rope_table(2400, rot, device=DEV) if rot else None
+    want_k, want_v = c["k_cache"].clone(), c["v_cache"].clone()
+    all_pos = torch.full((T,), -1, dtype=torch.int32, device=DEV)
+    all_pos[t] = pos.to(torch.int32)
+    turn = lambda x, w: B.lr_rope_at(x, *tables, w, hd, pos=all_pos, interleaved=interleaved) if rot else x
+    want_k[pg, row], want_v[pg, row] = turn(k, Hkv).view(T, Hkv, hd)[t], v.view(T, Hkv, hd)[t]
+    got = B.lr_kv_append(k, v, rope=tables, interleaved=interleaved, q=q, H=H, **c)
+    torch.cuda.synchronize()
+    assert torch.equal(c["k_cache"], want_k) and torch.equal(c["v_cache"], want_v)
+    assert torch.equal(got[t], turn(q, H)[t])

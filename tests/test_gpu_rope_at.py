@@ -48,7 +48,7 @@ def _close(got, ref, mag, dtype):
 
 
 # T, H, hd, rot, columns behind the heads
-SHAPES = [(1, 1, 128, 128, 0), (16, 32, 128, 128, 0), (37, 3, 80, 32, 8), (130, 5, 64, 16, 0), (5, 40, 256, 240, 24), (257, 2, 192, 192, 136),
+SHAPES = [(1, 1, 128, 128, 0), (2, 1, 8192, 64, 0), (16, 32, 128, 128, 0), (37, 3, 80, 32, 8), (130, 5, 64, 16, 0), (5, 40, 256, 240, 24), (257, 2, 192, 192, 136),
           (3, 7, 16, 16, 0), (1, 300, 96, 48, 0)]
 
 
@@ -82,6 +82,23 @@ def test_rotation(T, H, hd, rot, extra, dtype):
             torch.cuda.synchronize()
             assert torch.equal(place[inside][:, :H * hd], out[inside][:, :H * hd])
             assert torch.equal(place[~inside], x[~inside]) and torch.equal(place[:, H * hd:], x[:, H * hd:])
+
+
+@pytest.mark.parametrize("hd,rot", [(80, 32), (96, 96), (128, 8)])
+def test_fp32_rows_that_start_on_16_bytes(hd, rot):
+    """In vectors of four: the bits of the form that takes rows from anywhere."""
+    T, H = 123, 3
+    g = torch.Generator(device=DEV).manual_seed(5)
+    x = torch.randn((T, H * hd), generator=g, device=DEV)
+    pos = torch.randint(0, 300, (T,), generator=g, device=DEV, dtype=torch.int32)
+    cos, sin = B.lr_rope_table(300, rot, device=DEV)
+    odd = torch.zeros((T, H * hd + 1), device=DEV)
+    odd[:, 1:] = x
+    for interleaved in (False, True):
+        a = B.lr_rope_at(x, cos, sin, H, hd, pos=pos, interleaved=interleaved)
+        b = B.lr_rope_at(odd[:, 1:], cos, sin, H, hd, pos=pos, interleaved=interleaved)
+        torch.cuda.synchronize()
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])

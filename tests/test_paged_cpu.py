@@ -95,6 +95,18 @@ def test_attention_paged_arguments():
     assert _paged(T=0) == 0 and _paged(_cache(batch=0)) == 0
 
 
+@pytest.mark.parametrize("H,kv", [(32, 8), (16, 16), (5, 1)])
+def test_a_workspace_for_more_tokens_or_keys_serves_for_fewer(H, kv):
+    size = lambda T, batch, cols: B.lib().lr_attention_paged_workspace_bytes(_cache(n_kv_heads=kv, batch=batch, max_pages=cols, table_ld=cols), T, H)
+    for batch in (1, 7, 64, 300):
+        sizes = [size(T, batch, 100) for T in [*range(1, 200), *range(200, 20000, 333)]]
+        assert sizes == sorted(sizes)
+        sizes = [size(64, batch, cols) for cols in range(1, 3000, 7)]
+        assert sizes == sorted(sizes)
+    assert size(1, 1, 8) == 0 and size(1, 1, 9) > 0              # 128 keys are one split
+    assert max(size(T, 64, 1 << 20) for T in (1, 64, 4096, 1 << 20)) < 128 << 20
+
+
 T4 = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
 I4 = lambda *s: torch.zeros(s, dtype=torch.int32)
 KC, TAB, CU, LEN, COS = T4(6, 16, 2, 128), I4(3, 4), I4(4), I4(3), torch.zeros(64, 64)

@@ -12,7 +12,9 @@ from paper_2512_12131_amd import build as bld
 pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None, reason="needs hipcc")
 
 
-def test_descriptors_of_inline_loads_are_settled(tmp_path):
+def test_descriptors_of_inline_loads_are_settled(tmp_path, monkeypatch):
+    # (loads that pass by the caches among them)
+    monkeypatch.setattr(test_isa_cpu, "LOAD", re.compile(r"buffer_load_dword(?:x4)? v\d+, s\[(\d+):(\d+)\], 0 offen (?:nt )?lds"))
     test_isa_cpu.test_descriptors_of_inline_loads_are_settled("attention_paged.hip", tmp_path)
 
 
