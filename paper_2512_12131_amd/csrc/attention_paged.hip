@@ -834,11 +834,13 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
       items = (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.blocks;
       parts = part_rows_of(a, s, splits);
     }
-    item_end = item0 + wave_scan(items);
+    // wide sequences' items, which take longer, before the others' of the same 64
+    const uint32_t wide = s.rows > R_NARROW ? items : 0, wide_end = wave_scan(wide), other_end = wave_scan(items - wide);
+    item_end = item0 + (wide > 0 ? wide_end : last_lane(wide_end) + other_end);
     part_end = part0 + wave_scan(parts);
-    hit = __builtin_amdgcn_ballot_w64(v < item_end);
+    hit = __builtin_amdgcn_ballot_w64(v - (item_end - items) < items);
     if (hit) break;
-    item0 = last_lane(item_end);
+    item0 += last_lane(wide_end) + last_lane(other_end);
     part0 = last_lane(part_end);
   }
   if (hit == 0) return;
