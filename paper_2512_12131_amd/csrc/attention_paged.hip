@@ -109,10 +109,12 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
 //   narrow  w / ROUNDS, but more than sqrt(w / 64): a split's way in and out costs as much as some tiles, so splits should grow with the work: s
 //           splits save w (1 - 1 / s) and cost s.  While w is few times PLACES, w / PLACES, so that every item finds a place on the chip at
 //           once (one sequence of 4096 keys 12.4 -> 10.6 us, 8 of 2000 20.4 -> 16.8, one of 16384 20.1 -> 18.0).
-//   wide    w / PLACES (of little work half of the places, a CU each): more splits than places save nothing.  And no less than sqrt(x / 6150), x the tiles times their rows: len tiles take len * 1.6
-//           us, and x / len rows of sums 0.26 ns each on their way through memory.  A sequence of two of the latter is not split, since the join
-//           takes some us by itself.  (us, against the narrow rule for both: a prompt of 777 tokens 31.2 -> 25.9, of 2048 70 -> 56, 512
-//           tokens over 8192 keys 93 -> 83, over 32768 301 -> 268, the mixed batch 101 -> 93.)
+//   wide    w / PLACES (of little work half of the places, a CU each): more splits than places save nothing.  And no less than
+//           sqrt(x / 6150), x the tiles times their rows: len tiles take len * 1.6
+//           us, and x / len rows of sums 0.26 ns each on their way through memory.  A sequence of two of the latter, or of three tiles, is not
+//           split, since the join takes some us by itself.  (us, against the narrow rule for both: a prompt of 777 tokens 31.2 -> 25.9, of
+//           2048 70 -> 56, 512 tokens over 8192 keys 93 -> 83, over 32768 301 -> 268, the mixed batch 101 -> 93.  Four tiles split in two: 10
+//           tokens over 250 keys 12.8 -> 11.7; three: 3 prompts of 108 behind 26 keys 13.1 -> 14.6.)
 struct SplitLen { uint32_t narrow, wide, whole; };      // whole: wide sequences of up to so many tiles are not split
 // Sum over the lanes, in an order of its own: both kernels get the same bits.  (Products and sums are rounded one by one wherever this is inlined.)
 __device__ __forceinline__ float lanes_sum(float x) {
@@ -144,7 +146,7 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& fir
   const float places = PLACES;
   const uint32_t narrow = w <= 4.f * places ? part(places) : max(part(ROUNDS), root(w, 1.f / 64.f));
   const uint32_t traffic = max(root(x, 1.f / 6150.f), (uint32_t)MIN_SPLIT), fill = max(part(places), min(part(places / 2), 8u));
-  return SplitLen{max(narrow, (uint32_t)MIN_SPLIT), max(fill, traffic), 2 * traffic};
+  return SplitLen{max(narrow, (uint32_t)MIN_SPLIT), max(fill, traffic), max(2 * root(x, 1.f / 6150.f), 3u)};
 }
 // (rounded to the nearer number, and as even as they can be)
 __device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
@@ -994,8 +996,9 @@ Bounds bounds(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
   Bounds b;
   b.split = most > 1;
   b.items = std::min(Hkv * blocks * most, Hkv * blocks + cuts + wide);
-  // rows of sums: all rows in every split, or those of the splits there are (narrow: of several at most twice a sequence's share, wide: 5 / 4)
-  b.part_rows = b.split ? std::min(T * H * most, 2 * cuts * std::min<int64_t>(rows, R_NARROW) + wide * R_WIDE * 5 / 4) : 0;
+  // rows of sums: all rows in every split, or those of the splits there are (rounded to the nearer number, two or more are at most 4 / 3 of a
+  // sequence's share)
+  b.part_rows = b.split ? std::min(T * H * most, (cuts * std::min<int64_t>(rows, R_NARROW) + wide * R_WIDE) * 4 / 3 + 1) : 0;
   return b;
 }
 
