@@ -337,7 +337,7 @@ int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t
  * outside [0, n_pages) is no page, keys past max_pages * page_size do not exist.
  * page_size, head_dim and the strides (elements) are multiples of 8, k and v 16-byte aligned (LR_EALIGN); pages of both layouts
  * [page_size, n_kv_heads, head_dim] and [n_kv_heads, page_size, head_dim] are a matter of the strides.  Limits (LR_EUNSUPPORTED):
- * 2^35 elements from the first to the last of k, 2^31 - 1 keys of a sequence, 2^26 tokens of a call, token_stride < 2^26.       */
+ * 2^35 elements from the first to the last of k, 2^31 - 1 keys of a sequence, 2^16 sequences and 2^25 tokens of a call, token_stride < 2^26.  */
 typedef struct {
   void *k, *v;
   int64_t n_pages, page_size, n_kv_heads, head_dim;
@@ -362,7 +362,8 @@ int lr_kv_append(const lr_kv_cache* cache, const void* k, int64_t ldk, const voi
  * h / (H / n_kv_heads); lse[T, H] (fp32, NULL: not written) = log of the softmax's sum.  Any mixture of long and single-token sequences.
  * A token that sees no key has o = 0 and lse = -infinity; a page number that is no page holds zeros.  H % n_kv_heads == 0, scale > 0.
  * dt LR_BF16, head_dim 128, causal 1, otherwise LR_EUNSUPPORTED.  The workspace holds the parts of sequences whose keys are split over workgroups;
- * its size depends on T, H and the cache's sizes, not on the lists.                                                            */
+ * its size depends on T, H and the cache's sizes, not on the lists.  o overlaps nothing that is read.  LR_EUNSUPPORTED also where T * H passes
+ * 2^31 - 1, or the sequences' heads and rows (n_kv_heads of each sequence that can have a token, and one for every 128 of T * H) 2^24 - 2^12.  */
 size_t lr_attention_paged_workspace_bytes(const lr_kv_cache* cache, int64_t T, int64_t H);
 int lr_attention_paged_fwd(const lr_kv_cache* cache, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse,
                            int64_t T, int64_t H, float scale, int causal, int dt, void* ws, size_t ws_bytes, void* stream);

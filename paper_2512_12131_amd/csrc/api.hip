@@ -1478,7 +1478,7 @@ static int check_cache(const lr_kv_cache* c, bool pointers, KvCache* out) {
   if (c->n_pages <= 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 || c->batch < 0 || c->max_pages <= 0 ||
       c->table_ld < c->max_pages || c->page_stride <= 0 || c->token_stride <= 0 || c->head_stride <= 0)
     return LR_EINVAL;
-  if (c->n_pages > most || c->page_size > most || c->max_pages > most / c->page_size || c->batch > (1 << 24) || c->n_kv_heads > (1 << 16) ||
+  if (c->n_pages > most || c->page_size > most || c->max_pages > most / c->page_size || c->batch > (1 << 16) || c->n_kv_heads > (1 << 16) ||
       c->head_dim > (1 << 16) || c->token_stride >= (1 << 26) || c->page_stride > far || c->head_stride > far ||
       (c->n_pages > 1 && c->page_stride > far / (c->n_pages - 1)) || c->table_ld > far / (c->batch > 0 ? c->batch : 1))
     return LR_EUNSUPPORTED;
@@ -1494,7 +1494,7 @@ static int check_cache(const lr_kv_cache* c, bool pointers, KvCache* out) {
                  FastDiv::of(c->page_size)};
   return LR_OK;
 }
-constexpr int64_t PAGED_TOKENS = (int64_t)1 << 26;
+constexpr int64_t PAGED_TOKENS = (int64_t)1 << 25;
 
 int lr_kv_append(const lr_kv_cache* cache, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, void* q_out,
                  int64_t ldqo, int64_t T, int64_t H, const float* cos_tab, const float* sin_tab, int64_t table_rows, int64_t rot,
@@ -1526,7 +1526,7 @@ static int check_paged(const lr_kv_cache* cache, bool pointers, int64_t T, int64
   TRY(check_cache(cache, pointers, c));
   if (T < 0 || H <= 0 || H > (1 << 16) || H % c->n_kv_heads) return LR_EINVAL;
   if (T > PAGED_TOKENS || T * H > 0x7fffffffLL || c->head_dim != 128) return LR_EUNSUPPORTED;
-  return LR_OK;
+  return attention_paged_fits(T, (int)H, c->n_kv_heads, c->batch, c->capacity) ? LR_OK : LR_EUNSUPPORTED;
 }
 
 size_t lr_attention_paged_workspace_bytes(const lr_kv_cache* cache, int64_t T, int64_t H) {

@@ -245,6 +245,7 @@ hipError_t k_kv_append(const KvCache& c, const void* k, int64_t ldk, const void*
                        hipStream_t);
 
 // ---- attention over the pages of a cache (attention_paged.hip) -----------------------------------
+bool attention_paged_fits(int64_t T, int H, int Hkv, int batch, int64_t capacity);      // a launch has room for the items
 size_t attention_paged_ws_bytes(int64_t T, int H, int Hkv, int batch, int64_t capacity);
 hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int64_t T, int H, float scale,
                                 void* ws, hipStream_t);

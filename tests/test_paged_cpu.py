@@ -95,6 +95,19 @@ def test_attention_paged_arguments():
     assert _paged(T=0) == 0 and _paged(_cache(batch=0)) == 0
 
 
+def test_calls_past_a_launch_are_refused():
+    """Sequences and tokens that a launch's lanes (2^32) cannot hold, and lists that every workgroup would read for too long."""
+    assert _append(_cache(batch=(1 << 16) + 1)) == EUNSUPPORTED and _paged(_cache(batch=(1 << 16) + 1)) == EUNSUPPORTED
+    assert _append(T=(1 << 25) + 1) == EUNSUPPORTED and _paged(T=(1 << 25) + 1) == EUNSUPPORTED
+    big = dict(n_kv_heads=256, page_stride=16 * 256 * 128, token_stride=256 * 128, batch=1 << 16)
+    for T, kv, batch in ((1 << 16, 256, 1 << 16), (1 << 20, 1024, 1 << 14), ((1 << 25) - 1, 64, 1)):
+        cache = lambda: _cache(**{**big, "n_kv_heads": kv, "batch": batch})
+        args = dict(T=T, H=kv, ldq=kv * 128, ldo=kv * 128)
+        assert B.lib().lr_attention_paged_workspace_bytes(cache(), T, kv) == 0, (T, kv)
+        assert _paged(cache(), **args) == EUNSUPPORTED, (T, kv)
+    assert B.lib().lr_attention_paged_workspace_bytes(_cache(**{**big, "batch": 1 << 15, "max_pages": 64, "table_ld": 64}), 1 << 15, 256) > 0
+
+
 @pytest.mark.parametrize("H,kv", [(32, 8), (16, 16), (5, 1)])
 def test_a_workspace_for_more_tokens_or_keys_serves_for_fewer(H, kv):
     size = lambda T, batch, cols: B.lib().lr_attention_paged_workspace_bytes(_cache(n_kv_heads=kv, batch=batch, max_pages=cols, table_ld=cols), T, H)
