@@ -162,41 +162,51 @@ __device__ __forceinline__ uint32_t part_rows_of(const PagedArgs& a, const Seq& 
 }
 
 // ---- pages ----------------------------------------------------------------------------------------------
-// Of the 64 groups of one window: place, bytes from there on that are read (0: none), and the next window's page numbers.
+// Of the 64 groups of one window: place, and bytes from there on that are read (0: none).
 struct Pages {
   uint32_t place, bytes;
-  int raw;
 };
 struct PageSource {
   const int32_t* row;     // of the page table
   int end;                // keys that are read end here
   uint32_t head;          // of the key / value head, in units of 16 bytes
+  int* spot;              // in LDS, the wavefront's own: the next window's page numbers
 };
+constexpr int SPOTS = 4 * TILE_BYTES;      // behind the tiles, 256 bytes for a wavefront
+static_assert(SPOTS + 4 * 256 <= LDS_BYTES, "page numbers behind the tiles");
 __device__ __forceinline__ int ask_pages(ArgPtr a, const PageSource& p, int w, int lane) {
   const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u;
   return key < (uint32_t)p.end ? p.row[div_by(key, a->c.by_page.mul, a->c.by_page.shift)] : -1;
 }
-__device__ __forceinline__ void places(ArgPtr a, Pages& pg, const PageSource& p, int w, int lane) {
+// ... into the spot, on the way while others are worked on.  A load into registers would not do: the compiler waits for it where the loop comes round,
+// and so for all tiles' loads before it (a prompt of 2048 tokens 57.5 -> 53.8 us without, 64 single tokens over 1000 keys 47.1 -> 45.5).
+__device__ __forceinline__ void ask_ahead(ArgPtr a, const PageSource& p, int w, int lane) {
+  const uint32_t col = div_by((uint32_t)w * 512u + (uint32_t)lane * 8u, a->c.by_page.mul, a->c.by_page.shift);
+  const uint32_t cols = div_by((uint32_t)p.end - 1u, a->c.by_page.mul, a->c.by_page.shift) + 1u;
+  const uint64_t row = (uint64_t)(uintptr_t)p.row;
+  lds_dma4_at(rsrc_t{(uint32_t)row, (uint32_t)(row >> 32), cols * 4u, 0x00020000u}, (uint32_t)(uintptr_t)LRB_LDS_PTR(p.spot), col * 4u);
+}
+__device__ __forceinline__ void places(ArgPtr a, Pages& pg, int raw, const PageSource& p, int w, int lane) {
   const uint32_t key = (uint32_t)w * 512u + (uint32_t)lane * 8u, row = (uint32_t)(a->c.token_stride >> 3);
   const uint32_t in = key - div_by(key, a->c.by_page.mul, a->c.by_page.shift) * (uint32_t)a->c.page_size;
-  pg.place = (uint32_t)((uint64_t)(uint32_t)pg.raw * (uint64_t)(a->c.page_stride >> 3) + (uint64_t)in * row) + p.head;
+  pg.place = (uint32_t)((uint64_t)(uint32_t)raw * (uint64_t)(a->c.page_stride >> 3) + (uint64_t)in * row) + p.head;
   const int rows = min(p.end - (int)key, 8);
-  pg.bytes = (uint32_t)pg.raw < (uint32_t)a->c.n_pages && rows > 0 ? (uint32_t)(rows - 1) * row * 16u + 256u : 0u;
+  pg.bytes = (uint32_t)raw < (uint32_t)a->c.n_pages && rows > 0 ? (uint32_t)(rows - 1) * row * 16u + 256u : 0u;
 }
-// Before the loads of tile t, TILES of them to a window: the next window where t is its first one; its page numbers are asked for half a window ahead.
+// Before the loads of tile t, TILES of them to a window: the next window where t is its first one; its page numbers are asked for half a window ahead, and
+// have landed by now, since the loop waits for younger loads.
 template <int TILES>
 __device__ __forceinline__ void next_window(Pages& pg, const PageSource& p, int t, int lane) {
   Pages n = pg;
-  if ((t & (TILES - 1)) == 0) places(args_again(), n, p, t / TILES, lane);
-  else if ((t & (TILES - 1)) == TILES / 2) n.raw = ask_pages(args_again(), p, t / TILES + 1, lane);
+  if ((t & (TILES - 1)) == 0) places(args_again(), n, p.spot[lane], p, t / TILES, lane);
+  else if ((t & (TILES - 1)) == TILES / 2) ask_ahead(args_again(), p, t / TILES + 1, lane);
   pg = n;
 }
 template <int TILES>
 __device__ __forceinline__ void first_window(ArgPtr a, Pages& pg, const PageSource& p, int t, int lane) {
-  pg.raw = ask_pages(a, p, t / TILES, lane);
-  const int next = ask_pages(a, p, t / TILES + 1, lane);
-  places(a, pg, p, t / TILES, lane);
-  pg.raw = next;
+  const int raw = ask_pages(a, p, t / TILES, lane);
+  p.spot[lane] = ask_pages(a, p, t / TILES + 1, lane);
+  places(a, pg, raw, p, t / TILES, lane);
 }
 // Descriptors of a group's keys and values: the same place in both.
 struct Group { uint64_t at; uint32_t bytes; };
@@ -212,6 +222,26 @@ __device__ __forceinline__ Group group(const Pages& pg, int g) {
 __device__ __forceinline__ rsrc_t group_rsrc(const Group& g, const uint16_t* base) {
   const uint64_t addr = (uint64_t)(uintptr_t)base + g.at;
   return rsrc_t{(uint32_t)addr, (uint32_t)(addr >> 32), g.bytes, 0x00020000u};
+}
+
+// For long runs of tiles: the groups' addresses in one of the caches, so that a descriptor is three lanes' values and nothing else (24 scalar
+// instructions less per tile and wavefront than from places: a wavefront that is alone on its SIMD is bound by how many instructions it issues).
+struct Spots { uint32_t lo, hi, bytes; };
+__device__ __forceinline__ Spots spots(const Pages& pg, const uint16_t* base) {
+  const uint64_t at = (uint64_t)(uintptr_t)base + ((uint64_t)pg.place << 4);
+  return Spots{(uint32_t)at, (uint32_t)(at >> 32), pg.bytes};
+}
+template <bool SETTLE>
+__device__ __forceinline__ rsrc_t spot_rsrc(const Spots& s, int g) {
+  uint32_t lo = __builtin_amdgcn_readlane(s.lo, g & 63), hi = __builtin_amdgcn_readlane(s.hi, g & 63);
+  uint32_t bytes = __builtin_amdgcn_readlane(s.bytes, g & 63);
+  if constexpr (SETTLE) asm volatile("s_nop 4" : "+s"(lo), "+s"(hi), "+s"(bytes));
+  return rsrc_t{lo, hi, bytes, 0x00020000u};
+}
+// lds_dma_at a fixed distance from an address
+template <uint32_t OFF>
+__device__ __forceinline__ void lds_dma_from(rsrc_t rs, uint32_t lds, uint32_t voff) {
+  asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds" ::"s"(lds), "i"(OFF), "v"(voff), "s"(rs) : "m0", "scc", "memory");
 }
 
 // ---- one wavefront's share of a tile: 32 rows, NB blocks of 32 keys ------------------------------------------
@@ -400,7 +430,7 @@ __device__ __forceinline__ void narrow_item(const Seq& s, const int32_t* table, 
   const float c = in->scale * LOG2E;
   const int blocks = (max(key_hi - key_lo, 0) + 31) / 32, share = (blocks + 3) / 4;
   const int j0 = min(wave * share, blocks) + key_lo / 32, j1 = min((wave + 1) * share, blocks) + key_lo / 32;
-  const PageSource src = {table, min(key_hi, j1 * 32), (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
+  const PageSource src = {table, min(key_hi, j1 * 32), (uint32_t)((int64_t)kvh * in->c.head_stride >> 3), (int*)(smem + SPOTS + wave * 256)};
   unsigned char* sK = smem + wave * 16384;
   unsigned char* sV = sK + 8192;
   const uint32_t ldsK = (uint32_t)(uintptr_t)LRB_LDS_PTR(sK), ldsV = ldsK + 8192;
@@ -556,6 +586,8 @@ __device__ __forceinline__ bool wide_short(ArgPtr in, Rows& st, const WideTiles&
   return bad;
 }
 
+template <int N>
+__device__ __forceinline__ void lds_reads_left() { __builtin_amdgcn_s_waitcnt(0xc07f | N << 8); }
 // An iteration works on two key tiles, as the dense forward's does: the scores of tile t + 1 and the output of tile t, with the softmax of tile t and
 // the maximum of the new scores threaded between their MFMAs, one barrier in the middle.
 constexpr int BARRIER = 12;
@@ -564,22 +596,31 @@ constexpr int softmax_elems(int n) { return n < 0 ? 0 : n < 16 ? 5 * (n + 1) / 4
 __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
   unsigned char* const smem = w.smem;
   const int t0 = w.t0, t1 = w.t1, tw = w.tw, lim0 = w.lim0, wave = w.wave, lane = w.lane;
-  Pages pk, pv;                           // windows of K's loads and of V's, which follow two tiles behind
-  first_window<8>(in, pk, src, t0, lane);
-  pv = pk;
-  auto load = [&](const Group& g, bool isV, int t, int i) {     // load i of tile t into the slot of its parity; past the keys: zeros
-    lds_dma_at(group_rsrc(g, isV ? w.cV : w.cK), w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096, isV ? w.offV : w.offK);
+  Pages pg;
+  first_window<8>(in, pg, src, t0, lane);
+  Spots pk = spots(pg, w.cK), pv = spots(pg, w.cV);      // windows of K's loads and of V's, which follow two tiles behind
+  auto next = [&](int t) {
+    next_window<8>(pg, src, t, lane);
+    Spots n = pk;
+    if ((t & 7) == 0) {
+      asm volatile("");                         // (a branch, not three selections per tile)
+      n = spots(pg, w.cK);
+    }
+    pk = n;
   };
-  auto dma = [&](bool isV, int t, int i) { load(group(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), isV, t, i); };
+  auto dma = [&](bool isV, int t, int i) {     // load i of tile t into the slot of its parity; past the keys: zeros
+    lds_dma_at(spot_rsrc<true>(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096,
+               isV ? w.offV : w.offK);
+  };
   if (t0 < t1) {
 #pragma unroll
     for (int i = 0; i < 4; i++) dma(false, t0, i);
 #pragma unroll
     for (int i = 0; i < 4; i++) dma(true, t0, i);
-    next_window<8>(pk, src, t0 + 1, lane);
+    next(t0 + 1);
 #pragma unroll
     for (int i = 0; i < 4; i++) dma(false, t0 + 1, i);
-    next_window<8>(pk, src, t0 + 2, lane);
+    next(t0 + 2);
   }
   f32x16 sa[2], sb[2];                          // scores of the tile whose softmax comes next, and of the one after it
   bf16x8 fr[AHEAD];                             // operands read ahead, slot n in fr[n % AHEAD]
@@ -627,12 +668,15 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
   };
   // loads 0 .. 7 of tile t's iteration, into the slots just left: V of t + 1, K of t + 3
   auto next_load = [&](int t, int i) { dma(i < 4, t + (i < 4 ? 1 : 3), i & 3); };
-  auto next_group = [&](int t, int i) { return group<false>(i < 4 ? pv : pk, (t + (i < 4 ? 1 : 3)) * 8 + (i & 3) * 2 + (wave >> 1)); };
+  auto next_rsrc = [&](int t, int i) { return spot_rsrc<false>(i < 4 ? pv : pk, (t + (i < 4 ? 1 : 3)) * 8 + (i & 3) * 2 + (wave >> 1)); };
   auto windows = [&](int t) {                   // of the loads of tile t's iteration
-    next_window<8>(pk, src, t + 3, lane);
-    const bool over = ((t + 1) & 7) == 0;
-    pv.place = over ? pk.place : pv.place;
-    pv.bytes = over ? pk.bytes : pv.bytes;
+    next(t + 3);
+    Spots n = pv;
+    if (((t + 1) & 7) == 0) {
+      asm volatile("");
+      n = spots(pg, w.cV);
+    }
+    pv = n;
   };
   // elements F .. T - 1 of a tile's softmax
   auto softmax_to = [&](const f32x16 (&x)[2], auto Fc, auto Tc) {
@@ -663,25 +707,33 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
 #pragma unroll
       for (int e = 0; e < 16; e++) sn[nb][e] = 0.f;
     float mx0 = -INFINITY, mx1 = -INFINITY;
-    Group ahead = {};
+    rsrc_t ahead = {};
     unroll_for<32>([&](auto Nc) {
       constexpr int n = decltype(Nc)::value;
+      if constexpr (n % 2 == 0 && n != BARRIER) {      // the last two operands may be on their way
+        lds_reads_left<(n < 14 || n >= 30 ? 2 : 4)>();
+        __builtin_amdgcn_sched_barrier(0);
+      }
       if constexpr (n < 16) sn[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[n % AHEAD], qf[n >> 1], sn[n & 1], 0, 0, 0);
       else out(Nc);
       if constexpr (n == BARRIER) {
         turn();
         if constexpr (decltype(LAST)::value) bad |= careful(w, t);
       }
-      // operands: V only from behind the barrier, then K of the tile after next
+      // operands, two at a time (half of the waits for them): V only from behind the barrier, then K of the tile after next
       unroll_for<32>([&](auto I) {
         constexpr int x = decltype(I)::value + AHEAD;               // slot that reads
-        constexpr int at = x - AHEAD < BARRIER && x >= 16 ? BARRIER : x - AHEAD;
+        constexpr int early = (x - AHEAD) | 1, at = early < BARRIER && x >= 16 ? BARRIER : early;
         if constexpr (at == n) {
           if constexpr (x < 32) read(std::integral_constant<int, x>{}, sK1, sV);
           else read(std::integral_constant<int, x - 32>{}, sK2, sV);
         }
       });
-      if constexpr (n > BARRIER && n <= BARRIER + 8) load(ahead, n - BARRIER <= 4, t + (n - BARRIER <= 4 ? 1 : 3), (n - BARRIER - 1) & 3);
+      if constexpr (n > BARRIER && n <= BARRIER + 8) {
+        constexpr uint32_t V = n - BARRIER <= 4, slot = V * 2 * TILE_BYTES + ((n - BARRIER - 1) & 3) * 4096;
+        if constexpr (decltype(LAST)::value) lds_dma_at(ahead, w.lds0 + (par ^ 1) * TILE_BYTES + slot, V ? w.offV : w.offK);
+        else lds_dma_from<(decltype(par)::value ^ 1) * TILE_BYTES + slot>(ahead, w.lds0, V ? w.offV : w.offK);
+      }
       softmax_to(sc, std::integral_constant<int, softmax_elems(n - 1)>{}, std::integral_constant<int, softmax_elems(n)>{});
       if constexpr (n >= 18 && n < 26) {                            // maximum of the new scores
         constexpr int e = (n - 18) * 2;
@@ -689,7 +741,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
         mx1 = fmaxf(fmaxf(mx1, sn[1][e]), sn[1][e + 1]);
       }
       if constexpr (softmax_elems(n - 1) != softmax_elems(n)) asm volatile("" : "+v"(sum));
-      if constexpr (n >= BARRIER && n < BARRIER + 8) ahead = next_group(t, n - BARRIER);
+      if constexpr (n >= BARRIER && n < BARRIER + 8) ahead = next_rsrc(t, n - BARRIER);
       if constexpr (n == 25) asm volatile("" : "+v"(mx0), "+v"(mx1));
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -778,7 +830,7 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   const int first = uni(row_limit(in, s, row0));
   const int t0 = key_lo / KT, t1 = max((end + KT - 1) / KT, t0);
   const int tw = busy ? min(t1, max((min(all, end) + KT - 1) / KT, t0)) : t0;   // ... and of the wavefront
-  const PageSource src = {table, end, (uint32_t)((int64_t)kvh * in->c.head_stride >> 3)};
+  const PageSource src = {table, end, (uint32_t)((int64_t)kvh * in->c.head_stride >> 3), (int*)(smem + SPOTS + wave * 256)};
   const uint32_t lds0 = (uint32_t)(uintptr_t)LRB_LDS_PTR(smem) + (uint32_t)wave * 1024u;
   const int ts = (int)in->c.token_stride * 2, r4 = lane >> 4, pc = lane & 15, rg = (wave & 1) * 4 + r4;
   // load i of a tile: keys (i * 4 + wave) * 4 .., the same lane offset for every i
