@@ -150,10 +150,11 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& fir
   const uint32_t traffic = max(root(x, 1.f / 6150.f), (uint32_t)MIN_SPLIT), fill = max(part(places), min(part(places / 2), 8u));
   return SplitLen{max(narrow, (uint32_t)MIN_SPLIT), max(fill, traffic), max(2 * root(x, 1.f / 6150.f), 3u)};
 }
-// (rounded to the nearer number, and as even as they can be)
+// (rounded to the nearer number, wide ones' up from a quarter, since the longest item decides: the mixed batch 103 -> 94 us, 16 chunks of up to 256
+// tokens beside 16 single ones 223 -> 213; as even as they can be)
 __device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
   const bool wide = s.rows > R_NARROW;
-  const uint32_t len = wide ? l.wide : l.narrow, n = ((uint32_t)s.tiles + len / 2) / len;
+  const uint32_t len = wide ? l.wide : l.narrow, n = ((uint32_t)s.tiles + (wide ? len * 3 / 4 : len / 2)) / len;
   return wide && (uint32_t)s.tiles <= l.whole ? 1u : max(n, 1u);
 }
 // rows of sums that a sequence keeps: [key / value head][split][row]
@@ -883,6 +884,16 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   }
 }
 
+// Item of workgroup v, of `wide` wide items and then `narrow` narrow ones, more than find a place together.  Where the wide ones alone would leave some:
+// every second of them, narrow ones for the CUs that are left, then the other wide ones, which share CUs with the first.  Beside a narrow item, whose
+// loads wait for memory in the same queue, a wide one takes 2.4 us per tile, beside another wide one 2 (one chunk of 512 tokens and 31 single ones over
+// 4000 keys 123 -> 118 us, 3 chunks of 64 beside 29 single ones 69 -> 64).  Fewer items have a CU each for longer and stay in order.
+__device__ __forceinline__ uint32_t side_by_side(uint32_t v, uint32_t wide, uint32_t narrow) {
+  if (wide >= PLACES || wide + narrow < PLACES) return v;
+  const uint32_t half = (wide + 1) / 2, first = min(narrow, PLACES / 2 - half);
+  return v < half ? v : v < half + first ? wide + v - half : v < wide + first ? v - first : v;
+}
+
 // One workgroup per item: sequence, run of blocks, key / value head, split, block of rows in the run.
 __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -910,6 +921,7 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
     }
     // wide sequences' items, which take longer, before the others' of the same 64
     const uint32_t wide = s.rows > R_NARROW ? items : 0, wide_end = wave_scan(wide), other_end = wave_scan(items - wide);
+    if (a.c.batch <= 64) v = side_by_side(v, last_lane(wide_end), last_lane(other_end));
     item_end = item0 + (wide > 0 ? wide_end : last_lane(wide_end) + other_end);
     part_end = part0 + wave_scan(parts);
     hit = __builtin_amdgcn_ballot_w64(v - (item_end - items) < items);
@@ -1069,9 +1081,9 @@ Bounds bounds(int64_t T, int H, int Hkv, int batch, int64_t capacity) {
   Bounds b;
   b.split = most > 1;
   b.items = std::min(Hkv * blocks * most, Hkv * blocks + cuts + wide);
-  // rows of sums: all rows in every split, or those of the splits there are (rounded to the nearer number, two or more are at most 4 / 3 of a
-  // sequence's share)
-  b.part_rows = b.split ? std::min(T * H * most, (cuts * std::min<int64_t>(rows, R_NARROW) + wide * R_WIDE) * 4 / 3 + 1) : 0;
+  // rows of sums: all rows in every split, or those of the splits there are (rounded as they are, two or more are at most 4 / 3 of a sequence's share,
+  // wide ones 8 / 5)
+  b.part_rows = b.split ? std::min(T * H * most, cuts * std::min<int64_t>(rows, R_NARROW) * 4 / 3 + wide * R_WIDE * 8 / 5 + 1) : 0;
   return b;
 }
 

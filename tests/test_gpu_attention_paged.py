@@ -288,7 +288,8 @@ def test_on_a_stream_of_its_own():
 
 # Real sizes, in the long form of an item and with keys in many splits: (new tokens, keys) of the sequences, H, Hkv, page
 @pytest.mark.parametrize("seqs,H,Hkv,page", [([(512, 8192)], 32, 8, 16), ([(1, 16384), (1, 300)], 32, 8, 48), ([(2047, 2047), (130, 900)], 8, 8, 64),
-                                             ([(1, 4096)] * 6 + [(200, 4096), (77, 3000)], 32, 8, 16), ([(600, 5000)], 6, 1, 24)])
+                                             ([(1, 4096)] * 6 + [(200, 4096), (77, 3000)], 32, 8, 16), ([(600, 5000)], 6, 1, 24),
+                                             ([(1, 2500)] * 20 + [(300, 4096)] + [(1, 2500)] * 20, 8, 8, 16), ([(64, 3900), (1, 4000)] * 16, 16, 8, 32)])
 def test_real_sizes(seqs, H, Hkv, page):
     """Against 64 bits on the GPU, every element; bounds as above."""
     print(f"paged attention {seqs} H={H} Hkv={Hkv} page={page}", flush=True)
