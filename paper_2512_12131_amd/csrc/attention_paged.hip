@@ -7,7 +7,7 @@
 //            before the end, where they join their sums.  Bound by memory: every key and value is read once (64 single tokens over 4600 keys on
 //            average, 32 / 8 heads, 1.2 GB: 193 us, 6.2 TB/s).
 //   wide     the four wavefronts take 32 rows each, keys and values pass through LDS in tiles of 64 for all of them.  Bound by the matrix
-//            and vector units (4 x 2048 tokens over 8192 keys: 0.88 - 0.92 ms, 1.05 - 1.09 PFLOP/s, matrix units busy for 56 % of the cycles at
+//            and vector units (4 x 2048 tokens over 8192 keys: 0.88 - 0.91 ms, 1.06 - 1.09 PFLOP/s, matrix units busy for 59 % of the cycles at
 //            the 1.7 GHz that the power limit leaves).
 // Both compute S^T = K Q^T and O^T += V^T P^T on 32 x 32 x 16 MFMAs with the running maximum and sum of a softmax (one lane column per row),
 // as attention.hip does.
@@ -834,7 +834,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
   return bad;
 }
 
-constexpr int LONG = 8;          // tiles from which on the long form is faster (its code and its way in are longer: items of 6 tiles 25 -> 27 us with it)
+constexpr int LONG = 8;          // tiles from which on the long form is faster (its code and its way in are longer: 64 tokens over 600 keys 18.8 -> 20.0 us with it from 4 tiles on, a prompt of 640 22.9 -> 23.8 without it up to 12)
 
 __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, int kvh, int row0, int key_lo, int key_hi, bool whole,
                                           uint32_t part0, unsigned char* smem) {
