@@ -115,7 +115,8 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
 //           sqrt(x / 6150), x the tiles times their rows: len tiles take len * 1.6
 //           us, and x / len rows of sums 0.26 ns each on their way through memory.  A sequence of two of the latter, or of three tiles, is not
 //           split, since the join takes some us by itself.  (us, against the narrow rule for both: a prompt of 777 tokens 31.2 -> 25.9, of
-//           2048 70 -> 56, 512 tokens over 8192 keys 93 -> 83, over 32768 301 -> 268, the mixed batch 101 -> 93.  Four tiles split in two: 10
+//           2048 70 -> 56, 512 tokens over 8192 keys 93 -> 83, over 32768 301 -> 268, 6 chunks of up to 256
+//           tokens beside 18 single ones over up to 4096 keys, the mixed batch below, 101 -> 93.  Four tiles split in two: 10
 //           tokens over 250 keys 12.8 -> 11.7; three: 3 prompts of 108 behind 26 keys 13.1 -> 14.6.)
 struct SplitLen { uint32_t narrow, wide, whole; };      // whole: wide sequences of up to so many tiles are not split
 // Sum over the lanes, in an order of its own: both kernels get the same bits.  (Products and sums are rounded one by one wherever this is inlined.)
