@@ -233,11 +233,11 @@ __device__ __forceinline__ Spots spots(const Pages& pg, const uint16_t* base) {
   const uint64_t at = (uint64_t)(uintptr_t)base + ((uint64_t)pg.place << 4);
   return Spots{(uint32_t)at, (uint32_t)(at >> 32), pg.bytes};
 }
-template <int WAIT>
+template <bool SETTLE>
 __device__ __forceinline__ rsrc_t spot_rsrc(const Spots& s, int g) {
   uint32_t lo = __builtin_amdgcn_readlane(s.lo, g & 63), hi = __builtin_amdgcn_readlane(s.hi, g & 63);
   uint32_t bytes = __builtin_amdgcn_readlane(s.bytes, g & 63);
-  if constexpr (WAIT > 0) asm volatile("s_nop %3" : "+s"(lo), "+s"(hi), "+s"(bytes) : "i"(WAIT - 1));
+  if constexpr (SETTLE) asm volatile("s_nop 4" : "+s"(lo), "+s"(hi), "+s"(bytes));
   return rsrc_t{lo, hi, bytes, 0x00020000u};
 }
 // lds_dma_at a fixed distance from an address
@@ -591,10 +591,8 @@ __device__ __forceinline__ bool wide_short(ArgPtr in, Rows& st, const WideTiles&
 template <int N>
 __device__ __forceinline__ void lds_reads_left() { __builtin_amdgcn_s_waitcnt(0xc07f | N << 8); }
 // An iteration works on two key tiles, as the dense forward's does: the scores of tile t + 1 and the output of tile t, with the softmax of tile t and
-// the maximum of the new scores threaded between their MFMAs.  Two barriers, one where K of tile t + 1 has been read and one where V of tile t has: each
-// frees a slot, and what is loaded into it has one and a half iterations.  (One barrier and one iteration: the mixed batch 81 -> 79 us, 8 chunks of 64
-// tokens beside 24 single ones over up to 8192 keys 120 -> 114, prompts by themselves the same within 1 %.)
-constexpr int K_READ = 12, V_READ = 28;
+// the maximum of the new scores threaded between their MFMAs, one barrier in the middle.
+constexpr int BARRIER = 12;
 constexpr int softmax_elems(int n) { return n < 0 ? 0 : n < 16 ? 5 * (n + 1) / 4 : n < 28 ? 5 + n : 32; }   // done by the end of slot n
 
 __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& w, const Seq& s, const PageSource& src, const bf16x8 (&qf)[8], float c) {
@@ -602,7 +600,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
   const int t0 = w.t0, t1 = w.t1, tw = w.tw, lim0 = w.lim0, wave = w.wave, lane = w.lane;
   Pages pg;
   first_window<8>(in, pg, src, t0, lane);
-  Spots pk = spots(pg, w.cK), pv = spots(pg, w.cV);      // windows of K's loads and of V's, which follow a tile behind
+  Spots pk = spots(pg, w.cK), pv = spots(pg, w.cV);      // windows of K's loads and of V's, which follow two tiles behind
   auto next = [&](int t) {
     next_window<8>(pg, src, t, lane);
     Spots n = pk;
@@ -613,7 +611,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     pk = n;
   };
   auto dma = [&](bool isV, int t, int i) {     // load i of tile t into the slot of its parity; past the keys: zeros
-    lds_dma_at(spot_rsrc<5>(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096,
+    lds_dma_at(spot_rsrc<true>(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)), w.lds0 + (uint32_t)((isV ? 2 : 0) + ((t - t0) & 1)) * TILE_BYTES + i * 4096,
                isV ? w.offV : w.offK);
   };
   if (t0 < t1) {
@@ -624,7 +622,6 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     next(t0 + 1);
 #pragma unroll
     for (int i = 0; i < 4; i++) dma(false, t0 + 1, i);
-    if (((t0 + 1) & 7) == 0) pv = spots(pg, w.cV);
     next(t0 + 2);
   }
   f32x16 sa[2], sb[2];                          // scores of the tile whose softmax comes next, and of the one after it
@@ -664,22 +661,20 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
         for (int e = 0; e < 16; e++) st.o[hb][e] *= alpha;
     }
   };
-  // Loads are asked for in the order of their use, K of t + 2, V of t + 1, K of t + 3, V of t + 2, four each.  The first barrier of tile t: everyone has read
-  // K of t + 1, V of t has landed.  The second: everyone has read V of t, K of t + 2 has landed.  At either only the two tiles asked for last may be
-  // on their way; a wavefront that is through with its own tiles leaves out loads behind the keys and waits for all.
-  auto turn = [&](auto Out) {
+  // everyone has read K of tile t + 1 and V of tile t - 1, and K of t + 2 and V of t have landed
+  auto turn = [&] {
     read_done();
-    landed<decltype(Out)::value>();
+    landed<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  using Two = std::integral_constant<int, 8>;
-  using None = std::integral_constant<int, 0>;
-  auto next_rsrc = [&](auto isV, int t, int i) { return spot_rsrc<isV ? 2 : 0>(isV ? pv : pk, t * 8 + i * 2 + (wave >> 1)); };   // (little else in V's slots)
+  // loads 0 .. 7 of tile t's iteration, into the slots just left: V of t + 1, K of t + 3
+  auto next_load = [&](int t, int i) { dma(i < 4, t + (i < 4 ? 1 : 3), i & 3); };
+  auto next_rsrc = [&](int t, int i) { return spot_rsrc<false>(i < 4 ? pv : pk, (t + (i < 4 ? 1 : 3)) * 8 + (i & 3) * 2 + (wave >> 1)); };
   auto windows = [&](int t) {                   // of the loads of tile t's iteration
     next(t + 3);
     Spots n = pv;
-    if (((t + 2) & 7) == 0) {
+    if (((t + 1) & 7) == 0) {
       asm volatile("");
       n = spots(pg, w.cV);
     }
@@ -717,28 +712,29 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
     rsrc_t ahead = {};
     unroll_for<32>([&](auto Nc) {
       constexpr int n = decltype(Nc)::value;
-      if constexpr (n % 2 == 0 && n != K_READ && n != V_READ) {      // the last two operands may be on their way
+      if constexpr (n % 2 == 0 && n != BARRIER) {      // the last two operands may be on their way
         lds_reads_left<(n < 14 || n >= 30 ? 2 : 4)>();
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (n < 16) sn[n & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[n % AHEAD], qf[n >> 1], sn[n & 1], 0, 0, 0);
       else out(Nc);
-      if constexpr (n == K_READ || n == V_READ) turn(Two{});
-      if constexpr (n == K_READ && decltype(LAST)::value) bad |= careful(w, t);
-      // operands, two at a time (half of the waits for them): V only from behind the first barrier, K of the tile after next from behind the second
+      if constexpr (n == BARRIER) {
+        turn();
+        if constexpr (decltype(LAST)::value) bad |= careful(w, t);
+      }
+      // operands, two at a time (half of the waits for them): V only from behind the barrier, then K of the tile after next
       unroll_for<32>([&](auto I) {
         constexpr int x = decltype(I)::value + AHEAD;               // slot that reads
-        constexpr int early = (x - AHEAD) | 1, at = early < K_READ && x >= 16 ? K_READ : early;
+        constexpr int early = (x - AHEAD) | 1, at = early < BARRIER && x >= 16 ? BARRIER : early;
         if constexpr (at == n) {
           if constexpr (x < 32) read(std::integral_constant<int, x>{}, sK1, sV);
           else read(std::integral_constant<int, x - 32>{}, sK2, sV);
         }
       });
-      if constexpr ((n > K_READ && n <= K_READ + 4) || n >= V_READ) {
-        constexpr bool V = n >= V_READ;                             // V of t + 2 into the slot of V of t, K of t + 3 into that of t + 1
-        constexpr uint32_t slot = V ? 2 * TILE_BYTES + (n - V_READ) * 4096 : (n - K_READ - 1) * 4096;
-        if constexpr (decltype(LAST)::value) lds_dma_at(ahead, w.lds0 + (V ? par : par ^ 1) * TILE_BYTES + slot, V ? w.offV : w.offK);
-        else lds_dma_from<(V ? decltype(par)::value : decltype(par)::value ^ 1) * TILE_BYTES + slot>(ahead, w.lds0, V ? w.offV : w.offK);
+      if constexpr (n > BARRIER && n <= BARRIER + 8) {
+        constexpr uint32_t V = n - BARRIER <= 4, slot = V * 2 * TILE_BYTES + ((n - BARRIER - 1) & 3) * 4096;
+        if constexpr (decltype(LAST)::value) lds_dma_at(ahead, w.lds0 + (par ^ 1) * TILE_BYTES + slot, V ? w.offV : w.offK);
+        else lds_dma_from<(decltype(par)::value ^ 1) * TILE_BYTES + slot>(ahead, w.lds0, V ? w.offV : w.offK);
       }
       softmax_to(sc, std::integral_constant<int, softmax_elems(n - 1)>{}, std::integral_constant<int, softmax_elems(n)>{});
       if constexpr (n >= 18 && n < 26) {                            // maximum of the new scores
@@ -747,8 +743,7 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
         mx1 = fmaxf(fmaxf(mx1, sn[1][e]), sn[1][e + 1]);
       }
       if constexpr (softmax_elems(n - 1) != softmax_elems(n)) asm volatile("" : "+v"(sum));
-      if constexpr (n >= K_READ && n < K_READ + 4) ahead = next_rsrc(std::false_type{}, t + 3, n - K_READ);
-      if constexpr (n >= V_READ - 1 && n < V_READ + 3) ahead = next_rsrc(std::true_type{}, t + 2, n - V_READ + 1);
+      if constexpr (n >= BARRIER && n < BARRIER + 8) ahead = next_rsrc(t, n - BARRIER);
       if constexpr (n == 25) asm volatile("" : "+v"(mx0), "+v"(mx1));
       __builtin_amdgcn_sched_barrier(0);
     });
@@ -776,8 +771,6 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
   if (t0 < t1) {
 #pragma unroll
     for (int i = 0; i < 4; i++) dma(false, t0 + 2, i);
-#pragma unroll
-    for (int i = 0; i < 4; i++) dma(true, t0 + 1, i);
   }
   const int plain = min(w.first / KT, tw);        // tiles without a hidden key
   int t = t0;
@@ -790,30 +783,18 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
 #pragma unroll
     for (int nb = 0; nb < 2; nb++) sa[nb] = sb[nb];
   }
-  // loads behind the first and the second barrier of tile t, of a wavefront without a tile after it
-  auto load_k = [&](int t) {
-    if (t + 3 < t1) {
-#pragma unroll
-      for (int i = 0; i < 4; i++) dma(false, t + 3, i);
-    }
-  };
-  auto load_v = [&](int t) {
-    if (t + 1 == t1) return;
-    turn(None{});
-    if (t + 2 < t1) {
-#pragma unroll
-      for (int i = 0; i < 4; i++) dma(true, t + 2, i);
-    }
-  };
   if (t < tw) {                                 // this wavefront's last tile
     const unsigned char* sV = smem + (2 + ((t - t0) & 1)) * TILE_BYTES;
     windows(t);
     rescale();
     sum = 0.f;
-    turn(None{});
+    turn();
     bad |= careful(w, t);
     unroll_for<AHEAD>([&](auto I) { read(std::integral_constant<int, 16 + decltype(I)::value>{}, smem, sV); });
-    load_k(t);
+    if (t + 1 < t1) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) next_load(t, i);
+    }
     softmax_to(sa, std::integral_constant<int, 0>{}, std::integral_constant<int, 16>{});
     unroll_for<16>([&](auto I) {
       constexpr int n = 16 + decltype(I)::value;
@@ -822,15 +803,16 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
       if constexpr (n < 24) softmax_to(sa, std::integral_constant<int, 16 + (n - 16) * 2>{}, std::integral_constant<int, 18 + (n - 16) * 2>{});
     });
     st.l = st.l * alpha + sum;
-    load_v(t);
     t++;
   }
   for (; t < t1; t++) {                         // nothing left for this wavefront but its share of the loads
     windows(t);
-    turn(None{});
+    turn();
     bad |= careful(w, t);
-    load_k(t);
-    load_v(t);
+    if (t + 1 < t1) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) next_load(t, i);
+    }
   }
   return bad;
 }
