@@ -7,7 +7,7 @@
 //            before the end, where they join their sums.  Bound by memory: every key and value is read once (64 single tokens over 4600 keys on
 //            average, 32 / 8 heads, 1.2 GB: 193 us, 6.2 TB/s).
 //   wide     the four wavefronts take 32 rows each, keys and values pass through LDS in tiles of 64 for all of them.  Bound by the matrix
-//            and vector units (4 x 2048 tokens over 8192 keys: 0.88 - 0.91 ms, 1.06 - 1.09 PFLOP/s, matrix units busy for 59 % of the cycles at
+//            and vector units (4 x 2048 tokens over 8192 keys: 0.88 - 0.91 ms, 1.06 - 1.09 PFLOP/s, matrix units busy for 60 % of the cycles at
 //            the 1.7 GHz that the power limit leaves).
 // Both compute S^T = K Q^T and O^T += V^T P^T on 32 x 32 x 16 MFMAs with the running maximum and sum of a softmax (one lane column per row),
 // as attention.hip does.
@@ -151,8 +151,8 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& fir
   const uint32_t traffic = max(root(x, 1.f / 6150.f), (uint32_t)MIN_SPLIT), fill = max(part(places), min(part(places / 2), 8u));
   return SplitLen{max(narrow, (uint32_t)MIN_SPLIT), max(fill, traffic), max(2 * root(x, 1.f / 6150.f), 3u)};
 }
-// (rounded to the nearer number, wide ones' up from a quarter, since the longest item decides: the mixed batch 103 -> 94 us, 16 chunks of up to 256
-// tokens beside 16 single ones 223 -> 213; as even as they can be)
+// (rounded to the nearer number, wide ones' up from a quarter, since the longest item decides: 16 chunks of up to 256 tokens beside 16 single ones
+// 222 -> 210 us, the mixed batch 97 -> 92; as even as they can be)
 __device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
   const bool wide = s.rows > R_NARROW;
   const uint32_t len = wide ? l.wide : l.narrow, n = ((uint32_t)s.tiles + (wide ? len * 3 / 4 : len / 2)) / len;
@@ -592,6 +592,7 @@ template <int N>
 __device__ __forceinline__ void lds_reads_left() { __builtin_amdgcn_s_waitcnt(0xc07f | N << 8); }
 // An iteration works on two key tiles, as the dense forward's does: the scores of tile t + 1 and the output of tile t, with the softmax of tile t and
 // the maximum of the new scores threaded between their MFMAs, one barrier in the middle.
+// (A barrier of its own for V's slot, which gives the loads half an iteration more, was 1 - 2 % slower.)
 constexpr int BARRIER = 12;
 constexpr int softmax_elems(int n) { return n < 0 ? 0 : n < 16 ? 5 * (n + 1) / 4 : n < 28 ? 5 + n : 32; }   // done by the end of slot n
 
@@ -867,12 +868,13 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   }
 }
 
-// Item of workgroup v, of `wide` wide items and then `narrow` narrow ones, more than find a place together.  Where the wide ones alone would leave some:
-// every second of them, narrow ones for the CUs that are left, then the other wide ones, which share CUs with the first.  Beside a narrow item, whose
+// Item of workgroup v, of `wide` wide items, a CU for each or fewer, and then `narrow` narrow ones, with them more than find a place together: every second
+// of the wide ones, narrow ones for the CUs that are left, then the other wide ones, which share CUs with the first.  Beside a narrow item, whose
 // loads wait for memory in the same queue, a wide one takes 2.4 us per tile, beside another wide one 2 (one chunk of 512 tokens and 31 single ones over
-// 4000 keys 123 -> 118 us, 3 chunks of 64 beside 29 single ones 69 -> 64).  Fewer items have a CU each for longer and stay in order.
+// 4000 keys 122 -> 118 us, 3 chunks of 64 beside 29 single ones 66 -> 65).  More wide items share CUs anyway and stay in order, the longest first
+// (the mixed batch 91, else 94 us), as fewer of both kinds do, which have a CU each.
 __device__ __forceinline__ uint32_t side_by_side(uint32_t v, uint32_t wide, uint32_t narrow) {
-  if (wide >= PLACES || wide + narrow < PLACES) return v;
+  if (wide > PLACES / 2 || wide + narrow < PLACES) return v;
   const uint32_t half = (wide + 1) / 2, first = min(narrow, PLACES / 2 - half);
   return v < half ? v : v < half + first ? wide + v - half : v < wide + first ? v - first : v;
 }
