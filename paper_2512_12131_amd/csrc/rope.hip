@@ -206,8 +206,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
         before += __popcll(__ballot(in && a.c.cu_q[in ? i + lane + 1 : 0] <= t));
       }
       if (before < a.c.batch && a.c.cu_q[before] <= t) {
-        const int64_t end = a.c.cu_q[before + 1] < a.T ? a.c.cu_q[before + 1] : a.T;
-        const int64_t p = (int64_t)a.c.kv_len[before] - (end - t);
+        // (counted from the sequence's last token, whether or not the call has that)
+        const int64_t p = (int64_t)a.c.kv_len[before] - ((int64_t)a.c.cu_q[before + 1] - t);
         if (p >= 0 && p < a.c.capacity && (a.rot == 0 || p < a.table_rows)) {
           const int col = (int)a.c.by_page.div((uint32_t)p);
           const int page = a.c.page_table[before * a.c.table_ld + col];
