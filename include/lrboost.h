@@ -333,7 +333,7 @@ int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t
  * cu_q[b] <= t < cu_q[b + 1]; kv_len[b] counts b's keys including the new ones, so that its new tokens stand at positions
  * kv_len[b] - (cu_q[b + 1] - cu_q[b]) and up.  The lists are DEVICE int32 and not read on the host: a captured call takes what they
  * hold when it is replayed.  Tokens before cu_q[0] or from cu_q[batch] on belong to nobody (a padded batch): nothing is written for
- * them.  Whatever the lists hold, nothing outside the cache and the other arguments is read or written: a page number
+ * them.  The lists may count more tokens than the call has: those it has keep their positions.  Whatever the lists hold, nothing outside the cache and the other arguments is read or written: a page number
  * outside [0, n_pages) is no page, keys past max_pages * page_size do not exist.
  * page_size, head_dim and the strides (elements) are multiples of 8, k and v 16-byte aligned (LR_EALIGN); pages of both layouts
  * [page_size, n_kv_heads, head_dim] and [n_kv_heads, page_size, head_dim] are a matter of the strides.  Limits (LR_EUNSUPPORTED):

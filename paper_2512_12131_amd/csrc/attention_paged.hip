@@ -91,14 +91,14 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
 __device__ __forceinline__ uint32_t last_lane(uint32_t x) { return __builtin_amdgcn_readlane(x, 63); }
 
 struct Seq {              // of one sequence
-  int tok0, n, kv;        // first token, new tokens, kv_len
+  int tok0, n, kv;        // first token, new tokens and keys with them: of the tokens that the call has
   int keys, tiles;        // keys that its last token sees, in 64-key tiles (at least one)
   int rows, blocks;       // rows per key / value head and items of them
 };
 __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
   Seq s;
   const int c0 = a.c.cu_q[b], c1 = a.c.cu_q[b + 1];
-  s.kv = a.c.kv_len[b];
+  s.kv = max(a.c.kv_len[b], 0) - max(max(c1, 0) - a.T, 0);      // (without those that are not there)
   s.tok0 = min(max(c0, 0), a.T);
   s.n = max(min(max(c1, 0), a.T) - s.tok0, 0);
   s.keys = (int)min((int64_t)max(s.kv, 0), a.c.capacity);

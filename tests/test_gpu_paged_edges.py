@@ -1,0 +1,60 @@
+"""The paged cache at the edges of its lists: calls of fewer tokens than the lists count, batches of no or of very many sequences, values
+that are no numbers in single columns, long runs of pages.  Bounds as in test_gpu_attention_paged.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as po
+from paper_2512_12131_amd import binding as B
+from test_gpu_attention_paged import HD, _dense, call, compare
+from test_gpu_kv_append import BF, DEV, lists, make, np64
+
+pytestmark = pytest.mark.gpu
+
+
+def against_64_bits(q, o, lse, c, seqs, H):
+    """Every element of o and lse against 64 bits on the GPU, all heads of a sequence at once."""
+    Hkv = c["k_cache"].shape[2]
+    t0, grp = int(c["cu_q"][0]), H // Hkv
+    for b, (n, kv) in enumerate(seqs):
+        k, v = (x.double().view(kv, Hkv, HD).permute(1, 2, 0).contiguous() for x in _dense(c, b, kv))      # [Hkv, hd, keys]
+        qq = q[t0:t0 + n, :H * HD].double().view(n, Hkv, grp, HD).permute(1, 0, 2, 3).reshape(Hkv, n * grp, HD)
+        hidden = (torch.arange(kv, device=DEV)[None] > torch.arange(kv - n, kv, device=DEV)[:, None]).repeat_interleave(grp, 0)[None]
+        s = torch.bmm(qq, k) * HD ** -0.5
+        d = 128 * 2.0 ** -24 * (torch.bmm(qq.abs(), k.abs()) * HD ** -0.5).masked_fill(hidden, 0).amax(-1)
+        s = s.masked_fill(hidden, float("-inf"))
+        l = torch.logsumexp(s, -1)
+        w, v = torch.exp(s - l[..., None]), v.transpose(1, 2).contiguous()
+        rows = lambda x: x.view(Hkv, n, grp, -1).permute(1, 0, 2, 3).reshape(n, H, -1)
+        ref, mag, d, l = rows(torch.bmm(w, v)), rows(torch.bmm(w, v.abs())), rows(d)[..., 0], rows(l)[..., 0]
+        err = (o[t0:t0 + n, :H * HD].double().view(n, H, HD) - ref).abs()
+        assert bool((err <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * d + 2.0 ** -18)[..., None] * mag).all()), b
+        lerr = (lse[t0:t0 + n].double() - l).abs()
+        assert bool((lerr <= d + 2.0 ** -20 * (1 + l.abs()) + kv * 2.0 ** -24).all()), (b, float(lerr.max()))
+        t0 += n
+
+
+# ---- lists that count more tokens than the call has ----------------------------------------------------------
+@pytest.mark.parametrize("seqs,H,Hkv,T", [([(5, 30)], 1, 1, 3), ([(4, 4)], 8, 2, 1), ([(1, 40), (60, 200)], 4, 2, 45), ([(1, 300), (8, 900)], 8, 1, 4),
+                                          ([(200, 1200), (1, 9)], 4, 2, 130), ([(150, 150), (3, 50)], 2, 2, 150)])
+def test_attention_of_the_first_tokens_of_a_batch(seqs, H, Hkv, T):
+    """A token's position is counted from its sequence's last one, whether or not the call has that."""
+    print(f"first {T} tokens of {seqs}", flush=True)
+    c, every = make(seqs, Hkv, HD, 16, seed=20)
+    _, _, table = lists(c)
+    cu = np.cumsum([0] + [n for n, _ in seqs])
+    for b, (n, kv) in enumerate(seqs):                # what the tokens that are not there would have been the first to see
+        for j in range(kv - min(n, max(0, int(cu[b + 1]) - T)), kv):
+            c["k_cache"][table[b, j // 16], j % 16], c["v_cache"][table[b, j // 16], j % 16] = float("nan"), float("inf")
+    q, o, lse = call(c, every, H)
+    short, short_lse = torch.full_like(o[:T], 7.0), torch.full_like(lse[:T], 7.0)
+    B.lr_attention_paged_fwd(q[:T], H=H, o=short, lse=short_lse, **c)
+    torch.cuda.synchronize()
+    assert bool(short.isfinite().all()) and bool(short_lse.isfinite().all())
+    # the rows that the call has not are what the oracle computes, which knows of no call
+    ref, lse_ref, *_ = po.attention_paged(np64(q).reshape(every, H, HD), *(np.nan_to_num(np64(c[n]), nan=0, posinf=0) for n in ("k_cache", "v_cache")),
+                                          table, cu, [kv for _, kv in seqs], H, HD ** -0.5)
+    rest, rest_lse = torch.from_numpy(ref[T:]).to(DEV, BF).view(every - T, -1), torch.from_numpy(lse_ref[T:]).to(DEV, torch.float32)
+    compare(torch.cat([short, rest]), torch.cat([short_lse, rest_lse]), q, c, H)
