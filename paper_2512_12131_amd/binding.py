@@ -515,7 +515,7 @@ def lr_attention_paged_workspace_bytes(k_cache, page_table, T, H):
     pages, page_size, Hkv, hd = k_cache.shape
     batch, cols = page_table.shape
     c = KvCache(None, None, pages, page_size, Hkv, hd, k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), None, batch, cols,
-                page_table.stride(0), None, None)
+                page_table.stride(0) if batch > 1 else cols, None, None)
     return lib().lr_attention_paged_workspace_bytes(C.byref(c), T, H)
 
 
