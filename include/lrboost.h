@@ -337,7 +337,7 @@ int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t
  * outside [0, n_pages) is no page, keys past max_pages * page_size do not exist.
  * page_size, head_dim and the strides (elements) are multiples of 8, k and v 16-byte aligned (LR_EALIGN); pages of both layouts
  * [page_size, n_kv_heads, head_dim] and [n_kv_heads, page_size, head_dim] are a matter of the strides.  Limits (LR_EUNSUPPORTED):
- * 2^35 elements from the first to the last of k, 2^31 - 1 keys of a sequence, 2^16 sequences and 2^25 tokens of a call, token_stride < 2^26.  */
+ * 2^35 elements from the first to the last of k, 2^31 - 2048 keys of a sequence, 2^16 sequences and 2^25 tokens of a call, token_stride < 2^26.  */
 typedef struct {
   void *k, *v;
   int64_t n_pages, page_size, n_kv_heads, head_dim;

@@ -1474,11 +1474,12 @@ int lr_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, const int32_t
 
 static int check_cache(const lr_kv_cache* c, bool pointers, KvCache* out) {
   if (!c) return LR_EINVAL;
-  const int64_t most = 0x7fffffffLL, far = (int64_t)1 << 35;
+  // keys of a sequence: what tiles and looked up windows reach past the last one is below 2^31 too
+  const int64_t most = 0x7fffffffLL, far = (int64_t)1 << 35, keys = ((int64_t)1 << 31) - 2048;
   if (c->n_pages <= 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0 || c->batch < 0 || c->max_pages <= 0 ||
       c->table_ld < c->max_pages || c->page_stride <= 0 || c->token_stride <= 0 || c->head_stride <= 0)
     return LR_EINVAL;
-  if (c->n_pages > most || c->page_size > most || c->max_pages > most / c->page_size || c->batch > (1 << 16) || c->n_kv_heads > (1 << 16) ||
+  if (c->n_pages > most || c->page_size > most || c->max_pages > keys / c->page_size || c->batch > (1 << 16) || c->n_kv_heads > (1 << 16) ||
       c->head_dim > (1 << 16) || c->token_stride >= (1 << 26) || c->page_stride > far || c->head_stride > far ||
       (c->n_pages > 1 && c->page_stride > far / (c->n_pages - 1)) || c->table_ld > far / (c->batch > 0 ? c->batch : 1))
     return LR_EUNSUPPORTED;
