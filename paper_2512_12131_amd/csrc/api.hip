@@ -1488,7 +1488,8 @@ static int check_cache(const lr_kv_cache* c, bool pointers, KvCache* out) {
   TRY(check_dims_bf16(LR_BF16, {c->page_size, c->head_dim, c->page_stride, c->token_stride, c->head_stride}));
   if (pointers) {
     TRY(check_ptrs(LR_BF16, {c->k, c->v}));
-    TRY(check_ptrs(LR_F32, {c->page_table, c->cu_q, c->kv_len}));
+    TRY(check_ptrs(LR_F32, {c->cu_q}));
+    if (c->batch > 0) TRY(check_ptrs(LR_F32, {c->page_table, c->kv_len}));      // (empty tensors may have null pointers)
   }
   *out = KvCache{(uint16_t*)c->k, (uint16_t*)c->v, c->page_stride, c->token_stride, c->head_stride, c->table_ld, c->max_pages * c->page_size,
                  c->page_table, c->cu_q, c->kv_len, (int)c->n_pages, (int)c->page_size, (int)c->n_kv_heads, (int)c->head_dim, (int)c->batch,

@@ -58,3 +58,16 @@ def test_attention_of_the_first_tokens_of_a_batch(seqs, H, Hkv, T):
                                           table, cu, [kv for _, kv in seqs], H, HD ** -0.5)
     rest, rest_lse = torch.from_numpy(ref[T:]).to(DEV, BF).view(every - T, -1), torch.from_numpy(lse_ref[T:]).to(DEV, torch.float32)
     compare(torch.cat([short, rest]), torch.cat([short_lse, rest_lse]), q, c, H)
+
+
+def test_a_batch_of_no_sequences():
+    """Every token belongs to nobody: nothing is written."""
+    cache = torch.randn((4, 16, 2, HD), device=DEV).to(BF)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device=DEV)
+    none = {"k_cache": cache.clone(), "v_cache": cache.clone(), "page_table": i32(0, 4), "cu_q": i32(1), "kv_len": i32(0)}
+    x = torch.randn((3, 4 * HD), device=DEV).to(BF)
+    out = torch.full_like(x, 7.0)
+    B.lr_kv_append(x, x, q=x, H=4, q_out=out, **none)
+    q, o, lse = call(none, 3, 4)
+    assert bool((out == 7).all()) and bool((o == 7).all()) and bool((lse == 7).all())
+    assert torch.equal(none["k_cache"], cache) and torch.equal(none["v_cache"], cache)

@@ -2,7 +2,7 @@
 import torch
 
 from paper_2512_12131_amd import binding as B
-from test_paged_cpu import EUNSUPPORTED, _append, _cache, _paged
+from test_paged_cpu import EINVAL, EUNSUPPORTED, _append, _cache, _paged
 
 
 def test_a_workspace_query_takes_every_table_that_the_call_takes():
@@ -22,3 +22,11 @@ def test_keys_of_a_sequence():
     assert query(most) > 0 and _paged(cache(most), T=0) == 0 and _append(cache(most), T=0) == 0
     for keys in (most + 8, (1 << 31) - 64, (1 << 31) - 8):
         assert query(keys) == 0 and _paged(cache(keys), T=0) == EUNSUPPORTED and _append(cache(keys), T=0) == EUNSUPPORTED, keys
+
+
+def test_a_batch_of_no_sequences_needs_no_lists():
+    """Empty tensors have null pointers; the one boundary of cu_q is there."""
+    none = lambda **over: _cache(batch=0, page_table=None, kv_len=None, **over)
+    assert _append(none()) == 0 and _paged(none()) == 0
+    assert _append(none(k=None)) == EINVAL and _paged(none(cu_q=None)) == EINVAL
+    assert _append(_cache(page_table=None)) == EINVAL and _paged(_cache(kv_len=None)) == EINVAL
