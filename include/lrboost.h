@@ -312,7 +312,8 @@ int lr_attention_gqa_bwd(const void* q, const void* k, const void* v, const void
  * w_i = base^(-2 i / rot) scaled for contexts longer than the one trained on: context = 0 divides all of them by `factor`
  * (1: none); context > 0 goes by t_i = context * w_i / (2 pi), the turns over the trained context: a frequency of t_i <= low is divided
  * by factor, one of t_i >= high is kept, linearly in between.  Angles are formed in 64 bits, each entry is rounded once.
- * rot even, at most 8192 (else LR_EUNSUPPORTED); first >= 0, first + n <= 2^31; base > 0, factor > 0, mscale finite, low < high.
+ * rot even, at most 8192 (else LR_EUNSUPPORTED); first >= 0, first + n <= 2^31; base > 0, factor > 0, mscale finite, low < high.  A base or
+ * factor below 1 makes angles larger than the positions: above 2^31, LR_EUNSUPPORTED.
  * The tables serve lr_rope_at and lr_kv_append, and with rot = 128 lr_rope and the block (rope_cos, rope_sin).                 */
 int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_t first, double base, double factor,
                   double context, double low, double high, double mscale, void* stream);

@@ -1433,6 +1433,18 @@ int lr_rope(void* x, int64_t ldx, const float* cos_tab, const float* sin_tab, in
 }
 
 // ---- rotary tables, rotation at positions, paged cache ---------------------------------------------
+// The largest of a table's frequencies, as the kernel forms them: 1, where neither base nor factor is below it.
+static double largest_frequency(int64_t half, double base, double factor, double context, double low, double high) {
+  if (base >= 1.0 && factor >= 1.0) return 1.0;
+  double most = 0.0;
+  for (int64_t i = 0; i < half; i++) {
+    const double w = std::pow(base, -(double)i / (double)half), turns = context / 6.283185307179586477 * w;
+    const double keep = context > 0.0 ? std::fmin(1.0, std::fmax(0.0, (turns - low) / (high - low))) : 0.0;
+    most = std::fmax(most, w * (keep + (1.0 - keep) / factor));
+  }
+  return most;
+}
+
 int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_t first, double base, double factor, double context,
                   double low, double high, double mscale, void* stream) {
   if (n < 0 || rot <= 0 || rot % 2 || first < 0 || n > ((int64_t)1 << 31) || first > ((int64_t)1 << 31) - n) return LR_EINVAL;
@@ -1442,6 +1454,8 @@ int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_
   if (context > 0 && (!(low < high) || !std::isfinite(low) || !std::isfinite(high))) return LR_EINVAL;
   if (rot > 8192) return LR_EUNSUPPORTED;
   if (n == 0) return LR_OK;
+  // (up to 2^31 an angle's rounding to 64 bits is 2^-22 at most, and its reduction exact)
+  if (!((double)(first + n - 1) * largest_frequency(rot / 2, base, factor, context, low, high) <= 2147483648.0)) return LR_EUNSUPPORTED;
   TRY(check_ptrs(LR_F32, {cos_tab, sin_tab}));
   return k_rope_table(cos_tab, sin_tab, n, (int)(rot / 2), first, base, factor, context, low, high, mscale, (hipStream_t)stream) == hipSuccess
              ? LR_OK : LR_ELAUNCH;

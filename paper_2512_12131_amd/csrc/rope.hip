@@ -12,7 +12,7 @@ namespace {
 // cos / sin [n, rot / 2] of (first + p) w_i.  The frequencies w_i = base^(-2i / rot), scaled for long contexts frequency by
 // frequency: one that turns at least `high` times over the `context` trained on is kept, one that turns at most `low` times is divided
 // by `factor`, linearly in between.
-// Angles of far positions (2^31 at most) need all of 64 bits; there the reduction to [-pi/4, pi/4] is exact to 1e-16 with pi / 2 in two parts,
+// Angles of far positions (2^31 at most, the caller refuses others) need all of 64 bits; there the reduction to [-pi/4, pi/4] is exact to 1e-16 with pi / 2 in two parts,
 // and Taylor's polynomials of degree 13 and 14 are to 2e-14: vector units multiply and add 64 bits as fast as 32.
 __device__ __forceinline__ void sincos_f64(double a, double* sn, double* cs) {
   const double k = rint(a * 0.63661977236758134308);

@@ -30,3 +30,18 @@ def test_a_batch_of_no_sequences_needs_no_lists():
     assert _append(none()) == 0 and _paged(none()) == 0
     assert _append(none(k=None)) == EINVAL and _paged(none(cu_q=None)) == EINVAL
     assert _append(_cache(page_table=None)) == EINVAL and _paged(_cache(kv_len=None)) == EINVAL
+
+
+def test_angles_of_the_tables():
+    """Up to 2^31, whatever the base and the scaling make of the positions.  Accepted calls get as far as the missing output."""
+    def f(*, n=4, rot=8, first=0, base=1e4, factor=1.0, context=0.0, low=1.0, high=32.0):
+        return B.lib().lr_rope_table(None, None, n, rot, first, base, factor, context, low, high, 1.0, None)
+    far = 1 << 31
+    # frequencies 1, 1000^(1/4) .. 1000^(3/4) = 177.8; 1e4^(-3/4) = 0.001 of which is divided by the factor
+    for args in ({}, dict(first=far - 4), dict(first=far - 4, factor=32.0), dict(base=1e-3, first=int(far / 1000 ** 0.75) - 1000), dict(factor=0.5, first=far // 2 - 3),
+                 dict(factor=1e-6, context=4096.0, n=1000), dict(factor=1e-9, n=1), dict(rot=8192, base=0.5, first=far // 2 - 4), dict(base=1e300)):
+        assert f(**args) == EINVAL, args
+    for args in (dict(base=1e-3, first=int(far / 1000 ** 0.75) + 1000), dict(factor=0.5, first=far // 2), dict(factor=1e-6, context=4096.0, first=far // 100),
+                 dict(factor=1e-9), dict(factor=1e-300), dict(rot=8192, base=0.5, first=far // 2 + far // 1000), dict(base=1e-300)):
+        assert f(**args) == EUNSUPPORTED, args
+    assert f(n=0, factor=1e-300) == 0
