@@ -1556,7 +1556,7 @@ int lr_attention_paged_fwd(const lr_kv_cache* cache, const void* q, int64_t ldq,
   TRY(check_dt(dt));
   TRY(check_paged(cache, true, T, H, &c));
   if (dt != LR_BF16 || causal != 1) return LR_EUNSUPPORTED;
-  if (ldq < H * 128 || ldo < H * 128 || !(scale > 0) || !std::isfinite(scale)) return LR_EINVAL;
+  if (ldq < H * 128 || ldo < H * 128 || !(scale > 0) || !std::isfinite(scale * 1.44269504f)) return LR_EINVAL;      // (the exponent's factor)
   TRY(check_dims_bf16(dt, {ldq, ldo}));
   if (T == 0 || c.batch == 0) return LR_OK;
   TRY(check_ptrs(dt, {q, o}));

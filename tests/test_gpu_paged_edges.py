@@ -71,3 +71,37 @@ def test_a_batch_of_no_sequences():
     q, o, lse = call(none, 3, 4)
     assert bool((out == 7).all()) and bool((o == 7).all()) and bool((lse == 7).all())
     assert torch.equal(none["k_cache"], cache) and torch.equal(none["v_cache"], cache)
+
+
+# ---- large logits ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("seqs", [[(1, 777), (5, 70)], [(200, 700)], [(300, 3000)]])
+def test_logits_up_to_the_stated_size(seqs):
+    """Keys score 0, 1, .. 6 times 2^22, over and over (at most 2^24.6): a row is the mean of the values of its
+    largest.  Probabilities of that mean are alike, so o is off by its own rounding and that of 32-bit sums; lse by half a step of the
+    exponent's 32 bits (2^-24 of 2^25.2)."""
+    H, Hkv, page = 4, 2, 16
+    c, T = make(seqs, Hkv, HD, page, seed=26)
+    _, _, table = lists(c)
+    c["k_cache"].zero_()
+    for b, (_, kv) in enumerate(seqs):
+        for j in range(kv):
+            c["k_cache"][table[b, j // page], j % page, :, 0] = j % 7
+    q = torch.zeros((T, H, HD), dtype=BF, device=DEV)
+    q[..., 0] = 1.0
+    o, lse = B.lr_attention_paged_fwd(q.view(T, -1), H=H, scale=2.0 ** 22, **c)
+    torch.cuda.synchronize()
+    t0 = 0
+    for b, (n, kv) in enumerate(seqs):
+        v = _dense(c, b, kv)[1].double().view(kv, Hkv, HD)
+        score = torch.arange(kv, device=DEV) % 7
+        seen = torch.arange(kv, device=DEV)[None] <= torch.arange(kv - n, kv, device=DEV)[:, None]
+        best = torch.where(seen, score, -1).amax(1)
+        w = (seen & (score[None] == best[:, None])).double()
+        for h in range(H):
+            ref = w @ v[:, h // 2].contiguous() / w.sum(1, keepdim=True)
+            mag = w @ v[:, h // 2].abs().contiguous() / w.sum(1, keepdim=True)
+            err = (o[t0:t0 + n, h * HD:(h + 1) * HD].double() - ref).abs()
+            assert bool((err <= 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2.0 ** -18) * mag).all()), (b, h)
+            l = best.double() * 2.0 ** 22 + torch.log(w.sum(1))
+            assert bool(((lse[t0:t0 + n, h].double() - l).abs() <= 2.0 ** -22 * (1 + l.abs())).all()), (b, h)
+        t0 += n

@@ -45,3 +45,11 @@ def test_angles_of_the_tables():
                  dict(factor=1e-9), dict(factor=1e-300), dict(rot=8192, base=0.5, first=far // 2 + far // 1000), dict(base=1e-300)):
         assert f(**args) == EUNSUPPORTED, args
     assert f(n=0, factor=1e-300) == 0
+
+
+def test_scales_of_the_attention():
+    """The exponent's factor, scale * log2(e), is finite in 32 bits."""
+    for scale in (2.4e38, 3.4e38):
+        assert _paged(scale=scale, T=0) == EINVAL, scale
+    for scale in (2.3e38, 1.0, 1e-37):
+        assert _paged(scale=scale, T=0) == 0, scale
