@@ -105,3 +105,77 @@ def test_logits_up_to_the_stated_size(seqs):
             l = best.double() * 2.0 ** 22 + torch.log(w.sum(1))
             assert bool(((lse[t0:t0 + n, h].double() - l).abs() <= 2.0 ** -22 * (1 + l.abs())).all()), (b, h)
         t0 += n
+
+
+# ---- values that are no numbers --------------------------------------------------------------------------------
+# (new tokens, keys), H, Hkv, the key whose value it is: one item of few rows, few tiles, many tiles, keys in several splits, both joined
+VALUES = [([(5, 41)], 4, 1, 39), ([(8, 700), (1, 90)], 4, 1, 696), ([(150, 150)], 4, 2, 70), ([(150, 470)], 1, 1, 400), ([(200, 1100)], 1, 1, 1003),
+          ([(40, 360), (1, 200)], 2, 2, 330), ([(64, 3900), (1, 400)], 16, 8, 3871), ([(300, 3000)], 4, 1, 2800)]
+
+
+@pytest.mark.parametrize("seqs,H,Hkv,at", VALUES)
+def test_values_that_are_no_numbers_reach_their_columns(seqs, H, Hkv, at):
+    """Finite keys: a row that sees the key has the infinity or NaN in exactly the columns of its value, the rows before, and all other
+    columns, what they have without it."""
+    print(f"values that are no numbers {seqs} H={H} Hkv={Hkv} at {at}", flush=True)
+    n, kv = seqs[0]
+    before = at - (kv - n)                            # tokens of the first sequence that don't see it
+    assert 0 < before < n
+    c, T = make(seqs, Hkv, HD, 16, seed=22)
+    _, _, table = lists(c)
+    clean = {**c, "v_cache": c["v_cache"].clone()}
+    columns = {3: float("inf"), 64: float("-inf"), 77: float("nan"), 127: float("inf")}
+    for col, x in columns.items():
+        c["v_cache"][table[0, at // 16], at % 16, :, col] = x
+        clean["v_cache"][table[0, at // 16], at % 16, :, col] = 0
+    q, o, lse = call(c, T, H)
+    _, o0, lse0 = call(clean, T, H)
+    against_64_bits(q, o0, lse0, clean, seqs, H)
+    assert torch.equal(lse, lse0)
+    seen, got = o[before:n].float().view(-1, HD), o.clone()
+    for col, x in columns.items():
+        assert bool((seen[:, col] == x).all() if x == x else seen[:, col].isnan().all()), col
+        got[before:n].view(-1, H, HD)[..., col] = o0[before:n].view(-1, H, HD)[..., col]
+    assert torch.equal(got, o0)
+
+
+# ---- long runs of pages, many sequences ------------------------------------------------------------------------
+def _tiles(kv):
+    return max(1, -(-kv // 64))
+
+
+def _narrow_blocks(seqs, Hkv):
+    """32-key blocks of the longest run that one wavefront takes, of a batch of single tokens: the kernel's rule for splits."""
+    w = Hkv * sum(_tiles(kv) for _, kv in seqs)
+    assert w > 4 * 512
+    length = max(-(-w // 2048), int((w / 64) ** 0.5) + 1, 2)
+    longest = 0
+    for _, kv in seqs:
+        splits = max(1, (_tiles(kv) + length // 2) // length)
+        longest = max(longest, -(-(-(-_tiles(kv) // splits) * 2) // 4))
+    return longest
+
+
+@pytest.mark.parametrize("page", [8, 16, 48])
+def test_single_tokens_over_long_runs_of_pages(page):
+    """A wavefront's keys pass more than one window of 512, whose page numbers are on their way while others are worked on."""
+    seqs = [(1, 8192 - 97 * b) for b in range(64)]
+    assert _narrow_blocks(seqs, 8) >= 16           # (half a window and the two blocks around it are 10)
+    c, T = make(seqs, 8, HD, page, seed=23)
+    q, o, lse = call(c, T, 32)
+    against_64_bits(q, o, lse, c, seqs, 32)
+    again = call(c, T, 32)
+    assert torch.equal(o, again[1]) and torch.equal(lse, again[2])
+
+
+@pytest.mark.parametrize("seqs,H,Hkv,page", [
+    # more sequences than lanes, long ones of many rows among the first 64, the next and the last
+    ([(1, 300)] * 30 + [(70, 2000)] + [(1, 500)] * 60 + [(100, 2500), (2, 900)] + [(1, 200)] * 40 + [(300, 300), (1, 3000)], 8, 2, 16),
+    ([(1, 2000)] * 100 + [(256, 4096)] + [(1, 2000)] * 19, 8, 2, 64),
+    # very many
+    ([(1, 1 + 7 * b % 301) for b in range(1500)], 4, 1, 8), ([(1 + b % 3, 3 + b % 40) for b in range(4200)], 2, 1, 8)])
+def test_more_sequences_than_lanes(seqs, H, Hkv, page):
+    print(f"{len(seqs)} sequences H={H} Hkv={Hkv} page={page}", flush=True)
+    c, T = make(seqs, Hkv, HD, page, seed=24)
+    q, o, lse = call(c, T, H)
+    against_64_bits(q, o, lse, c, seqs, H)
