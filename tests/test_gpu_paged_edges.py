@@ -179,3 +179,33 @@ def test_more_sequences_than_lanes(seqs, H, Hkv, page):
     c, T = make(seqs, Hkv, HD, page, seed=24)
     q, o, lse = call(c, T, H)
     against_64_bits(q, o, lse, c, seqs, H)
+
+
+# ---- what a row's rounding may cost ------------------------------------------------------------------------------
+@pytest.mark.parametrize("n,kv", [(150, 700), (50, 100), (40, 640), (3, 640), (600, 8000)])
+def test_a_row_that_one_key_takes(n, kv):
+    """The largest probability of a row counts in full: where one key has nearly all of the weight, o is its value, rounded once.  The first
+    key scores 0, key 70 5 a (a the query's, 0.8 .. 1.05), all others -30 a.  With w0 = exp(-5 a) <= 0.02 the first key's weight
+    relative to the largest, rounded to bf16 (2^-8), and the others' at most kv exp(-28) < 2^-25:
+    |o - ref| <= 2^-8 |ref| + (2^-8 w0 + 2^-18) 2 max|v|."""
+    H, Hkv, page = 4, 2, 16
+    c, T = make([(n, kv)], Hkv, HD, page, seed=25)
+    _, _, table = lists(c)
+    c["k_cache"].zero_()
+    c["k_cache"][..., 0] = -30.0
+    for j, x in ((0, 0.0), (70, 5.0)):
+        c["k_cache"][table[0, j // page], j % page, :, 0] = x
+    q = torch.zeros((T, H, HD), dtype=BF, device=DEV)
+    q[..., 0] = torch.linspace(0.8, 1.05, T * H, device=DEV).view(T, H).to(BF)
+    o, _ = B.lr_attention_paged_fwd(q.view(T, -1), H=H, scale=1.0, **c)
+    torch.cuda.synchronize()
+    k, v = (x.double().view(kv, Hkv, HD) for x in _dense(c, 0, kv))
+    limit = torch.arange(kv - n, kv, device=DEV)
+    rows = limit >= 70                               # tokens that see the key
+    for h in range(H):
+        s = q[:, h, 0].double()[:, None] * k[None, :, h // 2, 0]
+        w = torch.softmax(s.masked_fill(torch.arange(kv, device=DEV)[None] > limit[:, None], float("-inf")), 1)
+        ref, a = w @ v[:, h // 2].contiguous(), q[:, h, 0].double()[:, None]
+        err = (o[:, h * HD:(h + 1) * HD].double() - ref).abs()
+        bound = 2.0 ** -8 * ref.abs() + (2.0 ** -8 * torch.exp(-5 * a) + 2.0 ** -18) * 2 * v.abs().max()
+        assert bool((err <= bound)[rows].all()), (h, float((err / bound)[rows].max()))
