@@ -63,8 +63,8 @@ __device__ __forceinline__ ArgPtr args_again() {
 }
 __device__ __forceinline__ uint32_t div_by(uint32_t n, uint32_t mul, uint32_t shift) { return (uint32_t)(((uint64_t)n * mul) >> shift); }
 
-// The running maximum of a row that has seen no key: finite, so that no difference of two of them is undefined, and below any score whose
-// product with the exponent's factor c is finite.
+// The running maximum of a row that has seen no key: finite, so that no difference of two of them is undefined, and below the score of any
+// logit that the library takes (2^26 in magnitude, at factors c from 2^-100 on).
 __device__ __forceinline__ float no_score(float c) { return -3.0e38f / fmaxf(c, 1.f); }
 
 // ---- the split of the work ------------------------------------------------------------------------------
@@ -213,12 +213,11 @@ __device__ __forceinline__ void first_window(ArgPtr a, Pages& pg, const PageSour
 // Descriptors of a group's keys and values: the same place in both.
 struct Group { uint64_t at; uint32_t bytes; };
 // A vector write of a scalar needs five wait states before a load's descriptor has it, and the compiler does not see the loads: asked for right before
-// them, the group waits (SETTLE); asked for a slot of other work earlier, it does not have to (the machine code is checked for either).
-template <bool SETTLE = true>
+// them, a group waits (the machine code is checked for it).
 __device__ __forceinline__ Group group(const Pages& pg, int g) {
   const uint32_t place = __builtin_amdgcn_readlane(pg.place, g & 63);
   uint32_t bytes = __builtin_amdgcn_readlane(pg.bytes, g & 63);
-  if constexpr (SETTLE) asm volatile("s_nop 4" : "+s"(bytes));
+  asm volatile("s_nop 4" : "+s"(bytes));
   return Group{(uint64_t)place << 4, bytes};
 }
 __device__ __forceinline__ rsrc_t group_rsrc(const Group& g, const uint16_t* base) {
@@ -228,6 +227,7 @@ __device__ __forceinline__ rsrc_t group_rsrc(const Group& g, const uint16_t* bas
 
 // For long runs of tiles: the groups' addresses in one of the caches, so that a descriptor is three lanes' values and nothing else (24 scalar
 // instructions less per tile and wavefront than from places: a wavefront that is alone on its SIMD is bound by how many instructions it issues).
+// Asked for a slot of other work before the load, a descriptor does not have to wait (no SETTLE; the machine code is checked for either).
 struct Spots { uint32_t lo, hi, bytes; };
 __device__ __forceinline__ Spots spots(const Pages& pg, const uint16_t* base) {
   const uint64_t at = (uint64_t)(uintptr_t)base + ((uint64_t)pg.place << 4);
