@@ -343,8 +343,11 @@ void same_type(const at::Tensor& a, std::initializer_list<const at::Tensor*> oth
   for (const at::Tensor* t : others)
     if (t->defined() && t->scalar_type() != a.scalar_type()) fail(g_lr_error, "operands of one type expected");
 }
-void rows_as_wide(const at::Tensor& t, int64_t T, int64_t width) {
+// The row stride of T rows that are at least as wide (of a single row any will do).
+int64_t rows_as_wide(const at::Tensor& t, int64_t T, int64_t width) {
   if (t.dim() != 2 || t.size(0) != T || t.size(1) < width) fail(PyExc_ValueError, "unexpected shape");
+  const int64_t ld = stride_of(t);
+  return T > 1 ? ld : width;
 }
 // rows and pairs of the tables
 void tables_of(const at::Tensor& cos, const at::Tensor& sin, int64_t& rows, int64_t& half) {
@@ -375,16 +378,15 @@ PyObject* rope_at(Args& a) {
   const at::Tensor pos = a.optional();
   const int inter = a.enumerator(), inverse = a.enumerator();
   at::Tensor out = a.optional();
-  const int64_t T = rows_of(x), ldx = stride_of(x);
+  const int64_t T = rows_of(x);
   const int dt = dt_of(x);
   int64_t rows, half;
   tables_of(cos, sin, rows, half);
   const int32_t* pp = indices(pos, T);
-  rows_as_wide(x, T, H * hd);
+  const int64_t ldx = rows_as_wide(x, T, H * hd);
   if (!out.defined()) out = fresh({T, H * hd}, x.scalar_type(), x);
   same_type(x, {&out});
-  rows_as_wide(out, T, H * hd);
-  const int64_t ldo = stride_of(out);
+  const int64_t ldo = rows_as_wide(out, T, H * hd);
   on_current_device({&x, &cos, &sin, &pos, &out});
   void *px = ptr(x), *pc = dense(cos), *ps = dense(sin), *po = ptr(out), *st = stream();
   call("lr_rope_at", [&] { return lr_rope_at(px, ldx, po, ldo, pp, (float*)pc, (float*)ps, rows, T, H, hd, 2 * half, inter, inverse, dt, st); });
@@ -424,20 +426,17 @@ PyObject* kv_append(Args& a) {
   const int64_t H = a.integer();
   at::Tensor q_out = a.optional();
   const lr_kv_cache c = ct.view();
-  const int64_t T = rows_of(k), ldk = stride_of(k), ldv = stride_of(v);
+  const int64_t T = rows_of(k);
   const int dt = dt_of(k);
   int64_t rows = 0, half = 0, ldq = 0, ldqo = 0;
   if (cos.defined() != sin.defined()) fail(PyExc_ValueError, "both tables or neither expected");
   if (cos.defined()) tables_of(cos, sin, rows, half);
   if (cos.defined() && half == 0) fail(PyExc_ValueError, "tables without columns");
-  rows_as_wide(k, T, c.n_kv_heads * c.head_dim);
-  rows_as_wide(v, T, c.n_kv_heads * c.head_dim);
+  const int64_t ldk = rows_as_wide(k, T, c.n_kv_heads * c.head_dim), ldv = rows_as_wide(v, T, c.n_kv_heads * c.head_dim);
   if (q.defined()) {
-    rows_as_wide(q, T, H * c.head_dim);
-    ldq = stride_of(q);
+    ldq = rows_as_wide(q, T, H * c.head_dim);
     if (!q_out.defined()) q_out = fresh({T, H * c.head_dim}, q.scalar_type(), q);
-    rows_as_wide(q_out, T, H * c.head_dim);
-    ldqo = stride_of(q_out);
+    ldqo = rows_as_wide(q_out, T, H * c.head_dim);
   }
   same_type(k, {&v, &q, &q_out});
   on_current_device({&k, &v, &ct.k, &ct.v, &ct.table, &ct.cu, &ct.len, &cos, &sin, &q, &q_out});
@@ -457,13 +456,12 @@ PyObject* attention_paged_fwd(Args& a) {
   const int causal = a.enumerator();
   at::Tensor o = a.optional(), lse = a.optional(), ws = a.optional();
   const lr_kv_cache c = ct.view();
-  const int64_t T = rows_of(q), ldq = stride_of(q);
+  const int64_t T = rows_of(q);
   const int dt = dt_of(q);
-  rows_as_wide(q, T, H * c.head_dim);
+  const int64_t ldq = rows_as_wide(q, T, H * c.head_dim);
   if (!o.defined()) o = fresh({T, H * c.head_dim}, q.scalar_type(), q);
-  rows_as_wide(o, T, H * c.head_dim);
+  const int64_t ldo = rows_as_wide(o, T, H * c.head_dim);
   same_type(q, {&o});
-  const int64_t ldo = stride_of(o);
   if (!lse.defined()) lse = fresh({T, H}, at::kFloat, q);
   if (lse.scalar_type() != at::kFloat || lse.dim() != 2 || lse.size(0) != T || lse.size(1) != H) fail(PyExc_ValueError, "lse [T, H] fp32 expected");
   on_current_device({&q, &ct.k, &ct.v, &ct.table, &ct.cu, &ct.len, &o, &lse, &ws});

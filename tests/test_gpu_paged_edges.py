@@ -209,3 +209,34 @@ def test_a_row_that_one_key_takes(n, kv):
         err = (o[:, h * HD:(h + 1) * HD].double() - ref).abs()
         bound = 2.0 ** -8 * ref.abs() + (2.0 ** -8 * torch.exp(-5 * a) + 2.0 ** -18) * 2 * v.abs().max()
         assert bool((err <= bound)[rows].all()), (h, float((err / bound)[rows].max()))
+
+
+# ---- dimensions of one ------------------------------------------------------------------------------------------
+def _one_row(t, pad=0):
+    """The values of t [1, n] in a tensor whose row stride is 1, as a turned column has it."""
+    out = torch.zeros((t.shape[1] + pad, 1), dtype=t.dtype, device=t.device).t()
+    out[:, :t.shape[1]] = t
+    assert out.stride() == (1, 1)
+    return out
+
+
+def test_one_token_with_any_row_stride():
+    H, Hkv = 4, 2
+    g = torch.Generator(device=DEV).manual_seed(27)
+    q, k, v = (torch.randn((1, w * HD), generator=g, device=DEV).to(BF) for w in (H, Hkv, Hkv))
+    rope = B.lr_rope_table(64, HD, device=DEV)
+    got = []
+    for row in (lambda t: t, _one_row, lambda t: _one_row(t, 3)):
+        c, _ = make([(1, 40)], Hkv, HD, 16, seed=27)
+        out = row(torch.zeros_like(q))
+        qr = B.lr_kv_append(row(k), row(v), rope=rope, q=row(q), H=H, q_out=out, **c)
+        turned = B.lr_rope_at(row(q), *rope, H, HD, pos=torch.full((1,), 39, dtype=torch.int32, device=DEV), out=row(torch.zeros_like(q)))
+        place = row(q.clone())
+        B.lr_rope_at(place, *rope, H, HD, pos=torch.full((1,), 39, dtype=torch.int32, device=DEV), out=place)
+        o, lse = B.lr_attention_paged_fwd(qr, H=H, o=row(torch.zeros_like(q)), **c)
+        torch.cuda.synchronize()
+        assert qr.data_ptr() == out.data_ptr()
+        got.append([c["k_cache"], c["v_cache"], qr[:, :H * HD], turned[:, :H * HD], place[:, :H * HD], o[:, :H * HD], lse])
+    assert torch.equal(got[0][3], got[0][2])
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
