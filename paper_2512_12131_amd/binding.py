@@ -514,8 +514,8 @@ def lr_attention_paged_workspace_bytes(k_cache, page_table, T, H):
     """Bytes of a workspace for calls of T tokens and H query heads on such a cache."""
     pages, page_size, Hkv, hd = k_cache.shape
     batch, cols = page_table.shape
-    c = KvCache(None, None, pages, page_size, Hkv, hd, k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), None, batch, cols,
-                page_table.stride(0) if batch > 1 else cols, None, None)
+    strides = [k_cache.stride(i) if k_cache.shape[i] > 1 else hd for i in range(3)]      # (as the call: of one page, token or head any will do)
+    c = KvCache(None, None, pages, page_size, Hkv, hd, *strides, None, batch, cols, page_table.stride(0) if batch > 1 else cols, None, None)
     return lib().lr_attention_paged_workspace_bytes(C.byref(c), T, H)
 
 

@@ -400,14 +400,17 @@ struct CacheTensors {
   lr_kv_cache view() const {
     if (k.dim() != 4 || v.sizes() != k.sizes() || table.dim() != 2) fail(PyExc_ValueError, "unexpected shape of the cache or its page table");
     if (k.scalar_type() != at::kBFloat16 || v.scalar_type() != at::kBFloat16) fail(g_lr_error, "a bf16 cache expected");
-    if (k.stride(3) != 1 || v.strides() != k.strides()) fail(PyExc_AssertionError, "caches with the same strides and contiguous heads expected");
+    bool alike = k.stride(3) == 1 && v.stride(3) == 1;
+    for (int i = 0; i < 3; i++) alike &= k.size(i) <= 1 || v.stride(i) == k.stride(i);
+    if (!alike) fail(PyExc_AssertionError, "caches with the same strides and contiguous heads expected");
     if (table.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
     if (table.size(1) > 1 && table.stride(1) != 1) fail(PyExc_AssertionError, "row-major page table expected");
     const int64_t batch = table.size(0), cols = table.size(1);
     lr_kv_cache c;
     c.k = ptr(k); c.v = ptr(v);
     c.n_pages = k.size(0); c.page_size = k.size(1); c.n_kv_heads = k.size(2); c.head_dim = k.size(3);
-    c.page_stride = k.stride(0); c.token_stride = k.stride(1); c.head_stride = k.stride(2);
+    const auto stride = [&](int i) { return k.size(i) > 1 ? k.stride(i) : c.head_dim; };      // (of one page, token or head any will do)
+    c.page_stride = stride(0); c.token_stride = stride(1); c.head_stride = stride(2);
     c.page_table = (const int32_t*)ptr(table);
     c.batch = batch; c.max_pages = cols;
     c.table_ld = batch > 1 ? table.stride(0) : cols;

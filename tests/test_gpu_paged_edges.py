@@ -240,3 +240,26 @@ def test_one_token_with_any_row_stride():
     assert torch.equal(got[0][3], got[0][2])
     for other in got[1:]:
         assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+def test_one_page_and_one_head_with_any_stride():
+    """Turned dimensions of one: the bits of the plain cache."""
+    g = torch.Generator(device=DEV).manual_seed(28)
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=DEV)
+    for pages, heads in ((1, 2), (4, 1)):
+        plain = [torch.randn((pages, 48, heads, HD), generator=g, device=DEV).to(BF) for _ in range(2)]
+        lens = {"page_table": i32([list(range(pages))[::-1]]), "cu_q": i32([0, 3]), "kv_len": i32([48 * pages - 5])}
+        k, v, q = (torch.randn((3, w * HD), generator=g, device=DEV).to(BF) for w in (heads, heads, 4))
+        dim, got = (0 if pages == 1 else 2), []
+        for turn in (False, True):
+            caches = [x.clone() for x in plain]
+            if turn:
+                caches = [torch.stack([x.select(dim, 0)], -1).movedim(-1, dim) for x in caches]
+                assert caches[0].stride(dim) == 1
+                caches[1] = plain[1].clone()                       # strides of its own
+            c = {"k_cache": caches[0], "v_cache": caches[1], **lens}
+            B.lr_kv_append(k, v, **c)
+            o, lse = B.lr_attention_paged_fwd(q, H=4, **c)
+            torch.cuda.synchronize()
+            got.append([o, lse, *caches])
+        assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -1,4 +1,5 @@
 """Limits of the rotary tables and the paged cache: the boundary of each, from both sides, before anything reaches a device."""
+import pytest
 import torch
 
 from paper_2512_12131_amd import binding as B
@@ -53,3 +54,20 @@ def test_scales_of_the_attention():
         assert _paged(scale=scale, T=0) == EINVAL, scale
     for scale in (2.3e38, 1.0, 1e-37):
         assert _paged(scale=scale, T=0) == 0, scale
+
+
+def test_caches_of_one_page_or_head():
+    """Strides of dimensions of one say nothing: turned ones have any, and keys and values need not have the same."""
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    page = bf(16, 2, 128, 1).permute(3, 0, 1, 2)                   # [1, 16, 2, 128]
+    head = bf(6, 16, 128, 1).permute(0, 1, 3, 2)                   # [6, 16, 1, 128]
+    other = bf(6, 1, 16, 128).transpose(1, 2)
+    assert page.is_contiguous() and page.stride(0) == 1 and head.stride(2) == 1 and other.stride(2) == 2048 and head.shape == other.shape
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    for k, v in ((page, page), (page, bf(1, 16, 2, 128)), (head, head), (head, other), (other, head)):
+        heads = k.shape[2]
+        assert B.lr_attention_paged_workspace_bytes(k, i32(1, 30), 1, 4) > 0
+        with pytest.raises(B.LrError, match="current GPU"):        # as far as a CPU tensor gets
+            B.lr_attention_paged_fwd(bf(1, 512), k, v, i32(1, 30), i32(2), i32(1), 4)
+        with pytest.raises(B.LrError, match="current GPU"):
+            B.lr_kv_append(bf(1, heads * 128), bf(1, heads * 128), k, v, i32(1, 30), i32(2), i32(1))
