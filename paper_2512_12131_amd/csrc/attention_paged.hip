@@ -861,17 +861,6 @@ __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, in
   }
 }
 
-// Item of workgroup v, of `wide` wide items, a CU for each or fewer, and then `narrow` narrow ones, with them more than find a place together: every second
-// of the wide ones, narrow ones for the CUs that are left, then the other wide ones, which share CUs with the first.  Beside a narrow item, whose
-// loads wait for memory in the same queue, a wide one takes 2.4 us per tile, beside another wide one 2 (one chunk of 512 tokens and 31 single ones over
-// 4000 keys 122 -> 118 us, 3 chunks of 64 beside 29 single ones 66 -> 65).  More wide items share CUs anyway and stay in order, the longest first
-// (the mixed batch 91, else 94 us), as fewer of both kinds do, which have a CU each.
-__device__ __forceinline__ uint32_t side_by_side(uint32_t v, uint32_t wide, uint32_t narrow) {
-  if (wide > PLACES / 2 || wide + narrow < PLACES) return v;
-  const uint32_t half = (wide + 1) / 2, first = min(narrow, PLACES / 2 - half);
-  return v < half ? v : v < half + first ? wide + v - half : v < wide + first ? v - first : v;
-}
-
 // One workgroup per item: sequence, run of blocks, key / value head, split, block of rows in the run.
 __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -899,7 +888,6 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
     }
     // wide sequences' items, which take longer, before the others' of the same 64
     const uint32_t wide = s.rows > R_NARROW ? items : 0, wide_end = wave_scan(wide), other_end = wave_scan(items - wide);
-    if (a.c.batch <= 64) v = side_by_side(v, last_lane(wide_end), last_lane(other_end));
     item_end = item0 + (wide > 0 ? wide_end : last_lane(wide_end) + other_end);
     part_end = part0 + wave_scan(parts);
     hit = __builtin_amdgcn_ballot_w64(v - (item_end - items) < items);
