@@ -868,12 +868,11 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
   Seq s = {};
   if (lane < a.c.batch) s = load_seq(a, lane);
   const SplitLen len = split_len(a, s);
-  // The hardware deals workgroups to the 8 XCDs in rotation; a run, which reads the same keys, stays on one.  Back and forth over the XCDs: a
-  // prompt's runs shrink, and dealt in one direction the first XCD had the longest of every eight (4 x 4096 tokens: 1.04 ms).
+  // The hardware deals workgroups to the 8 XCDs in rotation; a run, which reads the same keys, stays on one.
   uint32_t v = blockIdx.x;
   if (a.runs) {
-    const uint32_t x = v % 8, j = v / 8, round = j / RUN;
-    v = (round * 8 + (round & 1 ? 7 - x : x)) * RUN + j % RUN;
+    const uint32_t x = v % 8, j = v / 8;
+    v = (j / RUN * 8 + x) * RUN + j % RUN;
   }
   uint32_t item0 = 0, part0 = 0, item_end, part_end, splits, items, parts;
   uint64_t hit = 0;
