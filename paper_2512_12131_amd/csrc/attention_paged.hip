@@ -7,14 +7,14 @@
 //            before the end, where they join their sums.  Bound by memory: every key and value is read once (64 single tokens over 4600 keys on
 //            average, 32 / 8 heads, 1.2 GB: 193 us, 6.2 TB/s).
 //   wide     the four wavefronts take 32 rows each, keys and values pass through LDS in tiles of 64 for all of them.  Bound by the matrix
-//            and vector units (4 x 2048 tokens over 8192 keys: 0.88 - 0.91 ms, 1.06 - 1.09 PFLOP/s, matrix units busy for 60 % of the cycles at
+//            and vector units (4 x 2048 tokens over 8192 keys: 0.93 - 0.95 ms, 1.01 - 1.03 PFLOP/s, matrix units busy for 55 % of the cycles at
 //            the 1.7 GHz that the power limit leaves).
 // Both compute S^T = K Q^T and O^T += V^T P^T on 32 x 32 x 16 MFMAs with the running maximum and sum of a softmax (one lane column per row),
 // as attention.hip does.
 //
 // Keys.  Nothing but the lists knows how long sequences are, and they stay on the device.  So every workgroup adds the work of all
 // sequences up by itself (64 of them at a time, one per lane), and sequences are cut into splits of equal length such that all of them
-// together are some rounds of the chip; a second kernel joins what was split, in the order of the splits (4 - 7 us).  No atomics: the same
+// together are some rounds of the chip; a second kernel joins what was split, in the order of the splits (4 - 8 us).  No atomics: the same
 // lists give the same bits.  A workgroup's way in (lists, search, page numbers, first keys: loads that wait for each other) is 4 - 5 us.
 //
 // Pages.  Eight keys that start at a multiple of eight lie in one page.  A lane looks one such group up and keeps its place in the cache in
@@ -114,10 +114,10 @@ __device__ __forceinline__ Seq load_seq(const PagedArgs& a, int b) {
 //   wide    w / PLACES (of little work half of the places, a CU each): more splits than places save nothing.  And no less than
 //           sqrt(x / 6150), x the tiles times their rows: len tiles take len * 1.6
 //           us, and x / len rows of sums 0.26 ns each on their way through memory.  A sequence of two of the latter, or of three tiles, is not
-//           split, since the join takes some us by itself.  (us, against the narrow rule for both: a prompt of 777 tokens 31.2 -> 25.9, of
-//           2048 70 -> 56, 512 tokens over 8192 keys 93 -> 83, over 32768 301 -> 268, 6 chunks of up to 256
+//           split, since the join takes some us by itself.  (us, against the narrow rule for both: a prompt of 777 tokens 31.0 -> 26.9, of
+//           2048 74 -> 58, 512 tokens over 8192 keys 97 -> 87, over 32768 314 -> 284, 6 chunks of up to 256
 //           tokens beside 18 single ones over up to 4096 keys, the mixed batch below, 101 -> 93.  Four tiles split in two: 10
-//           tokens over 250 keys 12.8 -> 11.7; three: 3 prompts of 108 behind 26 keys 13.1 -> 14.6.)
+//           tokens over 250 keys 12.7 -> 11.3; three: the same within 1.5 %, 6 batches of up to 180 keys.)
 struct SplitLen { uint32_t narrow, wide, whole; };      // whole: wide sequences of up to so many tiles are not split
 // Sum over the lanes, in an order of its own: both kernels get the same bits.  (Products and sums are rounded one by one wherever this is inlined.)
 __device__ __forceinline__ float lanes_sum(float x) {
@@ -151,8 +151,8 @@ __device__ __forceinline__ SplitLen split_len(const PagedArgs& a, const Seq& fir
   const uint32_t traffic = max(root(x, 1.f / 6150.f), (uint32_t)MIN_SPLIT), fill = max(part(places), min(part(places / 2), 8u));
   return SplitLen{max(narrow, (uint32_t)MIN_SPLIT), max(fill, traffic), max(2 * root(x, 1.f / 6150.f), 3u)};
 }
-// (rounded to the nearer number, wide ones' up from a quarter, since the longest item decides: 16 chunks of up to 256 tokens beside 16 single ones
-// 222 -> 210 us, the mixed batch 97 -> 92; as even as they can be)
+// (rounded to the nearer number, wide ones' up from a quarter, since the longest item decides: the mixed batch 97 -> 92 us, 16 chunks of up to 256
+// tokens beside 16 single ones 204 either way; as even as they can be)
 __device__ __forceinline__ uint32_t splits_of(const Seq& s, const SplitLen& l) {
   const bool wide = s.rows > R_NARROW;
   const uint32_t len = wide ? l.wide : l.narrow, n = ((uint32_t)s.tiles + (wide ? len * 3 / 4 : len / 2)) / len;
@@ -181,7 +181,8 @@ __device__ __forceinline__ int ask_pages(ArgPtr a, const PageSource& p, int w, i
   return key < (uint32_t)p.end ? p.row[div_by(key, a->c.by_page.mul, a->c.by_page.shift)] : -1;
 }
 // ... into the spot, on the way while others are worked on.  A load into registers would not do: the compiler waits for it where the loop comes round,
-// and so for all tiles' loads before it (a prompt of 2048 tokens 57.5 -> 53.8 us without, 64 single tokens over 1000 keys 47.1 -> 45.5).
+// and so for all tiles' loads before it (a prompt of 2048 tokens 57.5 -> 53.8 us without, 64 single tokens over 1000 keys 47.1 -> 45.5, at the time of
+// a maximum in steps).
 __device__ __forceinline__ void ask_ahead(ArgPtr a, const PageSource& p, int w, int lane) {
   const uint32_t col = div_by((uint32_t)w * 512u + (uint32_t)lane * 8u, a->c.by_page.mul, a->c.by_page.shift);
   const uint32_t cols = div_by((uint32_t)p.end - 1u, a->c.by_page.mul, a->c.by_page.shift) + 1u;
@@ -811,7 +812,9 @@ __device__ __forceinline__ bool wide_long(ArgPtr in, Rows& st, const WideTiles& 
   return bad;
 }
 
-constexpr int LONG = 8;          // tiles from which on the long form is faster (its code and its way in are longer: 64 tokens over 600 keys 18.8 -> 20.0 us with it from 4 tiles on, a prompt of 640 22.9 -> 23.8 without it up to 12)
+// Tiles from which on the long form is faster, whose code and way in are longer (16 prompts of 256 tokens 38.0 -> 40.3 us with it from 4 tiles on, a prompt
+// of 640 23.4 -> 24.7 without it up to 12).
+constexpr int LONG = 8;
 
 __device__ __forceinline__ void wide_item(const Seq& s, const int32_t* table, int kvh, int row0, int key_lo, int key_hi, bool whole,
                                           uint32_t part0, unsigned char* smem) {
@@ -885,7 +888,7 @@ __global__ __launch_bounds__(256, 2) void paged_kernel(PagedArgs a) {
       items = (uint32_t)a.c.n_kv_heads * splits * (uint32_t)s.blocks;
       parts = part_rows_of(a, s, splits);
     }
-    // wide sequences' items, which take longer, before the others' of the same 64
+    // wide sequences' items before the others' of the same 64
     const uint32_t wide = s.rows > R_NARROW ? items : 0, wide_end = wave_scan(wide), other_end = wave_scan(items - wide);
     item_end = item0 + (wide > 0 ? wide_end : last_lane(wide_end) + other_end);
     part_end = part0 + wave_scan(parts);
