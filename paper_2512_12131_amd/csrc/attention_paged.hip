@@ -7,7 +7,7 @@
 //            before the end, where they join their sums.  Bound by memory: every key and value is read once (64 single tokens over 4600 keys on
 //            average, 32 / 8 heads, 1.2 GB: 193 us, 6.2 TB/s).
 //   wide     the four wavefronts take 32 rows each, keys and values pass through LDS in tiles of 64 for all of them.  Bound by the matrix
-//            and vector units (4 x 2048 tokens over 8192 keys: 0.93 - 0.95 ms, 1.01 - 1.03 PFLOP/s, matrix units busy for 55 % of the cycles at
+//            and vector units (4 x 2048 tokens over 8192 keys: 0.93 - 0.98 ms, 0.98 - 1.03 PFLOP/s, matrix units busy for 55 % of the cycles at
 //            the 1.7 GHz that the power limit leaves).
 // Both compute S^T = K Q^T and O^T += V^T P^T on 32 x 32 x 16 MFMAs with the running maximum and sum of a softmax (one lane column per row),
 // as attention.hip does.
