@@ -361,7 +361,7 @@ int lr_kv_append(const lr_kv_cache* cache, const void* k, int64_t ldk, const voi
 /* Causal attention of the new tokens over the cache, which holds their own keys and values already: o[T, ldo] (H heads) =
  * softmax(scale * q . k) . v over the keys at positions up to the token's own, query head h on key / value head
  * h / (H / n_kv_heads); lse[T, H] (fp32, NULL: not written) = log of the softmax's sum.  Any mixture of long and single-token sequences.
- * A token that sees no key has o = 0 and lse = -infinity; a page number that is no page holds zeros.  H % n_kv_heads == 0, scale > 0,
+ * A token that sees no key, or only keys whose logits are -infinity, has o = 0 and lse = -infinity; a page number that is no page holds zeros.  H % n_kv_heads == 0, scale > 0,
  * scale * log2(e) finite.  Logits scale * q . k are formed in 32 bits and below 2^26 in magnitude (where neighbours are 4 apart): far above, a row may come
  * out as zeros or NaN.
  * dt LR_BF16, head_dim 128, causal 1, otherwise LR_EUNSUPPORTED.  The workspace holds the parts of sequences whose keys are split over workgroups;

@@ -263,3 +263,24 @@ def test_one_page_and_one_head_with_any_stride():
             torch.cuda.synchronize()
             got.append([o, lse, *caches])
         assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("seqs", [[(1, 300), (3, 70)], [(150, 150)], [(200, 1500)]])
+def test_rows_whose_logits_are_all_minus_infinity(seqs):
+    """They are as rows without keys; beside them, rows that see one finite key are its value."""
+    H, Hkv, page = 4, 2, 16
+    c, T = make(seqs, Hkv, HD, page, seed=29)
+    _, _, table = lists(c)
+    n, kv = seqs[0]
+    last = tuple(torch.tensor(x, device=DEV) for x in (table[0, (kv - 1) // page], (kv - 1) % page))
+    c["k_cache"].zero_()
+    c["k_cache"][..., 0] = float("-inf")
+    c["k_cache"][last[0], last[1], :, 0] = 2.0          # the last key of the first sequence
+    q = torch.zeros((T, H, HD), dtype=BF, device=DEV)
+    q[..., 0] = 1.0
+    o, lse = B.lr_attention_paged_fwd(q.view(T, -1), H=H, **c)
+    torch.cuda.synchronize()
+    v = c["v_cache"][last].repeat_interleave(H // Hkv, 0)
+    seen = torch.arange(T, device=DEV) == n - 1
+    assert torch.equal(o[seen].view(H, HD), v) and bool((lse[seen] - 2 * HD ** -0.5).abs().max() < 2.0 ** -20)
+    assert bool((o[~seen] == 0).all()) and bool(lse[~seen].isneginf().all())
