@@ -318,7 +318,7 @@ int lr_attention_gqa_bwd(const void* q, const void* k, const void* v, const void
 int lr_rope_table(float* cos_tab, float* sin_tab, int64_t n, int64_t rot, int64_t first, double base, double factor,
                   double context, double low, double high, double mscale, void* stream);
 /* out[T, ldo] = x[T, ldx] (H heads of hd columns from column 0) with the first rot columns of every head rotated by row pos[t] (DEVICE
- * int32; NULL: t) of the tables [table_rows, rot / 2]: pairs (i, i + rot / 2), or (2i, 2i + 1) where interleaved != 0, become
+ * int32; NULL: t, T <= table_rows) of the tables [table_rows, rot / 2]: pairs (i, i + rot / 2), or (2i, 2i + 1) where interleaved != 0, become
  * (a c - b s, b c + a s).  inverse != 0 uses -s: the transpose, which is its gradient.  Columns rot.. of a head are copied; a row of
  * out whose position is outside the tables is left as it was, and so are columns past the heads.  out may be x with ldo = ldx (in
  * place); any other overlap is not allowed.  LR_BF16: hd and the strides multiples of 8, rot of 16, all pointers 16-byte aligned but
