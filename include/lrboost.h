@@ -371,6 +371,70 @@ size_t lr_attention_paged_workspace_bytes(const lr_kv_cache* cache, int64_t T, i
 int lr_attention_paged_fwd(const lr_kv_cache* cache, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse,
                            int64_t T, int64_t H, float scale, int causal, int dt, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- who holds the pages ------------------------------------------------------------------------ */
+/* refs[n_pages] (DEVICE int32) counts the holders of every page: the entries of page tables that name it, and whoever else is to keep it (a
+ * prompt's beginning that is held for later).  Pages of count 0 are free.  lr_kv_fork and lr_kv_compact read lists and write new ones (no output
+ * overlaps an input), so the caller keeps the old state until the new one is accepted.  All lists are DEVICE int32 and not read on the host; entries
+ * outside [0, n_pages) are no page.  The same lists give the same result.
+ *
+ * lr_kv_fork makes the page tables of n_out sequences from those of n_in: new sequence i goes on with the len_in[p] keys of p = parent[i] (outside
+ * [0, n_in): a sequence without keys) and has room for grow[i] new ones (below 0: 0), len_out[i] = len_in[p] + grow[i] (at most 2^31 - 1): the kv_len
+ * of lr_kv_append.  An old sequence that is nobody's parent ends.  Pages that its keys fill are shared by all children.  The half filled page
+ * stays with the first child where refs is 1; any other child takes a fresh page, to which lr_kv_copy has to bring copy_rows[i] tokens of
+ * copy_src[i] (copy_dst[i] the fresh page; -1, -1, 0: no copy) before new keys are appended.  The first child also keeps the pages behind.  A column that new
+ * keys reach and that has no page yet takes a fresh one: the lowest free ones (refs 0 at the call: pages that it frees are free for the next), given to the
+ * sequences in order.  Where there are too few, or no column is left, entries are -1 and missing[0] counts the pages that are missing.  refs_out follows all
+ * entries of the old and new tables.  Up to 2^14 old and new sequences, 2^26 pages (LR_EUNSUPPORTED).                                 */
+size_t lr_kv_fork_workspace_bytes(int64_t n_pages, int64_t n_in, int64_t n_out);
+int lr_kv_fork(const int32_t* refs_in, int64_t n_pages, int64_t page_size, const int32_t* table_in, int64_t ld_in, const int32_t* len_in,
+               int64_t n_in, const int32_t* parent, const int32_t* grow, int32_t* refs_out, int32_t* table_out, int64_t ld_out,
+               int32_t* len_out, int64_t n_out, int64_t max_pages, int32_t* copy_src, int32_t* copy_dst, int32_t* copy_rows,
+               int32_t* missing, void* ws, size_t ws_bytes, void* stream);
+/* Moves the held pages (refs above 0) together: with H of them, page_map[n_pages] gives every held page its new number below H (-1: free), the table
+ * [batch, max_pages] and refs follow it, n_live[0] = H.  The held pages from H on move, in order, into the free ones below, in order: copy_src and
+ * copy_dst [n_pages / 2] list them for lr_kv_copy, -1 behind the last.                                                                 */
+size_t lr_kv_compact_workspace_bytes(int64_t n_pages);
+int lr_kv_compact(const int32_t* refs_in, int64_t n_pages, const int32_t* table_in, int64_t ld_in, int64_t batch, int64_t max_pages, int32_t* refs_out,
+                  int32_t* table_out, int64_t ld_out, int32_t* copy_src, int32_t* copy_dst, int32_t* page_map, int32_t* n_live, void* ws,
+                  size_t ws_bytes, void* stream);
+/* Copies, for i < n, the first rows[i] tokens (NULL: all; taken as at least 0 and at most page_size) of page src[i] onto page dst[i], keys and values of
+ * all heads.  Entries with no page in src or dst are passed over.  A page that is written is in no other entry.  Of `cache` only the pages and their
+ * strides count (the lists may be NULL, batch 0).  Once for each layer whose cache the page tables describe.  At most 2^31 - 2^12 vectors of eight
+ * elements in a page's keys (LR_EUNSUPPORTED).                                                                                       */
+int lr_kv_copy(const lr_kv_cache* cache, const int32_t* src, const int32_t* dst, const int32_t* rows, int64_t n, void* stream);
+
+/* ---- which sequences go on ---------------------------------------------------------------------- */
+/* Beam search's choice: for each of `batch` prompts the n candidates (beam w, token v) of highest
+ *   score[b, w] + logits[b * beams + w, v] - log sum_u exp(logits[b * beams + w, u])
+ * in falling order, formed in 64 bits; equal ones by beam, then by token.  logits [batch * beams, ldl] (dt), V tokens; parent [batch, n] receives the
+ * row b * beams + w (what lr_kv_fork takes), token [batch, n] the token, score_out [batch, n] the score, rounded to fp32.  done [batch, beams] (int32, NULL: none):
+ * a beam with done != 0 has ended; its one candidate is done_token at its score, its logits are not read.  Logits of -infinity are no candidates; a beam whose
+ * score is no finite number, or whose logits hold a NaN, +infinity or nothing above -infinity, has none.  Where there are fewer than n: parent and token
+ * -1, score -infinity.  beams and n at most 64, V at most 2^20, batch * beams at most 2^20 (LR_EUNSUPPORTED).  Rows may start on any
+ * element.                                                                                                                          */
+size_t lr_beam_select_workspace_bytes(int64_t batch, int64_t beams, int64_t V, int64_t n);
+int lr_beam_select(const void* logits, int64_t ldl, const float* score, const int32_t* done, int64_t done_token, int32_t* parent, int32_t* token,
+                   float* score_out, int64_t batch, int64_t beams, int64_t V, int64_t n, int dt, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- products of 8-bit integers ----------------------------------------------------------------- */
+/* Rows as integers of 8 bits with a scale each: scale[t] = max_j |x[t, j]| / 127, at least 2^-126, and q[t, j] the whole number nearest to
+ * 127 x[t, j] / max_j |x[t, j]| (ties to even; of rows below 127 * 2^-126, x[t, j] * 2^126), -127 .. 127.  A row with an infinity or a NaN: scale NaN, zeros.  Activations by token, weights
+ * [out, in] by output channel.  q rows start on 16 bytes (q and ldq multiples of 16, LR_EALIGN) and are written up to the next multiple of 16 columns, with
+ * zeros.  LR_BF16: n and ldx multiples of 8, x 16-byte aligned.                                                                      */
+int lr_quant_rows(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t T, int64_t n, int dt, void* stream);
+/* c[m, n] = sa[m] * sb[n] * sum_k a[m, k] * b[n, k], the sum exact, the product in fp32 (the row's scale first), rounded to dt.  a [M, lda], b [N, ldb]: rows
+ * start on 16 bytes (pointers and strides multiples of 16) and can be read up to the next multiple of 16 columns, whatever is there.  c [M, ldc]: rows start on 16
+ * bytes; N is any.  K at most 133144 (2^31 / 127^2), lda and ldb at most 2^22 (LR_EUNSUPPORTED).                                       */
+int lr_matmul_q8(const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb, void* c, int64_t ldc, int64_t M,
+                 int64_t N, int64_t K, int dt, void* stream);
+/* The forward of one bottleneck layer with both weights in 8 bits: y = Q(act(Q(x) . W_down^T)) . W_up^T, Q = lr_quant_rows and back; z and act(z) are
+ * fp32 and not rounded in between.  w_down [r, ld_down], s_down [r], w_up [d_out, ld_up], s_up [d_out] as lr_matmul_q8 takes b.  x, y: as lr_linear_fwd (y's rows start on 16
+ * bytes in LR_F32 too).                                                                                                             */
+size_t lr_linear_q8_workspace_bytes(int64_t T, int64_t d_in, int64_t r);
+int lr_linear_q8_fwd(const void* x, int64_t ldx, const int8_t* w_down, int64_t ld_down, const float* s_down, const int8_t* w_up, int64_t ld_up,
+                     const float* s_up, void* y, int64_t ldy, int64_t T, int64_t d_in, int64_t r, int64_t d_out, int act, int dt, void* ws,
+                     size_t ws_bytes, void* stream);
+
 /* ---- measurement aid (not on the compute path) ------------------------------------------ */
 /* Between begin and end every bf16 MFMA GEMM launch the library makes, and each attention forward /
  * backward call of the block, is bracketed by two HIP events on its stream.  end waits for the last one

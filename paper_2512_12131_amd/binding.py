@@ -108,6 +108,17 @@ _SIGS = {
                             _vp]),
     "lr_attention_paged_workspace_bytes": (_sz, [C.POINTER(KvCache), _i64, _i64]),
     "lr_attention_paged_fwd": (_int, [C.POINTER(KvCache), _vp, _i64, _vp, _i64, _vp, _i64, _i64, _f32, _int, _int, _vp, _sz, _vp]),
+    "lr_kv_fork_workspace_bytes": (_sz, [_i64] * 3),
+    "lr_kv_fork": (_int, [_vp, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "lr_kv_compact_workspace_bytes": (_sz, [_i64]),
+    "lr_kv_compact": (_int, [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "lr_kv_copy": (_int, [C.POINTER(KvCache), _vp, _vp, _vp, _i64, _vp]),
+    "lr_beam_select_workspace_bytes": (_sz, [_i64] * 4),
+    "lr_beam_select": (_int, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _int, _vp, _sz, _vp]),
+    "lr_quant_rows": (_int, [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _int, _vp]),
+    "lr_matmul_q8": (_int, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _int, _vp]),
+    "lr_linear_q8_workspace_bytes": (_sz, [_i64] * 3),
+    "lr_linear_q8_fwd": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _int, _int, _vp, _sz, _vp]),
     "lr_launch_timer_begin": (_int, [_int]),
     "lr_launch_timer_end": (_int, [_vp, _int, C.POINTER(_int)]),
     "lr_gemm_tile": (_int, [_int, _int, _int, _int, _int, _int, C.POINTER(_int), C.POINTER(_int)]),
@@ -517,6 +528,85 @@ def lr_attention_paged_workspace_bytes(k_cache, page_table, T, H):
     strides = [k_cache.stride(i) if k_cache.shape[i] > 1 else hd for i in range(3)]      # (as the call: of one page, token or head any will do)
     c = KvCache(None, None, pages, page_size, Hkv, hd, *strides, None, batch, cols, page_table.stride(0) if batch > 1 else cols, None, None)
     return lib().lr_attention_paged_workspace_bytes(C.byref(c), T, H)
+
+
+# ---- pages of the cache ------------------------------------------------------------------------
+def lr_kv_fork(refs, page_size, page_table, kv_len, parent, grow, out=None, ws=None):
+    """The page tables of the sequences `parent` [n] (rows of page_table [batch, columns], which has their kv_len keys; outside it: a new sequence)
+    with room for `grow` [n] new tokens each.  refs [pages] counts every page's holders.  Returns new (refs, page_table, kv_len, (src, dst, rows),
+    missing); src, dst and rows go to lr_kv_copy before new keys are appended, missing [1] counts pages that were not there.  All int32.
+    out: what an earlier call returned, to be written again."""
+    return _native().kv_fork(refs, page_size, page_table, kv_len, parent, grow, *_outs(out, 3, 3, 1), ws)
+
+
+def lr_kv_fork_workspace_bytes(pages, n_in, n_out):
+    return lib().lr_kv_fork_workspace_bytes(pages, n_in, n_out)
+
+
+def lr_kv_compact(refs, page_table, out=None, ws=None):
+    """Moves the pages in use (refs [pages] above 0) to the front.  Returns new (refs, page_table, (src, dst), page_map, n_live): src and dst
+    [pages / 2] go to lr_kv_copy, page_map [pages] gives the new numbers (-1: free), n_live [1] their count.  All int32.  out: what an earlier call
+    returned, to be written again."""
+    return _native().kv_compact(refs, page_table, *_outs(out, 2, 2, 2), ws)
+
+
+def lr_kv_compact_workspace_bytes(pages):
+    return lib().lr_kv_compact_workspace_bytes(pages)
+
+
+def _outs(out, before, pair, behind):
+    """The tensors of a result whose entry number `before` is a tuple of `pair` of them, in a row."""
+    if out is None:
+        return [None] * (before + pair + behind)
+    if len(out) != before + 1 + behind or len(out[before]) != pair:
+        raise LrError("out: the result of an earlier call expected")
+    return [*out[:before], *out[before], *out[before + 1:]]
+
+
+def lr_kv_copy(k_cache, v_cache, src, dst, rows=None):
+    """Copies page src[i] onto page dst[i], its first rows[i] tokens (None: all), in k_cache and v_cache (as lr_kv_append takes them).  int32;
+    entries below 0 are passed over."""
+    _native().kv_copy(k_cache, v_cache, src, dst, rows)
+
+
+# ---- beam search -------------------------------------------------------------------------------
+def lr_beam_select(logits, score, n=None, done=None, done_token=0, out=None, ws=None):
+    """logits [batch * beams, V], score [batch, beams] fp32.  Returns (parent, token, score) [batch, n] (n: None = beams) of the candidates of
+    highest score, in falling order; parent is a row of logits, -1 where there is no candidate left.  done [batch, beams] int32: beams that have ended
+    go on with done_token, at their score.  out: what an earlier call returned, to be written again."""
+    return _native().beam_select(logits, score, score.shape[-1] if n is None else n, done, done_token, *((None,) * 3 if out is None else out), ws)
+
+
+def lr_beam_select_workspace_bytes(batch, beams, V, n):
+    return lib().lr_beam_select_workspace_bytes(batch, beams, V, n)
+
+
+# ---- 8-bit integers ----------------------------------------------------------------------------
+def lr_quant_rows(x, q=None, scale=None):
+    """x [T, n] as integers of 8 bits and a scale for each row: returns (q [T, n] int8 in rows that start on 16 bytes, scale [T] fp32).  Activations by
+    token, weights [out, in] by output channel."""
+    return _native().quant_rows(x, q, scale)
+
+
+def lr_matmul_q8(a, sa, b, sb, dtype=torch.bfloat16, out=None):
+    """a [M, K], b [N, K] int8 with a scale for each row (lr_quant_rows): returns out [M, N] = (sa * a) @ (sb * b).T in dtype, in rows that start on 16
+    bytes."""
+    return _native().matmul_q8(a, sa, b, sb, _dt(out) if out is not None else _code(dtype), out)
+
+
+def _code(dtype):
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise LrError(f"unsupported dtype {dtype}")
+    return LR_F32 if dtype == torch.float32 else LR_BF16
+
+
+def lr_linear_q8_workspace_bytes(T, d_in, r):
+    return lib().lr_linear_q8_workspace_bytes(T, d_in, r)
+
+
+def lr_linear_q8_fwd(x, w_down, s_down, w_up, s_up, act=LR_ACT_SILU, y=None, ws=None):
+    """Returns y [T, d_out] of a bottleneck layer whose weights w_down [r, d_in], w_up [d_out, r] and their scales are those of lr_quant_rows."""
+    return _native().linear_q8_fwd(x, w_down, s_down, w_up, s_up, act, y, ws)
 
 
 # ---- measurement aid -----------------------------------------------------------------------

@@ -1565,6 +1565,218 @@ int lr_attention_paged_fwd(const lr_kv_cache* cache, const void* q, int64_t ldq,
   return attention_paged_bf16(c, q, ldq, o, ldo, lse, T, (int)H, scale, ws, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
 }
 
+// ---- pages of the cache ----------------------------------------------------------------------------
+constexpr int64_t PAGES_MOST = (int64_t)1 << 26;
+
+static int check_lists(std::initializer_list<const void*> ps) { return check_ptrs(LR_F32, ps); }
+// a list [rows, ld] of which n columns are used: first byte and the one behind the last
+struct Span { uintptr_t lo, hi; };
+static Span span_of(const void* p, int64_t rows, int64_t ld, int64_t n) {
+  return {(uintptr_t)p, rows > 0 && n > 0 ? (uintptr_t)p + (size_t)((rows - 1) * ld + n) * 4 : (uintptr_t)p};
+}
+static bool apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span* a = outs.begin(); a != outs.end(); a++) {
+    for (const Span& b : ins)
+      if (a->lo < b.hi && b.lo < a->hi) return false;
+    for (const Span* b = outs.begin(); b != a; b++)
+      if (a->lo < b->hi && b->lo < a->hi) return false;
+  }
+  return true;
+}
+
+static int check_fork_sizes(int64_t n_pages, int64_t n_in, int64_t n_out) {
+  if (n_pages <= 0 || n_in < 0 || n_out < 0) return LR_EINVAL;
+  return n_pages > PAGES_MOST || n_in > KV_FORK_MOST || n_out > KV_FORK_MOST ? LR_EUNSUPPORTED : LR_OK;
+}
+size_t lr_kv_fork_workspace_bytes(int64_t n_pages, int64_t n_in, int64_t n_out) {
+  return check_fork_sizes(n_pages, n_in, n_out) == LR_OK ? kv_fork_ws_bytes(n_in, n_out, n_pages) : 0;
+}
+int lr_kv_fork(const int32_t* refs_in, int64_t n_pages, int64_t page_size, const int32_t* table_in, int64_t ld_in, const int32_t* len_in,
+               int64_t n_in, const int32_t* parent, const int32_t* grow, int32_t* refs_out, int32_t* table_out, int64_t ld_out,
+               int32_t* len_out, int64_t n_out, int64_t max_pages, int32_t* copy_src, int32_t* copy_dst, int32_t* copy_rows,
+               int32_t* missing, void* ws, size_t ws_bytes, void* stream) {
+  TRY(check_fork_sizes(n_pages, n_in, n_out));
+  if (page_size <= 0 || max_pages <= 0 || ld_in < max_pages || ld_out < max_pages) return LR_EINVAL;
+  if (page_size > 0x7fffffffLL || max_pages > (((int64_t)1 << 31) - 2048) / page_size || ld_in > ((int64_t)1 << 40) || ld_out > ((int64_t)1 << 40))
+    return LR_EUNSUPPORTED;
+  TRY(check_lists({refs_in, refs_out, missing}));
+  if (n_in > 0) TRY(check_lists({table_in, len_in}));
+  if (n_out > 0) TRY(check_lists({parent, grow, table_out, len_out, copy_src, copy_dst, copy_rows}));
+  const auto list = [](const void* p, int64_t n) { return span_of(p, 1, n, n); };
+  if (!apart({list(refs_out, n_pages), span_of(table_out, n_out, ld_out, max_pages), list(len_out, n_out), list(copy_src, n_out), list(copy_dst, n_out),
+              list(copy_rows, n_out), list(missing, 1)},
+             {list(refs_in, n_pages), span_of(table_in, n_in, ld_in, max_pages), list(len_in, n_in), list(parent, n_out), list(grow, n_out)}))
+    return LR_EINVAL;
+  TRY(check_ws(ws, ws_bytes, kv_fork_ws_bytes(n_in, n_out, n_pages)));
+  KvFork f{};
+  f.refs_in = refs_in; f.table_in = table_in; f.len_in = len_in; f.parent = parent; f.grow = grow;
+  f.refs_out = refs_out; f.table_out = table_out; f.len_out = len_out;
+  f.copy_src = copy_src; f.copy_dst = copy_dst; f.copy_rows = copy_rows; f.missing = missing;
+  f.ld_in = ld_in; f.ld_out = ld_out;
+  f.n_pages = (int)n_pages; f.page_size = (int)page_size; f.n_in = (int)n_in; f.n_out = (int)n_out; f.max_pages = (int)max_pages;
+  f.by_page = FastDiv::of(page_size);
+  return k_kv_fork(f, ws, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+size_t lr_kv_compact_workspace_bytes(int64_t n_pages) { return n_pages > 0 && n_pages <= PAGES_MOST ? kv_compact_ws_bytes(n_pages) : 0; }
+int lr_kv_compact(const int32_t* refs_in, int64_t n_pages, const int32_t* table_in, int64_t ld_in, int64_t batch, int64_t max_pages, int32_t* refs_out,
+                  int32_t* table_out, int64_t ld_out, int32_t* copy_src, int32_t* copy_dst, int32_t* page_map, int32_t* n_live, void* ws,
+                  size_t ws_bytes, void* stream) {
+  if (n_pages <= 0 || batch < 0 || max_pages <= 0 || ld_in < max_pages || ld_out < max_pages) return LR_EINVAL;
+  if (n_pages > PAGES_MOST || batch > (1 << 16) || max_pages > 0x7fffffffLL || ld_in > ((int64_t)1 << 40) || ld_out > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  TRY(check_lists({refs_in, refs_out, page_map, n_live}));
+  if (n_pages > 1) TRY(check_lists({copy_src, copy_dst}));
+  if (batch > 0) TRY(check_lists({table_in, table_out}));
+  const auto list = [](const void* p, int64_t n) { return span_of(p, 1, n, n); };
+  if (!apart({list(refs_out, n_pages), span_of(table_out, batch, ld_out, max_pages), list(copy_src, n_pages / 2), list(copy_dst, n_pages / 2),
+              list(page_map, n_pages), list(n_live, 1)},
+             {list(refs_in, n_pages), span_of(table_in, batch, ld_in, max_pages)}))
+    return LR_EINVAL;
+  TRY(check_ws(ws, ws_bytes, kv_compact_ws_bytes(n_pages)));
+  KvCompact c{};
+  c.refs_in = refs_in; c.table_in = table_in; c.refs_out = refs_out; c.table_out = table_out;
+  c.copy_src = copy_src; c.copy_dst = copy_dst; c.page_map = page_map; c.n_live = n_live;
+  c.ld_in = ld_in; c.ld_out = ld_out; c.n_pages = n_pages; c.max_pages = max_pages; c.batch = (int)batch;
+  return k_kv_compact(c, ws, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+int lr_kv_copy(const lr_kv_cache* cache, const int32_t* src, const int32_t* dst, const int32_t* rows, int64_t n, void* stream) {
+  if (!cache || n < 0) return LR_EINVAL;
+  lr_kv_cache pages = *cache;      // (without its lists)
+  pages.page_table = pages.cu_q = pages.kv_len = nullptr;
+  pages.batch = 0;
+  pages.max_pages = pages.table_ld = 1;
+  KvCache c;
+  TRY(check_cache(&pages, false, &c));
+  TRY(check_ptrs(LR_BF16, {c.k, c.v}));
+  const int64_t head_vecs = c.head_dim / 8, row_vecs = c.n_kv_heads * head_vecs;
+  if (row_vecs > (((int64_t)1 << 31) - 4096) / c.page_size || n > ((int64_t)1 << 31)) return LR_EUNSUPPORTED;
+  if (n == 0) return LR_OK;
+  TRY(check_lists({src, dst}));
+  if ((uintptr_t)rows & 3) return LR_EALIGN;
+  KvCopy p{};
+  p.k = c.k; p.v = c.v; p.page_stride = c.page_stride; p.token_stride = c.token_stride; p.head_stride = c.head_stride;
+  p.n_pages = c.n_pages; p.page_size = c.page_size; p.row_vecs = (int)row_vecs; p.head_vecs = (int)head_vecs;
+  p.by_row = FastDiv::of(row_vecs); p.by_head = FastDiv::of(head_vecs);
+  p.src = src; p.dst = dst; p.rows = rows; p.n = n;
+  return k_kv_copy(p, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+// ---- candidates of highest score -------------------------------------------------------------------
+static int check_select_sizes(int64_t batch, int64_t beams, int64_t V, int64_t n) {
+  if (batch < 0 || beams <= 0 || V <= 0 || n <= 0) return LR_EINVAL;
+  return beams > BEAM_MOST || n > BEAM_MOST || V > (1 << 20) || batch > (1 << 20) / beams ? LR_EUNSUPPORTED : LR_OK;
+}
+size_t lr_beam_select_workspace_bytes(int64_t batch, int64_t beams, int64_t V, int64_t n) {
+  return check_select_sizes(batch, beams, V, n) == LR_OK ? beam_select_ws_bytes(batch * beams, V, n) : 0;
+}
+int lr_beam_select(const void* logits, int64_t ldl, const float* score, const int32_t* done, int64_t done_token, int32_t* parent, int32_t* token,
+                   float* score_out, int64_t batch, int64_t beams, int64_t V, int64_t n, int dt, void* ws, size_t ws_bytes, void* stream) {
+  TRY(check_dt(dt));
+  TRY(check_select_sizes(batch, beams, V, n));
+  if (ldl < V || (done && (done_token < 0 || done_token >= V))) return LR_EINVAL;
+  if (ldl > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  if (batch == 0) return LR_OK;
+  if (!logits) return LR_EINVAL;
+  if ((uintptr_t)logits & (dt == LR_BF16 ? 1 : 3)) return LR_EALIGN;
+  TRY(check_lists({score, parent, token, score_out}));
+  if ((uintptr_t)done & 3) return LR_EALIGN;
+  TRY(check_ws(ws, ws_bytes, beam_select_ws_bytes(batch * beams, V, n)));
+  BeamSelect s{};
+  s.logits = logits; s.ld = ldl; s.score = score; s.done = done; s.done_token = (int)done_token;
+  s.rows = (int)(batch * beams); s.beams = (int)beams; s.V = (int)V; s.n = (int)n;
+  s.parent = parent; s.token = token; s.score_out = score_out;
+  return k_beam_select(s, dt, ws, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+// ---- products of 8-bit integers --------------------------------------------------------------------
+constexpr int64_t Q8_K_MOST = 133144, Q8_LD_MOST = (int64_t)1 << 22;
+
+static int check_quant(const void* x, int64_t ldx, int64_t T, int64_t n, int dt) {
+  TRY(check_dt(dt));
+  if (T < 0 || T > 0x7fffffffLL || n <= 0 || n > 0x7fffffffLL || ldx < n) return LR_EINVAL;
+  if (ldx > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  TRY(check_dims_bf16(dt, {n, ldx}));
+  return T > 0 ? check_ptrs(dt, {x}) : LR_OK;
+}
+int lr_quant_rows(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t T, int64_t n, int dt, void* stream) {
+  TRY(check_quant(x, ldx, T, n, dt));
+  if (ldq < n) return LR_EINVAL;
+  if (ldq % 16) return LR_EALIGN;
+  if (ldq > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  if (T == 0) return LR_OK;
+  TRY(check_ptrs(LR_BF16, {q})); TRY(check_lists({scale}));
+  return k_quant_rows(x, ldx, q, ldq, scale, T, n, LR_ACT_IDENTITY, dt, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+// an operand [rows, ld] of integers with a scale for each row
+static int check_q8(const int8_t* p, int64_t ld, const float* s, int64_t K) {
+  if (ld < K) return LR_EINVAL;
+  if (ld % 16) return LR_EALIGN;
+  if (ld > Q8_LD_MOST) return LR_EUNSUPPORTED;
+  TRY(check_ptrs(LR_BF16, {p}));
+  return check_lists({s});
+}
+static int check_q8_out(const void* c, int64_t ldc, int64_t N, int dt) {
+  if (ldc < N) return LR_EINVAL;
+  if (ldc % (dt == LR_BF16 ? 8 : 4)) return LR_EALIGN;
+  if (ldc > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  return check_ptrs(LR_BF16, {c});
+}
+int lr_matmul_q8(const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb, void* c, int64_t ldc, int64_t M,
+                 int64_t N, int64_t K, int dt, void* stream) {
+  TRY(check_dt(dt));
+  if (M < 0 || M > 0x7fffffffLL - 255 || N <= 0 || N > 0x7fffffffLL - 255 || K <= 0) return LR_EINVAL;
+  if (K > Q8_K_MOST || M * N > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  if (M == 0) return LR_OK;
+  TRY(check_q8(a, lda, sa, K)); TRY(check_q8(b, ldb, sb, K)); TRY(check_q8_out(c, ldc, N, dt));
+  const Q8Op op{a, b, sa, sb, c, lda, ldb, ldc, (int)M, (int)N, (int)K, dt};
+  return gemm_q8(op, (hipStream_t)stream) == hipSuccess ? LR_OK : LR_ELAUNCH;
+}
+
+namespace {
+struct LinearQ8 {
+  int8_t *qx, *qa;
+  float *sx, *sz, *z;
+  int64_t ldx, ldz;
+};
+LinearQ8 linear_q8_parts(Ctx& c, int64_t T, int64_t d_in, int64_t r) {
+  LinearQ8 p{};
+  p.ldx = rup(d_in, 16); p.ldz = rup(r, 16);
+  p.qx = (int8_t*)c.take((size_t)T * p.ldx);
+  p.sx = (float*)c.take((size_t)T * sizeof(float));
+  p.z = (float*)c.take((size_t)T * p.ldz * sizeof(float));
+  p.qa = (int8_t*)c.take((size_t)T * p.ldz);
+  p.sz = (float*)c.take((size_t)T * sizeof(float));
+  return p;
+}
+}  // namespace
+size_t lr_linear_q8_workspace_bytes(int64_t T, int64_t d_in, int64_t r) {
+  if (T <= 0 || T > 0x7fffffffLL || d_in <= 0 || d_in > Q8_K_MOST || r <= 0 || r > Q8_K_MOST) return 0;
+  Ctx c; c.dry = true;
+  linear_q8_parts(c, T, d_in, r);
+  return c.peak;
+}
+int lr_linear_q8_fwd(const void* x, int64_t ldx, const int8_t* w_down, int64_t ld_down, const float* s_down, const int8_t* w_up, int64_t ld_up,
+                     const float* s_up, void* y, int64_t ldy, int64_t T, int64_t d_in, int64_t r, int64_t d_out, int act, int dt, void* ws,
+                     size_t ws_bytes, void* stream) {
+  TRY(check_act(act));
+  TRY(check_quant(x, ldx, T, d_in, dt));
+  if (r <= 0 || d_out <= 0 || d_out > 0x7fffffffLL - 255 || T > 0x7fffffffLL - 255) return LR_EINVAL;
+  TRY(check_dims_bf16(dt, {r, d_out}));
+  if (d_in > Q8_K_MOST || r > Q8_K_MOST || T * d_out > ((int64_t)1 << 40) || T * r > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  if (T == 0) return LR_OK;
+  TRY(check_q8(w_down, ld_down, s_down, d_in)); TRY(check_q8(w_up, ld_up, s_up, r)); TRY(check_q8_out(y, ldy, d_out, dt));
+  TRY(check_ws(ws, ws_bytes, lr_linear_q8_workspace_bytes(T, d_in, r)));
+  Ctx c; c.base = (char*)ws; c.cap = ws_bytes; c.st = (hipStream_t)stream;
+  const LinearQ8 p = linear_q8_parts(c, T, d_in, r);
+  LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));
+  LAUNCH(c, gemm_q8(Q8Op{p.qx, w_down, p.sx, s_down, p.z, p.ldx, ld_down, p.ldz, (int)T, (int)r, (int)d_in, LR_F32}, c.st));
+  LAUNCH(c, k_quant_rows(p.z, p.ldz, p.qa, p.ldz, p.sz, T, r, act, LR_F32, c.st));
+  LAUNCH(c, gemm_q8(Q8Op{p.qa, w_up, p.sz, s_up, y, p.ldz, ld_up, ldy, (int)T, (int)d_out, (int)r, dt}, c.st));
+  return status_of(c);
+}
+
 // ---- measurement aid ---------------------------------------------------------------------------
 int lr_launch_timer_begin(int max_launches) { return launch_timer_begin(max_launches) == 0 ? LR_OK : LR_EINVAL; }
 int lr_launch_timer_end(lr_launch_record* records, int max_records, int* n_records) {

@@ -250,6 +250,70 @@ size_t attention_paged_ws_bytes(int64_t T, int H, int Hkv, int batch, int64_t ca
 hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, void* o, int64_t ldo, float* lse, int64_t T, int H, float scale,
                                 void* ws, hipStream_t);
 
+// ---- pages of the cache (kv_pages.hip) -------------------------------------------------------------
+constexpr int KV_FORK_MOST = 1 << 14;      // sequences, old or new (two words of LDS for each)
+struct KvFork {
+  const int32_t *refs_in, *table_in, *len_in, *parent, *grow;
+  int32_t *refs_out, *table_out, *len_out, *copy_src, *copy_dst, *copy_rows, *missing;
+  int64_t ld_in, ld_out;
+  int n_pages, page_size, n_in, n_out, max_pages;
+  FastDiv by_page;
+  int32_t *found, *first, *count, *flags, *offset, *fresh;      // in the workspace
+};
+size_t kv_fork_ws_bytes(int64_t n_in, int64_t n_out, int64_t n_pages);
+hipError_t k_kv_fork(KvFork f, void* ws, hipStream_t st);
+struct KvCompact {
+  const int32_t *refs_in, *table_in;
+  int32_t *refs_out, *table_out, *copy_src, *copy_dst, *page_map, *n_live;
+  int64_t ld_in, ld_out, n_pages, max_pages;
+  int batch;
+  int spans;
+  int32_t *turn, *span_held;                                    // in the workspace
+};
+size_t kv_compact_ws_bytes(int64_t n_pages);
+hipError_t k_kv_compact(KvCompact c, void* ws, hipStream_t st);
+struct KvCopy {
+  uint16_t *k, *v;
+  int64_t page_stride, token_stride, head_stride;
+  int n_pages, page_size, row_vecs, head_vecs;                  // vectors of 8 elements of a token, of one of its heads
+  FastDiv by_row, by_head;
+  const int32_t *src, *dst, *rows;
+  int64_t n;
+  int runs;
+};
+hipError_t k_kv_copy(KvCopy c, hipStream_t st);
+
+// ---- candidates of highest score (beam_select.hip) -------------------------------------------------
+constexpr int BEAM_MOST = 64;              // beams of a prompt, and candidates
+struct BeamSelect {
+  const void* logits;
+  int64_t ld;
+  const float* score;
+  const int32_t* done;
+  int done_token, rows, beams, V, n;
+  int32_t *parent, *token;
+  float* score_out;
+  int parts, run;                          // runs of a row, logits of each
+  double* part_sum;                        // in the workspace
+  uint2* part_key;
+  float* part_ref;
+};
+size_t beam_select_ws_bytes(int64_t rows, int64_t V, int64_t n);
+hipError_t k_beam_select(BeamSelect s, int dt, void* ws, hipStream_t st);
+
+// ---- 8-bit integers (quant_q8.hip, gemm_q8.hip) ----------------------------------------------------
+// rows of x (act applied first) as integers and scales
+hipError_t k_quant_rows(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t T, int64_t n, int act, int dt, hipStream_t);
+// C[m, n] = sa[m] sb[n] sum_k A[m, k] B[n, k], rounded to dt
+struct Q8Op {
+  const int8_t *A, *B;
+  const float *sa, *sb;
+  void* C;
+  int64_t lda, ldb, ldc;
+  int M, N, K, dt;
+};
+hipError_t gemm_q8(const Q8Op& op, hipStream_t st);
+
 // ---- attention (attention.hip) ---------------------------------------------------------------
 hipError_t attention_fwd_bf16(const void* q, const void* k, const void* v, void* o, float* lse, int64_t ld,
                               int B, int S, int H, int hd, int causal, hipStream_t);

@@ -1,0 +1,386 @@
+// Pages of a key / value cache: who holds them (fork), where they lie (compact), and their copies.
+//
+// A page's count says how many entries of page tables hold it (and whoever else does); pages of count 0 are free.  Fork and compact
+// read the old lists and write new ones, so that a step that finds too few pages can be taken back.  Fresh pages are the lowest free
+// ones, given to the sequences in order: sums of whole numbers and prefix counts, so the same lists give the same result.
+#include "common.h"
+
+namespace lrb {
+namespace {
+
+__device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+}
+
+// Sum of v over the workgroup's threads before this one, and over all of them.  scratch: one entry per wavefront, free again after the call.
+template <class V>
+__device__ __forceinline__ V block_prefix(V v, V* scratch, V* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  V incl = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const V o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 63) scratch[wave] = incl;
+  __syncthreads();
+  V before = 0, all = 0;
+  for (int w = 0; w < nw; w++) {
+    if (w < wave) before += scratch[w];
+    all += scratch[w];
+  }
+  __syncthreads();
+  *total = all;
+  return before + incl - v;
+}
+
+constexpr int PLAN_T = 1024;      // threads of the planning workgroup
+constexpr int PLAN_PER = 8;       // counts per thread and step of its search for free pages
+
+// What the new sequence i is made of.
+struct Child {
+  int parent;                // -1: none
+  int64_t old, now;          // keys so far, with the new ones
+  int full, part;            // whole pages of the keys so far, keys behind them
+};
+__device__ __forceinline__ Child child_of(const KvFork& f, int i) {
+  Child c;
+  const int p = f.parent[i];
+  c.parent = p >= 0 && p < f.n_in ? p : -1;
+  c.old = c.parent >= 0 ? max(f.len_in[c.parent], 0) : 0;
+  c.now = c.old + max(f.grow[i], 0);
+  c.full = (int)f.by_page.div((uint32_t)c.old);
+  c.part = (int)c.old - c.full * f.page_size;
+  return c;
+}
+__device__ __forceinline__ bool is_page(const KvFork& f, int e) { return (uint32_t)e < (uint32_t)f.n_pages; }
+
+// Workgroup 0 plans: the first child of every parent, how many fresh pages each child takes, and the first so many free ones.  The
+// others copy the counts, which the second launch moves on.
+//
+// Bound: latency, of the lists that lead to each other and of the search through the counts: PLAN_T * PLAN_PER of them per step of
+// about a microsecond, no further than needed.
+__global__ __launch_bounds__(PLAN_T) void fork_plan_kernel(KvFork f) {
+  const int tid = threadIdx.x;
+  if (blockIdx.x > 0) {
+    for (int64_t i = (int64_t)(blockIdx.x - 1) * PLAN_T + tid; i < f.n_pages; i += (int64_t)(gridDim.x - 1) * PLAN_T) f.refs_out[i] = f.refs_in[i];
+    return;
+  }
+  extern __shared__ int first[];          // [n_in] the first child of a parent, then [n_in] its children
+  __shared__ int64_t scratch[PLAN_T / 64];
+  int* count = first + f.n_in;
+  for (int p = tid; p < f.n_in; p += PLAN_T) {
+    first[p] = 0x7fffffff;
+    count[p] = 0;
+  }
+  __syncthreads();
+  for (int i = tid; i < f.n_out; i += PLAN_T) {
+    const int p = f.parent[i];
+    if (p >= 0 && p < f.n_in) {
+      atomicMin(&first[p], i);
+      atomicAdd(&count[p], 1);
+    }
+  }
+  __syncthreads();
+  int64_t want = 0, beyond = 0;           // fresh pages so far; pages that no column of the table is left for
+  for (int i0 = 0; i0 < f.n_out; i0 += PLAN_T) {
+    const int i = i0 + tid;
+    int64_t need = 0, over = 0;
+    if (i < f.n_out) {
+      const Child c = child_of(f, i);
+      const int last = (int)min((c.now + f.page_size - 1) / f.page_size, (int64_t)f.max_pages);      // columns with keys
+      over = (c.now + f.page_size - 1) / f.page_size - last;
+      const bool heir = c.parent >= 0 && first[c.parent] == i;
+      int flags = heir ? 1 : 0;
+      need = max(last - c.full, 0);
+      if (heir) {
+        const int32_t* row = f.table_in + (int64_t)c.parent * f.ld_in;
+        // the half filled page stays where nobody else holds it
+        if (c.part > 0 && c.full < f.max_pages) {
+          const int e = row[c.full];
+          if (is_page(f, e) && f.refs_in[e] == 1) {
+            flags |= 2;
+            need--;
+          }
+        }
+#pragma unroll 8
+        for (int col = c.full + (c.part > 0 ? 1 : 0); col < last; col++) need -= is_page(f, row[col]) ? 1 : 0;
+      }
+      f.flags[i] = flags;
+    }
+    int64_t all;
+    const int64_t at = want + block_prefix(need, scratch, &all);
+    if (i < f.n_out) f.offset[i] = (int)min(at, (int64_t)f.n_pages);
+    want += all;
+    block_prefix(over, scratch, &all);
+    beyond += all;
+  }
+  for (int p = tid; p < f.n_in; p += PLAN_T) {
+    f.first[p] = first[p];
+    f.count[p] = count[p];
+  }
+  int64_t found = 0;
+  const bool vec = ((uintptr_t)f.refs_in & 15) == 0;
+  for (int64_t p0 = 0; p0 < f.n_pages && found < want; p0 += PLAN_T * PLAN_PER) {
+    const int64_t p = p0 + tid * PLAN_PER;
+    int r[PLAN_PER];
+    if (vec && p + PLAN_PER <= f.n_pages) {
+#pragma unroll
+      for (int j = 0; j < PLAN_PER; j += 4) *reinterpret_cast<int4*>(r + j) = *reinterpret_cast<const int4*>(f.refs_in + p + j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < PLAN_PER; j++) r[j] = p + j < f.n_pages ? f.refs_in[p + j] : 1;
+    }
+    int64_t mine = 0, all;
+#pragma unroll
+    for (int j = 0; j < PLAN_PER; j++) mine += r[j] == 0;
+    int64_t at = found + block_prefix(mine, scratch, &all);
+#pragma unroll
+    for (int j = 0; j < PLAN_PER; j++)
+      if (r[j] == 0 && at < f.n_pages) f.fresh[at++] = (int)(p + j);
+    found += all;
+  }
+  if (tid == 0) {
+    const int64_t lack = max(want - found, (int64_t)0) + beyond;
+    *f.found = (int)min(found, (int64_t)f.n_pages);
+    *f.missing = (int)min(lack, (int64_t)0x7fffffff);
+  }
+}
+
+// One wavefront per row: the new tables, lengths and copies, and how the old tables' pages change hands.
+__global__ __launch_bounds__(256) void fork_rows_kernel(KvFork f) {
+  const int lane = threadIdx.x & 63;
+  const int row = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row < f.n_out) {
+    const int i = row;
+    const Child c = child_of(f, i);
+    const int flags = f.flags[i], found = *f.found;
+    const bool heir = flags & 1, alone = flags & 2;
+    const int32_t* in = f.table_in + (int64_t)max(c.parent, 0) * f.ld_in;
+    int32_t* out = f.table_out + (int64_t)i * f.ld_out;
+    int at = f.offset[i];
+    bool copied = false;
+    for (int c0 = 0; c0 < f.max_pages; c0 += 64) {
+      const int col = c0 + lane;
+      const int e = c.parent >= 0 && col < f.max_pages ? in[col] : -1;
+      const bool page = is_page(f, e), half = col == c.full && c.part > 0 && page;
+      const bool keep = page && (col < c.full || (heir && (!half || alone)));
+      const bool take = col < f.max_pages && col >= c.full && !keep && (int64_t)col * f.page_size < c.now;
+      const uint64_t takers = __ballot(take);
+      const int slot = at + lanes_below(takers);
+      at += __popcll(takers);
+      const int got = take && slot < found ? f.fresh[slot] : -1;
+      if (col < f.max_pages) out[col] = keep ? e : got;
+      if (got >= 0) f.refs_out[got] = 1;
+      const bool copy = half && got >= 0;
+      if (copy) {
+        f.copy_src[i] = e;
+        f.copy_dst[i] = got;
+        f.copy_rows[i] = c.part;
+      }
+      copied |= __ballot(copy) != 0;
+    }
+    if (lane == 0) {
+      if (!copied) {
+        f.copy_src[i] = f.copy_dst[i] = -1;
+        f.copy_rows[i] = 0;
+      }
+      f.len_out[i] = (int)min(c.now, (int64_t)0x7fffffff);
+    }
+    return;
+  }
+  const int p = row - f.n_out;
+  if (p >= f.n_in) return;
+  const int children = f.count[p];
+  const bool alone = children > 0 && (f.flags[f.first[p]] & 2);
+  const uint32_t old = (uint32_t)max(f.len_in[p], 0);
+  const int full = (int)f.by_page.div(old), part = (int)old - full * f.page_size;
+  const int32_t* in = f.table_in + (int64_t)p * f.ld_in;
+  for (int col = lane; col < f.max_pages; col += 64) {
+    const int e = in[col];
+    if (!is_page(f, e)) continue;
+    // whole pages go to every child, the half filled one to an heir that nobody else shares it with, those behind to the heir
+    const int by = col < full ? children - 1 : children == 0 || (col == full && part > 0 && !alone) ? -1 : 0;
+    if (by != 0) atomicAdd(&f.refs_out[e], by);
+  }
+}
+
+constexpr int SPAN_T = 256, SPAN_PER = 8, SPAN = SPAN_T * SPAN_PER;   // pages of a workgroup
+
+__device__ __forceinline__ int held_mask(const KvCompact& c, int64_t p) {      // of SPAN_PER pages from p
+  int m = 0;
+#pragma unroll
+  for (int j = 0; j < SPAN_PER; j++) m |= (p + j < c.n_pages && c.refs_in[p + j] > 0) << j;
+  return m;
+}
+
+// Pages held of every span.
+__global__ __launch_bounds__(SPAN_T) void compact_count_kernel(KvCompact c) {
+  __shared__ int scratch[SPAN_T / 64];
+  int all;
+  block_prefix<int>(__popc(held_mask(c, (int64_t)blockIdx.x * SPAN + threadIdx.x * SPAN_PER)), scratch, &all);
+  if (threadIdx.x == 0) c.span_held[blockIdx.x] = all;
+}
+
+// With H the number of held pages: the j-th held page from H on moves into the j-th free one below H.  A page p below H has p - (held
+// pages before it) free ones before it, one from H on (held pages before it) - (held pages below H) movers.
+__global__ __launch_bounds__(SPAN_T) void compact_lists_kernel(KvCompact c) {
+  __shared__ int scratch[SPAN_T / 64];
+  __shared__ int sums[2];
+  int before = 0, held = 0, low = 0;             // held pages: of the spans before this one, of all, of the spans below that of page H
+  for (int s = threadIdx.x; s < c.spans; s += SPAN_T) {
+    const int n = c.span_held[s];
+    held += n;
+    if (s < (int)blockIdx.x) before += n;
+  }
+  int all;
+  block_prefix(held, scratch, &all);
+  held = all;
+  block_prefix(before, scratch, &all);
+  before = all;
+  const int cut = held / SPAN;                   // (held == n_pages: a span behind the last)
+  for (int s = threadIdx.x; s < min(cut, c.spans); s += SPAN_T) low += c.span_held[s];
+  block_prefix(low, scratch, &all);
+  low = all;
+  {
+    const int64_t p = (int64_t)cut * SPAN + threadIdx.x * SPAN_PER;
+    int m = held_mask(c, p);
+    const int64_t n = held - p;                  // of this thread's pages, those below H
+    m = n <= 0 ? 0 : n >= SPAN_PER ? m : m & ((1 << n) - 1);
+    block_prefix<int>(__popc(m), scratch, &all);
+    low += all;
+  }
+  const int moves = held - low, room = (int)(c.n_pages / 2);
+  const int64_t p = (int64_t)blockIdx.x * SPAN + threadIdx.x * SPAN_PER;
+  const int m = held_mask(c, p);
+  int rank = before + block_prefix<int>(__popc(m), scratch, &all);
+#pragma unroll
+  for (int j = 0; j < SPAN_PER; j++) {
+    const int64_t page = p + j;
+    if (page >= c.n_pages) break;
+    const bool is = (m >> j) & 1;
+    int to = -1;
+    if (page < held) {
+      if (is) to = (int)page;
+      else if ((int)page - rank < room) c.copy_dst[(int)page - rank] = (int)page;
+    } else if (is && rank - low < room) {
+      c.copy_src[rank - low] = (int)page;
+      to = -2 - (rank - low);                    // the third launch puts the page there
+    }
+    c.turn[page] = to;
+    rank += is;
+  }
+  for (int64_t j = (int64_t)blockIdx.x * SPAN_T + threadIdx.x; j < room; j += (int64_t)gridDim.x * SPAN_T)
+    if (j >= moves) c.copy_src[j] = c.copy_dst[j] = -1;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *c.n_live = held;
+}
+
+// The pages' new numbers, in the map, the counts and the table.
+__global__ __launch_bounds__(256) void compact_apply_kernel(KvCompact c) {
+  const int64_t cells = (int64_t)c.batch * c.max_pages, total = c.n_pages + cells;
+  const int held = *c.n_live;
+  for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < total; k += (int64_t)gridDim.x * 256) {
+    if (k < c.n_pages) {
+      const int t = c.turn[k], to = t <= -2 ? c.copy_dst[-2 - t] : t;
+      c.page_map[k] = to;
+      if (to >= 0) c.refs_out[to] = c.refs_in[k];
+      if (k >= held) c.refs_out[k] = 0;          // (below it every page is somebody's new place)
+    } else {
+      const int64_t row = (k - c.n_pages) / c.max_pages, col = (k - c.n_pages) % c.max_pages;
+      const int e = c.table_in[row * c.ld_in + col];
+      int to = -1;
+      if ((uint32_t)e < (uint32_t)c.n_pages) {
+        const int t = c.turn[e];
+        to = t <= -2 ? c.copy_dst[-2 - t] : t;
+      }
+      c.table_out[row * c.ld_out + col] = to;
+    }
+  }
+}
+
+// The first rows[i] tokens (NULL: all) of page src[i] onto page dst[i], keys and values.
+//
+// Bound: HBM.  A workgroup takes 8 KB of keys or values of a pair at a time, two 16-byte vectors per lane, in the order token, head, column.
+constexpr int COPY_PER = 2, COPY_RUN = 256 * COPY_PER;
+__global__ __launch_bounds__(256) void kv_copy_kernel(KvCopy c) {
+  const int64_t items = c.n * 2 * c.runs;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int64_t pair = it / (2 * c.runs);
+    const int part = (int)(it - pair * 2 * c.runs);
+    const int src = c.src[pair], dst = c.dst[pair];
+    if ((uint32_t)src >= (uint32_t)c.n_pages || (uint32_t)dst >= (uint32_t)c.n_pages || src == dst) continue;
+    const int rows = c.rows ? min(max(c.rows[pair], 0), c.page_size) : c.page_size;
+    const int end = rows * c.row_vecs;
+    const int run = part >> 1;
+    uint16_t* base = (part & 1) ? c.v : c.k;
+    const uint16_t* from = base + (int64_t)src * c.page_stride;
+    uint16_t* to = base + (int64_t)dst * c.page_stride;
+    uint4 q[COPY_PER];
+    int64_t off[COPY_PER];
+#pragma unroll
+    for (int j = 0; j < COPY_PER; j++) {
+      const int v = run * COPY_RUN + j * 256 + threadIdx.x;
+      const int t = (int)c.by_row.div((uint32_t)v), w = v - t * c.row_vecs;
+      const int h = (int)c.by_head.div((uint32_t)w), d = w - h * c.head_vecs;
+      off[j] = v < end ? t * c.token_stride + h * c.head_stride + d * 8 : -1;
+      if (off[j] >= 0) q[j] = *reinterpret_cast<const uint4*>(from + off[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < COPY_PER; j++)
+      if (off[j] >= 0) *reinterpret_cast<uint4*>(to + off[j]) = q[j];
+  }
+}
+
+}  // namespace
+
+size_t kv_fork_ws_bytes(int64_t n_in, int64_t n_out, int64_t n_pages) {
+  return (size_t)(2 * n_in + 2 * n_out + n_pages + 1) * sizeof(int32_t);
+}
+hipError_t k_kv_fork(KvFork f, void* ws, hipStream_t st) {
+  int32_t* w = (int32_t*)ws;
+  f.found = w;
+  f.first = w + 1;
+  f.count = f.first + f.n_in;
+  f.flags = f.count + f.n_in;
+  f.offset = f.flags + f.n_out;
+  f.fresh = f.offset + f.n_out;
+  // one-time opt-in to more than 64 KB of dynamic LDS (thread-safe function-local static)
+  static const hipError_t attr_err =
+      hipFuncSetAttribute((const void*)fork_plan_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * KV_FORK_MOST * (int)sizeof(int));
+  if (attr_err != hipSuccess) return attr_err;
+  const int64_t copies = (f.n_pages + 4 * PLAN_T - 1) / (4 * PLAN_T);
+  hipLaunchKernelGGL(fork_plan_kernel, dim3((uint32_t)(1 + (copies < 255 ? copies : 255))), dim3(PLAN_T), (size_t)2 * f.n_in * sizeof(int), st, f);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int rows = f.n_in + f.n_out;
+  if (rows > 0) hipLaunchKernelGGL(fork_rows_kernel, dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, st, f);
+  return hipGetLastError();
+}
+
+size_t kv_compact_ws_bytes(int64_t n_pages) { return (size_t)(n_pages + (n_pages + SPAN - 1) / SPAN) * sizeof(int32_t); }
+hipError_t k_kv_compact(KvCompact c, void* ws, hipStream_t st) {
+  c.spans = (int)((c.n_pages + SPAN - 1) / SPAN);
+  c.turn = (int32_t*)ws;
+  c.span_held = c.turn + c.n_pages;
+  hipLaunchKernelGGL(compact_count_kernel, dim3((uint32_t)c.spans), dim3(SPAN_T), 0, st, c);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(compact_lists_kernel, dim3((uint32_t)c.spans), dim3(SPAN_T), 0, st, c);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t blocks = (c.n_pages + (int64_t)c.batch * c.max_pages + 255) / 256;
+  hipLaunchKernelGGL(compact_apply_kernel, dim3((uint32_t)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st, c);
+  return hipGetLastError();
+}
+
+hipError_t k_kv_copy(KvCopy c, hipStream_t st) {
+  if (c.n == 0) return hipSuccess;
+  const int64_t vecs = (int64_t)c.page_size * c.row_vecs;
+  c.runs = (int)((vecs + COPY_RUN - 1) / COPY_RUN);
+  const int64_t items = c.n * 2 * c.runs;
+  hipLaunchKernelGGL(kv_copy_kernel, dim3((uint32_t)(items < (1 << 20) ? items : (1 << 20))), dim3(256), 0, st, c);
+  return hipGetLastError();
+}
+
+}  // namespace lrb

@@ -393,24 +393,31 @@ PyObject* rope_at(Args& a) {
   return wrap(out);
 }
 
+// pages and strides of k, v [pages, page size, heads, hd]
+lr_kv_cache pages_of(const at::Tensor& k, const at::Tensor& v) {
+  if (k.dim() != 4 || v.sizes() != k.sizes()) fail(PyExc_ValueError, "unexpected shape of the cache");
+  if (k.scalar_type() != at::kBFloat16 || v.scalar_type() != at::kBFloat16) fail(g_lr_error, "a bf16 cache expected");
+  bool alike = k.stride(3) == 1 && v.stride(3) == 1;
+  for (int i = 0; i < 3; i++) alike &= k.size(i) <= 1 || v.stride(i) == k.stride(i);
+  if (!alike) fail(PyExc_AssertionError, "caches with the same strides and contiguous heads expected");
+  lr_kv_cache c = {};
+  c.k = ptr(k); c.v = ptr(v);
+  c.n_pages = k.size(0); c.page_size = k.size(1); c.n_kv_heads = k.size(2); c.head_dim = k.size(3);
+  const auto stride = [&](int i) { return k.size(i) > 1 ? k.stride(i) : c.head_dim; };      // (of one page, token or head any will do)
+  c.page_stride = stride(0); c.token_stride = stride(1); c.head_stride = stride(2);
+  return c;
+}
+
 // k, v [pages, page size, heads, hd], page_table [batch, columns], cu_q [batch + 1], kv_len [batch]
 struct CacheTensors {
   const at::Tensor &k, &v, &table, &cu, &len;
   explicit CacheTensors(Args& a) : k(a.tensor()), v(a.tensor()), table(a.tensor()), cu(a.tensor()), len(a.tensor()) {}
   lr_kv_cache view() const {
-    if (k.dim() != 4 || v.sizes() != k.sizes() || table.dim() != 2) fail(PyExc_ValueError, "unexpected shape of the cache or its page table");
-    if (k.scalar_type() != at::kBFloat16 || v.scalar_type() != at::kBFloat16) fail(g_lr_error, "a bf16 cache expected");
-    bool alike = k.stride(3) == 1 && v.stride(3) == 1;
-    for (int i = 0; i < 3; i++) alike &= k.size(i) <= 1 || v.stride(i) == k.stride(i);
-    if (!alike) fail(PyExc_AssertionError, "caches with the same strides and contiguous heads expected");
+    if (table.dim() != 2) fail(PyExc_ValueError, "unexpected shape of the page table");
+    lr_kv_cache c = pages_of(k, v);
     if (table.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
     if (table.size(1) > 1 && table.stride(1) != 1) fail(PyExc_AssertionError, "row-major page table expected");
     const int64_t batch = table.size(0), cols = table.size(1);
-    lr_kv_cache c;
-    c.k = ptr(k); c.v = ptr(v);
-    c.n_pages = k.size(0); c.page_size = k.size(1); c.n_kv_heads = k.size(2); c.head_dim = k.size(3);
-    const auto stride = [&](int i) { return k.size(i) > 1 ? k.stride(i) : c.head_dim; };      // (of one page, token or head any will do)
-    c.page_stride = stride(0); c.token_stride = stride(1); c.head_stride = stride(2);
     c.page_table = (const int32_t*)ptr(table);
     c.batch = batch; c.max_pages = cols;
     c.table_ld = batch > 1 ? table.stride(0) : cols;
@@ -475,6 +482,210 @@ PyObject* attention_paged_fwd(Args& a) {
   return tuple(o, lse);
 }
 
+// ---- pages of the cache ----------------------------------------------------------------------
+at::Tensor fresh32(at::IntArrayRef sizes, const at::Tensor& like) { return fresh(sizes, at::kInt, like); }
+// a page table [rows, columns]: its row stride (of a single row any will do)
+int64_t table_stride(const at::Tensor& t) {
+  if (t.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
+  if (t.dim() != 2) fail(PyExc_ValueError, "unexpected number of dimensions");
+  if (t.size(0) > 0 && t.size(1) > 1 && t.stride(1) != 1) fail(PyExc_AssertionError, "row-major page table expected");
+  return t.size(0) > 1 ? t.stride(0) : t.size(1);
+}
+int32_t* written(const at::Tensor& t, int64_t n) { return (int32_t*)indices(t, n); }
+// a result that holds a tuple
+PyObject* nested(std::initializer_list<const at::Tensor*> before, std::initializer_list<const at::Tensor*> inner, std::initializer_list<const at::Tensor*> behind) {
+  PyObject* out = PyTuple_New(before.size() + 1 + behind.size());
+  PyObject* in = PyTuple_New(inner.size());
+  bool ok = out && in;
+  Py_ssize_t i = 0, j = 0;
+  const auto put = [&](PyObject* to, Py_ssize_t at, const at::Tensor* t) {
+    PyObject* o = ok ? THPVariable_Wrap(*t) : nullptr;
+    ok = o != nullptr;
+    if (ok) PyTuple_SET_ITEM(to, at, o);
+  };
+  for (const at::Tensor* t : before) put(out, i++, t);
+  for (const at::Tensor* t : inner) put(in, j++, t);
+  if (ok) {
+    PyTuple_SET_ITEM(out, i++, in);
+    in = nullptr;
+  }
+  for (const at::Tensor* t : behind) put(out, i++, t);
+  if (ok) return out;
+  Py_XDECREF(in);
+  Py_XDECREF(out);
+  throw PyError{};
+}
+
+PyObject* kv_fork(Args& a) {
+  const at::Tensor& refs = a.tensor();
+  const int64_t page = a.integer();
+  const at::Tensor &table = a.tensor(), &len = a.tensor(), &parent = a.tensor(), &grow = a.tensor();
+  at::Tensor refs_out = a.optional(), table_out = a.optional(), len_out = a.optional(), src = a.optional(), dst = a.optional(), rows = a.optional(),
+             missing = a.optional(), ws = a.optional();
+  const int64_t pages = rows_of(refs, 1), ld = table_stride(table), n_in = table.size(0), cols = table.size(1), n = rows_of(parent, 1);
+  const int32_t *pr = indices(refs, pages), *pl = indices(len, n_in), *pp = indices(parent, n), *pg = indices(grow, n), *pt = (const int32_t*)ptr(table);
+  if (!refs_out.defined()) refs_out = fresh32({pages}, refs);
+  if (!table_out.defined()) table_out = fresh32({n, cols}, refs);
+  for (at::Tensor* t : {&len_out, &src, &dst, &rows})
+    if (!t->defined()) *t = fresh32({n}, refs);
+  if (!missing.defined()) missing = fresh32({1}, refs);
+  const int64_t ldo = table_stride(table_out);
+  if (table_out.size(0) != n || table_out.size(1) != cols) fail(PyExc_ValueError, "unexpected shape of the new page table");
+  int32_t *qr = written(refs_out, pages), *ql = written(len_out, n), *qs = written(src, n), *qd = written(dst, n), *qw = written(rows, n),
+          *qm = written(missing, 1), *qt = (int32_t*)ptr(table_out);
+  on_current_device({&refs, &table, &len, &parent, &grow, &refs_out, &table_out, &len_out, &src, &dst, &rows, &missing, &ws});
+  if (!ws.defined()) ws = workspace(lr_kv_fork_workspace_bytes(pages, n_in, n), refs);
+  const size_t nb = ws.numel() * ws.element_size();
+  void *pw = dense(ws), *st = stream();
+  call("lr_kv_fork", [&] { return lr_kv_fork(pr, pages, page, pt, ld, pl, n_in, pp, pg, qr, qt, ldo, ql, n, cols, qs, qd, qw, qm, pw, nb, st); });
+  return nested({&refs_out, &table_out, &len_out}, {&src, &dst, &rows}, {&missing});
+}
+
+PyObject* kv_compact(Args& a) {
+  const at::Tensor &refs = a.tensor(), &table = a.tensor();
+  at::Tensor refs_out = a.optional(), table_out = a.optional(), src = a.optional(), dst = a.optional(), map = a.optional(), live = a.optional(),
+             ws = a.optional();
+  const int64_t pages = rows_of(refs, 1), ld = table_stride(table), batch = table.size(0), cols = table.size(1);
+  const int32_t *pr = indices(refs, pages), *pt = (const int32_t*)ptr(table);
+  if (!refs_out.defined()) refs_out = fresh32({pages}, refs);
+  if (!table_out.defined()) table_out = fresh32({batch, cols}, refs);
+  for (at::Tensor* t : {&src, &dst})
+    if (!t->defined()) *t = fresh32({pages / 2}, refs);
+  if (!map.defined()) map = fresh32({pages}, refs);
+  if (!live.defined()) live = fresh32({1}, refs);
+  const int64_t ldo = table_stride(table_out);
+  if (table_out.size(0) != batch || table_out.size(1) != cols) fail(PyExc_ValueError, "unexpected shape of the new page table");
+  int32_t *qr = written(refs_out, pages), *qs = written(src, pages / 2), *qd = written(dst, pages / 2), *qp = written(map, pages), *ql = written(live, 1),
+          *qt = (int32_t*)ptr(table_out);
+  on_current_device({&refs, &table, &refs_out, &table_out, &src, &dst, &map, &live, &ws});
+  if (!ws.defined()) ws = workspace(lr_kv_compact_workspace_bytes(pages), refs);
+  const size_t nb = ws.numel() * ws.element_size();
+  void *pw = dense(ws), *st = stream();
+  call("lr_kv_compact", [&] { return lr_kv_compact(pr, pages, pt, ld, batch, cols, qr, qt, ldo, qs, qd, qp, ql, pw, nb, st); });
+  return nested({&refs_out, &table_out}, {&src, &dst}, {&map, &live});
+}
+
+PyObject* kv_copy(Args& a) {
+  const at::Tensor &k = a.tensor(), &v = a.tensor(), &src = a.tensor(), &dst = a.tensor();
+  const at::Tensor rows = a.optional();
+  const lr_kv_cache c = pages_of(k, v);
+  const int64_t n = rows_of(src, 1);
+  const int32_t *ps = indices(src, n), *pd = indices(dst, n), *pr = indices(rows, n);
+  on_current_device({&k, &v, &src, &dst, &rows});
+  void* st = stream();
+  call("lr_kv_copy", [&] { return lr_kv_copy(&c, ps, pd, pr, n, st); });
+  Py_RETURN_NONE;
+}
+
+// ---- beam search -----------------------------------------------------------------------------
+PyObject* beam_select(Args& a) {
+  const at::Tensor &logits = a.tensor(), &score = a.tensor();
+  const int64_t n = a.integer();
+  const at::Tensor done = a.optional();
+  const int64_t end = a.integer();
+  at::Tensor parent = a.optional(), token = a.optional(), best = a.optional(), ws = a.optional();
+  const int64_t batch = rows_of(score), beams = score.size(1), V = size_of(logits, 1);
+  const int dt = dt_of(logits);
+  if (score.scalar_type() != at::kFloat) fail(g_lr_error, "fp32 scores expected");
+  const int64_t ld = rows_as_wide(logits, batch * beams, V);
+  if (done.defined() && done.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
+  if (done.defined() && done.sizes() != score.sizes()) fail(PyExc_ValueError, "unexpected shape of the ended beams");
+  const int64_t sizes[] = {batch, n < 0 ? 0 : n};
+  if (!parent.defined()) parent = fresh32(sizes, score);
+  if (!token.defined()) token = fresh32(sizes, score);
+  if (!best.defined()) best = fresh(sizes, at::kFloat, score);
+  if (parent.scalar_type() != at::kInt || token.scalar_type() != at::kInt || best.scalar_type() != at::kFloat) fail(g_lr_error, "int32 choices and fp32 scores expected");
+  for (const at::Tensor* t : {&parent, &token, &best})
+    if (t->sizes() != at::IntArrayRef(sizes)) fail(PyExc_ValueError, "unexpected shape of the choices");
+  on_current_device({&logits, &score, &done, &parent, &token, &best, &ws});
+  if (!ws.defined()) ws = workspace(lr_beam_select_workspace_bytes(batch, beams, V, n), score);
+  const size_t nb = ws.numel() * ws.element_size();
+  void *pl = ptr(logits), *ps = dense(score), *pd = dense(done), *pp = dense(parent), *pt = dense(token), *pb = dense(best), *pw = dense(ws), *st = stream();
+  call("lr_beam_select", [&] {
+    return lr_beam_select(pl, ld, (float*)ps, (int32_t*)pd, end, (int32_t*)pp, (int32_t*)pt, (float*)pb, batch, beams, V, n, dt, pw, nb, st);
+  });
+  return tuple(parent, token, best);
+}
+
+// ---- 8-bit integers --------------------------------------------------------------------------
+// Rows of `width` integers: their stride.  They are read, and written, up to the next multiple of 16.
+int64_t rows_q8(const at::Tensor& t, int64_t rows, int64_t width) {
+  if (t.scalar_type() != at::kChar) fail(g_lr_error, "int8 rows expected");
+  if (t.dim() != 2 || t.size(0) != rows || t.size(1) != width) fail(PyExc_ValueError, "unexpected shape");
+  const int64_t wide = (width + 15) / 16 * 16;
+  if (width > 1 && t.stride(1) != 1) fail(PyExc_AssertionError, "row-major 2-D tensor expected");
+  const int64_t ld = rows > 1 ? t.stride(0) : wide;
+  if (rows > 0 && t.defined() && (int64_t)t.storage().nbytes() < t.storage_offset() + (rows - 1) * ld + wide)
+    fail(g_lr_error, "rows that can be read up to the next multiple of 16 expected");
+  return ld;
+}
+void scales_of(const at::Tensor& s, int64_t n) {
+  if (s.scalar_type() != at::kFloat) fail(g_lr_error, "fp32 scales expected");
+  if (s.dim() != 1 || s.size(0) != n) fail(PyExc_ValueError, "a scale for each row expected");
+}
+// [rows, width] in rows that start on 16 bytes
+at::Tensor padded(int64_t rows, int64_t width, at::ScalarType dt, const at::Tensor& like) {
+  const int64_t per = 16 / (int64_t)at::elementSize(dt), ld = (width + per - 1) / per * per;
+  const at::Tensor t = fresh({rows, ld}, dt, like);
+  return ld == width ? t : t.narrow(1, 0, width);
+}
+
+PyObject* quant_rows(Args& a) {
+  const at::Tensor& x = a.tensor();
+  at::Tensor q = a.optional(), scale = a.optional();
+  const int64_t T = rows_of(x), n = x.size(1);
+  const int dt = dt_of(x);
+  const int64_t ldx = rows_as_wide(x, T, n);
+  if (!q.defined()) q = padded(T, n, at::kChar, x);
+  if (!scale.defined()) scale = fresh({T}, at::kFloat, x);
+  const int64_t ldq = rows_q8(q, T, n);
+  scales_of(scale, T);
+  on_current_device({&x, &q, &scale});
+  void *px = ptr(x), *pq = ptr(q), *ps = dense(scale), *st = stream();
+  call("lr_quant_rows", [&] { return lr_quant_rows(px, ldx, (int8_t*)pq, ldq, (float*)ps, T, n, dt, st); });
+  return tuple(q, scale);
+}
+
+PyObject* matmul_q8(Args& a) {
+  const at::Tensor &x = a.tensor(), &sx = a.tensor(), &w = a.tensor(), &sw = a.tensor();
+  const int dt = a.enumerator();
+  at::Tensor c = a.optional();
+  const int64_t M = rows_of(x), K = x.size(1), N = rows_of(w);
+  const int64_t ldx = rows_q8(x, M, K), ldw = rows_q8(w, N, K);
+  scales_of(sx, M);
+  scales_of(sw, N);
+  if (!c.defined()) c = padded(M, N, scalar(dt), x);
+  if (c.dim() != 2 || c.size(0) != M || c.size(1) != N || (N > 1 && c.stride(1) != 1)) fail(PyExc_ValueError, "unexpected shape");
+  const int64_t per = dt == LR_BF16 ? 8 : 4, ldc = M > 1 ? c.stride(0) : (N + per - 1) / per * per;
+  on_current_device({&x, &sx, &w, &sw, &c});
+  void *px = ptr(x), *ps = dense(sx), *pw = ptr(w), *pt = dense(sw), *pc = ptr(c), *st = stream();
+  call("lr_matmul_q8", [&] { return lr_matmul_q8((int8_t*)px, ldx, (float*)ps, (int8_t*)pw, ldw, (float*)pt, pc, ldc, M, N, K, dt, st); });
+  return wrap(c);
+}
+
+PyObject* linear_q8_fwd(Args& a) {
+  const at::Tensor &x = a.tensor(), &wd = a.tensor(), &sd = a.tensor(), &wu = a.tensor(), &su = a.tensor();
+  const int act = a.enumerator();
+  at::Tensor y = a.optional(), ws = a.optional();
+  const int64_t T = rows_of(x), d = x.size(1), r = rows_of(wd), n = rows_of(wu);
+  const int dt = dt_of(x);
+  const int64_t ldx = rows_as_wide(x, T, d), ldd = rows_q8(wd, r, d), ldu = rows_q8(wu, n, r);
+  scales_of(sd, r);
+  scales_of(su, n);
+  if (!y.defined()) y = padded(T, n, x.scalar_type(), x);
+  if (y.dim() != 2 || y.size(0) != T || y.size(1) != n || (n > 1 && y.stride(1) != 1)) fail(PyExc_ValueError, "unexpected shape");
+  same_type(x, {&y});
+  const int64_t per = dt == LR_BF16 ? 8 : 4, ldy = T > 1 ? y.stride(0) : (n + per - 1) / per * per;
+  on_current_device({&x, &wd, &sd, &wu, &su, &y, &ws});
+  if (!ws.defined()) ws = workspace(lr_linear_q8_workspace_bytes(T, d, r), x);
+  const size_t nb = ws.numel() * ws.element_size();
+  void *px = ptr(x), *pd = ptr(wd), *qd = dense(sd), *pu = ptr(wu), *qu = dense(su), *py = ptr(y), *pw = dense(ws), *st = stream();
+  call("lr_linear_q8_fwd", [&] {
+    return lr_linear_q8_fwd(px, ldx, (int8_t*)pd, ldd, (float*)qd, (int8_t*)pu, ldu, (float*)qu, py, ldy, T, d, r, n, act, dt, pw, nb, st);
+  });
+  return wrap(y);
+}
+
 // No C++ exception leaves an entry; torch's own become the Python exceptions that they are elsewhere (out of memory, a device's error,
 // an interpreter's exception that crossed torch).
 template <PyObject* (*F)(Args&)>
@@ -498,7 +709,8 @@ PyObject* set_error(PyObject*, PyObject* type) {
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))(&entry<f>), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {
     ENTRY(linear_fwd), ENTRY(linear_fwd_static), ENTRY(linear_bwd), ENTRY(group_fwd), ENTRY(group_bwd), ENTRY(attention_fwd), ENTRY(attention_bwd),
-    ENTRY(rope_table), ENTRY(rope_at), ENTRY(kv_append), ENTRY(attention_paged_fwd), ENTRY(rms_stat), ENTRY(rmsnorm_apply), ENTRY(rmsnorm_bwd), ENTRY(swiglu_fwd), ENTRY(swiglu_bwd),
+    ENTRY(rope_table), ENTRY(rope_at), ENTRY(kv_append), ENTRY(attention_paged_fwd), ENTRY(kv_fork), ENTRY(kv_compact), ENTRY(kv_copy), ENTRY(beam_select),
+    ENTRY(quant_rows), ENTRY(matmul_q8), ENTRY(linear_q8_fwd), ENTRY(rms_stat), ENTRY(rmsnorm_apply), ENTRY(rmsnorm_bwd), ENTRY(swiglu_fwd), ENTRY(swiglu_bwd),
     {"set_error", set_error, METH_O, "the exception type of failed calls"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
