@@ -1690,7 +1690,8 @@ int lr_beam_select(const void* logits, int64_t ldl, const float* score, const in
 }
 
 // ---- products of 8-bit integers --------------------------------------------------------------------
-constexpr int64_t Q8_K_MOST = 133144, Q8_LD_MOST = (int64_t)1 << 22;
+// (offsets inside a tile of 256 rows are formed in 32 bits)
+constexpr int64_t Q8_K_MOST = 133144, Q8_LD_MOST = (int64_t)1 << 22, Q8_LDC_MOST = (int64_t)1 << 20;
 
 static int check_quant(const void* x, int64_t ldx, int64_t T, int64_t n, int dt) {
   TRY(check_dt(dt));
@@ -1720,7 +1721,7 @@ static int check_q8(const int8_t* p, int64_t ld, const float* s, int64_t K) {
 static int check_q8_out(const void* c, int64_t ldc, int64_t N, int dt) {
   if (ldc < N) return LR_EINVAL;
   if (ldc % (dt == LR_BF16 ? 8 : 4)) return LR_EALIGN;
-  if (ldc > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  if (ldc > Q8_LDC_MOST) return LR_EUNSUPPORTED;
   return check_ptrs(LR_BF16, {c});
 }
 int lr_matmul_q8(const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb, void* c, int64_t ldc, int64_t M,
@@ -1770,10 +1771,19 @@ int lr_linear_q8_fwd(const void* x, int64_t ldx, const int8_t* w_down, int64_t l
   TRY(check_ws(ws, ws_bytes, lr_linear_q8_workspace_bytes(T, d_in, r)));
   Ctx c; c.base = (char*)ws; c.cap = ws_bytes; c.st = (hipStream_t)stream;
   const LinearQ8 p = linear_q8_parts(c, T, d_in, r);
+  Q8Op down{p.qx, w_down, p.sx, s_down, p.z, p.ldx, ld_down, p.ldz, (int)T, (int)r, (int)d_in, LR_F32};
+  Q8Op up{p.qa, w_up, p.sz, s_up, y, p.ldz, ld_up, ldy, (int)T, (int)d_out, (int)r, dt};
+  // few rows: both products quantise their rows themselves (two launches), the first one writes act(z)
+  if (gemm_q8_quantises(T, d_in, x, ldx, dt) && gemm_q8_quantises(T, r, p.z, p.ldz, LR_F32)) {
+    down.act = act;
+    LAUNCH(c, gemm_q8_from(down, x, ldx, dt, false, c.st));
+    LAUNCH(c, gemm_q8_from(up, p.z, p.ldz, LR_F32, true, c.st));
+    return status_of(c);
+  }
   LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));
-  LAUNCH(c, gemm_q8(Q8Op{p.qx, w_down, p.sx, s_down, p.z, p.ldx, ld_down, p.ldz, (int)T, (int)r, (int)d_in, LR_F32}, c.st));
+  LAUNCH(c, gemm_q8(down, c.st));
   LAUNCH(c, k_quant_rows(p.z, p.ldz, p.qa, p.ldz, p.sz, T, r, act, LR_F32, c.st));
-  LAUNCH(c, gemm_q8(Q8Op{p.qa, w_up, p.sz, s_up, y, p.ldz, ld_up, ldy, (int)T, (int)d_out, (int)r, dt}, c.st));
+  LAUNCH(c, gemm_q8(up, c.st));
   return status_of(c);
 }
 

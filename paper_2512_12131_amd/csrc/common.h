@@ -302,7 +302,7 @@ size_t beam_select_ws_bytes(int64_t rows, int64_t V, int64_t n);
 hipError_t k_beam_select(BeamSelect s, int dt, void* ws, hipStream_t st);
 
 // ---- 8-bit integers (quant_q8.hip, gemm_q8.hip) ----------------------------------------------------
-// rows of x (act applied first) as integers and scales
+// rows of x as integers and scales; act != LR_ACT_IDENTITY (fp32, a result of our own): of act(x)
 hipError_t k_quant_rows(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t T, int64_t n, int act, int dt, hipStream_t);
 // C[m, n] = sa[m] sb[n] sum_k A[m, k] B[n, k], rounded to dt
 struct Q8Op {
@@ -311,8 +311,13 @@ struct Q8Op {
   void* C;
   int64_t lda, ldb, ldc;
   int M, N, K, dt;
+  int act = LR_ACT_IDENTITY;               // of C, before it is stored (gemm_q8_from alone)
 };
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st);
+// The same of x [M, K] in src_dt, quantised on the way in (op.A and op.sa are not read), with op.act behind it: for few rows.  ours: x is fp32, a result
+// of our own.
+bool gemm_q8_quantises(int64_t M, int64_t K, const void* x, int64_t ldx, int dt);
+hipError_t gemm_q8_from(const Q8Op& op, const void* x, int64_t ldx, int src_dt, bool ours, hipStream_t st);
 
 // ---- attention (attention.hip) ---------------------------------------------------------------
 hipError_t attention_fwd_bf16(const void* q, const void* k, const void* v, void* o, float* lse, int64_t ld,
