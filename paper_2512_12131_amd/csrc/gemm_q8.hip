@@ -133,8 +133,21 @@ __device__ __forceinline__ void q8_epilogue(const Q8Op& op, i32x16 (&acc)[T::FM]
 }
 
 // ---- ring tiles: a workgroup per output tile ----------------------------------------------------
+// dma16 past the caches' retention, for what is read once
+template <bool FIRST>
+__device__ __forceinline__ void dma16_once(rsrc_words rs, uint32_t lds, uint32_t voff) {
+  if constexpr (FIRST)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(voff), "s"(rs) : "m0", "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(lds), "v"(voff), "s"(rs) : "m0", "memory");
+}
+
 // (rows of 128 bytes are 64 elements of the bf16 kernels' offsets)
-template <class T, int OUT, bool EDGE, bool TAIL>
+// ONCE: one row of tiles and a weight that comes from memory.  Its rows are 4 KB or so apart, and workgroups that all walk k from its start ask for the
+// same few channels at a time: each column of tiles starts 5 slices further instead, and the weight passes by the caches.  us, weights from
+// memory, plain / starts apart / both: 64 x 32000 x 4096 32.7 / 27.7 / 24.4 (5.4 TB/s), 128 x 32000 x 4096 on 128 x 128 tiles 34.1 / 29.8 / 28.3, 64 x 11008 x
+// 4096 on 64 x 64 14.9 / 14.1 / 13.5; of a weight that the caches keep, 64 x 1000 x 4000, 11.5 / 11.6 / 17.3, so it has to be 16 MB.
+template <class T, int OUT, bool EDGE, bool TAIL, bool ONCE>
 __global__ __launch_bounds__(T::NT) void q8_ring_kernel(Q8Op op, int tiles_m, int tiles_n) {
   static_assert(T::NL == 0, "every wavefront loads and multiplies");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -152,13 +165,17 @@ __global__ __launch_bounds__(T::NT) void q8_ring_kernel(Q8Op op, int tiles_m, in
   int kl = 0;
   lane_offsets<T, false, T::BM>(offA, kl, op.lda / 2, m0, op.M, wave, lane);
   lane_offsets<T, false, T::BN>(offB, kl, op.ldb / 2, n0, op.N, wave, lane);
+  const int start = ONCE ? tn * 5 % nit : 0;
+  auto stage_of = [&](int it) { return !ONCE || it >= nit ? it : it + start >= nit ? it + start - nit : it + start; };
   auto issue_one = [&](int it, int slot, auto I, auto FIRST) {
     constexpr int s = decltype(I)::value / (T::LA + T::LB), j = decltype(I)::value % (T::LA + T::LB);
     constexpr bool is_a = j < T::LA;
     constexpr int i = is_a ? j : j - T::LA;
-    const int k0 = it * KST + s * BK;
+    const int k0 = stage_of(it) * KST + s * BK;
     const uint32_t dst = sbase + (uint32_t)(slot * T::STAGE + s * T::SLICE + (is_a ? 0 : T::A_BYTES)) + (uint32_t)(wave + T::NWL * i) * 1024u;
-    dma16<decltype(FIRST)::value>(is_a ? rsA : rsB, dst, k0 + kl < klen ? (is_a ? offA[is_a ? i : 0] : offB[is_a ? 0 : i]) + (uint32_t)k0 * 2u : RING_OOB);
+    const uint32_t off = k0 + kl < klen ? (is_a ? offA[is_a ? i : 0] : offB[is_a ? 0 : i]) + (uint32_t)k0 * 2u : RING_OOB;
+    if constexpr (ONCE && !is_a) dma16_once<decltype(FIRST)::value>(rsB, dst, off);
+    else dma16<decltype(FIRST)::value>(is_a ? rsA : rsB, dst, off);
   };
   i32x16 acc[T::FM][T::FN] = {};
   const Tail tail(op.K);
@@ -189,7 +206,7 @@ __global__ __launch_bounds__(T::NT) void q8_ring_kernel(Q8Op op, int tiles_m, in
       static_for<l1 - l0>([&](auto L) { issue_one(it + T::NS - 1, wr, std::integral_constant<int, l0 + decltype(L)::value>{}, std::false_type{}); });
 #pragma unroll
       for (int i = 0; i < T::FM; i++) {
-        if constexpr (TAIL) af[kk][i] = tail.of(af[kk][i], it * (KST / 8) + kk * 2 + fhalf);
+        if constexpr (TAIL) af[kk][i] = tail.of(af[kk][i], stage_of(it) * (KST / 8) + kk * 2 + fhalf);
 #pragma unroll
         for (int j = 0; j < T::FN; j++) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(bf[kk][j], af[kk][i], acc[i][j], 0, 0, 0);
       }
@@ -205,15 +222,20 @@ __global__ __launch_bounds__(T::NT) void q8_ring_kernel(Q8Op op, int tiles_m, in
   q8_epilogue<T, OUT, EDGE>(op, acc, scales, typename T::EpiStage{smem + wave * T::STAGE_BYTES}, wave, lane, m0, n0);
 }
 
-template <class T, int OUT, bool EDGE, bool TAIL>
-hipError_t launch_q8_ring(const Q8Op& op, hipStream_t st) {
-  auto kern = q8_ring_kernel<T, OUT, EDGE, TAIL>;
+template <class T, int OUT, bool EDGE, bool TAIL, bool ONCE>
+hipError_t launch_q8_ring_as(const Q8Op& op, hipStream_t st) {
+  auto kern = q8_ring_kernel<T, OUT, EDGE, TAIL, ONCE>;
   // one-time opt-in to more than 64 KB of dynamic LDS (thread-safe function-local static)
   static const hipError_t attr_err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
   if (attr_err != hipSuccess) return attr_err;
   const int tiles_m = (op.M + T::BM - 1) / T::BM, tiles_n = (op.N + T::BN - 1) / T::BN;
   hipLaunchKernelGGL(kern, dim3((uint32_t)tiles_m * tiles_n), dim3(T::NT), T::LDS_BYTES, st, op, tiles_m, tiles_n);
   return hipGetLastError();
+}
+template <class T, int OUT, bool EDGE, bool TAIL>
+hipError_t launch_q8_ring(const Q8Op& op, hipStream_t st) {
+  const bool once = op.M <= T::BM && (int64_t)op.N * op.K >= 16 << 20;
+  return once ? launch_q8_ring_as<T, OUT, EDGE, TAIL, true>(op, st) : launch_q8_ring_as<T, OUT, EDGE, TAIL, false>(op, st);
 }
 
 // ---- 256 x 256 tiles: at most one workgroup per CU, which walks its tiles in one stream of slices --------
@@ -368,13 +390,13 @@ __global__ __launch_bounds__(Big::NT) void q8_big_kernel(Q8Op op, int tiles_m, i
     const bool more = nid_next < tiles_end;
     if (more) nxt = source(nid_next);
     else nxt.rec_a = nxt.rec_b = 0;
+    Q8Scales<T, Big::EpiStage> scales;      // (asked for here, they don't wait behind the next tile's slices)
+    scales.load(op, cur.m0, cur.n0, wave, lane);
     load_frags(0, a0, b0, 0);
     slice(0, std::true_type{});
     for (int kt = 1; kt < nk; kt++) slice(kt, std::false_type{});
     int elane = lane, ewave = wave;
     asm volatile("" : "+v"(elane), "+s"(ewave));      // (the epilogue's addresses stay out of the loop over tiles)
-    Q8Scales<T, Big::EpiStage> scales;
-    scales.load(op, cur.m0, cur.n0, ewave, elane);
     issue(nk + 1, b1, OPB, Half1{});
     __builtin_amdgcn_sched_barrier(0);
     q8_epilogue<T, OUT, EDGE>(op, acc, scales, Big::EpiStage{smem + a2 + wave * 1024}, ewave, elane, cur.m0, cur.n0);

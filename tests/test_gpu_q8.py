@@ -97,7 +97,8 @@ def product(a, sa, b, sb, dtype):
 
 
 SHAPES = [(1, 1, 1), (1, 33, 15), (3, 7, 16), (33, 31, 17), (32, 64, 32), (5, 100, 129), (16, 1024, 4096), (16, 4096, 1024), (64, 2048, 512), (65, 129, 1000),
-          (100, 777, 333), (128, 128, 128), (129, 257, 640), (256, 512, 255), (777, 2047, 546), (300, 4096, 64), (1031, 768, 256), (2048, 2048, 2048)]
+          (100, 777, 333), (128, 128, 128), (129, 257, 640), (256, 512, 255), (777, 2047, 546), (300, 4096, 64), (1031, 768, 256), (2048, 2048, 2048),
+          (64, 8200, 2050), (40, 33000, 515), (128, 33000, 523), (100, 4100, 4109), (17, 16500, 1024)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
