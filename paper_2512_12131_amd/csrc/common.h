@@ -311,13 +311,13 @@ struct Q8Op {
   void* C;
   int64_t lda, ldb, ldc;
   int M, N, K, dt;
-  int act = LR_ACT_IDENTITY;               // of C, before it is stored (gemm_q8_from alone)
+  int act = LR_ACT_IDENTITY;               // of C, before it is stored (where gemm_q8_acts says so, and gemm_q8_from)
 };
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st);
-// The same of x [M, K] in src_dt, quantised on the way in (op.A and op.sa are not read), with op.act behind it: for few rows.  ours: x is fp32, a result
-// of our own.
-bool gemm_q8_quantises(int64_t M, int64_t K, const void* x, int64_t ldx, int dt);
-hipError_t gemm_q8_from(const Q8Op& op, const void* x, int64_t ldx, int src_dt, bool ours, hipStream_t st);
+// The same of fp32 rows x [M, K] of our own (on 16 bytes), quantised on the way in (op.A and op.sa are not read): for few rows.
+bool gemm_q8_acts(const Q8Op& op);
+bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K);
+hipError_t gemm_q8_from(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st);
 
 // ---- attention (attention.hip) ---------------------------------------------------------------
 hipError_t attention_fwd_bf16(const void* q, const void* k, const void* v, void* o, float* lse, int64_t ld,

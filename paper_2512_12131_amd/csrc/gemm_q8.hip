@@ -16,6 +16,7 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 // A's operand of chunk c with what lies behind K cleared
 struct Tail {
@@ -418,140 +419,138 @@ hipError_t launch_q8_big(const Q8Op& op, hipStream_t st) {
   return hipGetLastError();
 }
 
-// ---- up to 16 rows ------------------------------------------------------------------------------
-// A workgroup takes NT * 16 columns over all of k, its 16 wavefronts a share of k each: v_mfma_i32_16x16x64_i8 on operands that come from memory
-// straight into registers, R16_S steps of 64 k asked for at once, and the 16 sums added up through LDS.
+// ---- 16 x 16 pieces: few rows --------------------------------------------------------------------
+// A workgroup takes 16 rows and NT * 16 columns over all of k: A and B lie in LDS as they are (up to `chunk` k at a time), its 16 wavefronts take every
+// 16th step of 64 k each (v_mfma_i32_16x16x64_i8) and the 16 sums are added up through LDS.
 //
-// SRC: A is int8 with scales, or bf16 / fp32 rows (of at most R16_K columns) that every workgroup quantises for itself, `act` applied first.
-constexpr int R16_W = 16, R16_S = 4, R16_K = R16_W * R16_S * 64;
-enum : int { Q8_SRC = 0, BF16_SRC = 1, F32_SRC = 2, OURS_SRC = 3 };
+// OURS: A is fp32, the activations of a layer's first product, which every workgroup quantises for itself, a wavefront a row: it holds the row (of up to
+// 64 * 4 * OURS columns) in registers, whose largest element needs no other wavefront.  Bound: the way in and out of a launch, and what a CU takes in.
+// The layer 4096 -> 1024 -> 4096 of 16 tokens, us: 12.1 so, 13.0 with a launch for the quantisation between the products; with the bf16 rows
+// quantised by the first product too (128 KB for each of 64 workgroups) 12.9.
+constexpr int R16_W = 16, R16_SLICE = 2048, R16_LDS = 160 * 1024;
+constexpr int rows16_lds(int chunk, int nt) { return chunk / 128 * R16_SLICE * (1 + nt) + R16_W * nt * 1024; }
 
-template <int SRC, int NT, int OUT, bool TAIL>
-__global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const void* x, int64_t ldx) {
-  __shared__ int part[R16_W][NT * 256];
-  __shared__ uint32_t row_most[R16_W][16];
+template <int OURS, int NT, int OUT, bool TAIL>
+__global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const float* x, int64_t ldx, int chunk) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ float row_scale[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int m0 = blockIdx.y * 16, row = lane & 15, kq = (lane >> 4) * 16, n0 = blockIdx.x * (NT * 16);
-  const bool has = m0 + row < op.M;
-  constexpr uint32_t OOB = 0x80000000u;
-  const int kbytes = (op.K + 15) / 16 * 16;
-  const __amdgpu_buffer_rsrc_t rsB = __builtin_amdgcn_make_buffer_rsrc((void*)(op.B + (int64_t)n0 * op.ldb), 0, 0x7fffffffu, 0x00020000);
-  uint32_t offB[NT];
-#pragma unroll
-  for (int j = 0; j < NT; j++) offB[j] = n0 + j * 16 + row < op.N ? (uint32_t)(j * 16 + row) * (uint32_t)op.ldb : OOB;
-  const int steps = (kbytes + 63) / 64;
-  i32x4 acc[NT] = {};
-  float scale = 0.f;
-  if constexpr (SRC == Q8_SRC) {
-    const __amdgpu_buffer_rsrc_t rsA = __builtin_amdgcn_make_buffer_rsrc((void*)(op.A + (int64_t)m0 * op.lda), 0, 0x7fffffffu, 0x00020000);
-    const uint32_t offA = has ? (uint32_t)row * (uint32_t)op.lda : OOB;
-    const Tail tail(op.K);
-    for (int s0 = wave; s0 < steps; s0 += R16_W * R16_S) {
-      u32x4 a[R16_S], b[R16_S][NT];
-#pragma unroll
-      for (int s = 0; s < R16_S; s++) {
-        const int k = (s0 + s * R16_W) * 64 + kq;
-        const uint32_t at = k < kbytes ? (uint32_t)k : OOB;
-#pragma unroll
-        for (int j = 0; j < NT; j++) b[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rsB, (int)((offB[j] | at) & OOB ? OOB : offB[j] + at), 0, 0);
-        a[s] = __builtin_amdgcn_raw_buffer_load_b128(rsA, (int)((offA | at) & OOB ? OOB : offA + at), 0, 0);
-      }
-#pragma unroll
-      for (int s = 0; s < R16_S; s++) {
-        i32x4 fa = __builtin_bit_cast(i32x4, a[s]);
-        if constexpr (TAIL) fa = tail.of(fa, (s0 + s * R16_W) * 4 + (lane >> 4));
-#pragma unroll
-        for (int j = 0; j < NT; j++) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b[s][j]), fa, acc[j], 0, 0, 0);
-      }
+  const int m0 = blockIdx.y * 16, n0 = blockIdx.x * (NT * 16);
+  const int kbytes = (op.K + 15) / 16 * 16, slices = chunk / 128;
+  unsigned char* sB = smem + slices * R16_SLICE;                 // then NT of these
+  int* part = reinterpret_cast<int*>(sB + NT * slices * R16_SLICE);
+  const uint32_t lds = (uint32_t)(uintptr_t)LRB_LDS_PTR(smem);
+  const rsrc_words rsB = operand_rsrc(op.B + (int64_t)n0 * op.ldb), rsA = operand_rsrc(OURS ? op.B : op.A + (int64_t)m0 * op.lda);
+  // Loads of 8 rows x 128 bytes: the rows of A (as int8), then those of B, slice by slice
+  constexpr int FIRST_OP = OURS ? 1 : 0, PER = 2 * (1 + NT - FIRST_OP);
+  auto load = [&](int k0) {
+    for (int id = wave; id < slices * PER; id += R16_W) {
+      const int slice = id / PER, w = id % PER + 2 * FIRST_OP, o = w >> 1;      // o: 0 A, then the 16 columns of B
+      const int row = (w & 1) * 8 + (lane >> 3), lc = (lane & 7) ^ ((row >> 1) & 7);
+      const int k = k0 + slice * 128 + lc * 16;
+      const bool in = k < kbytes && (o == 0 ? m0 + row < op.M : n0 + (o - 1) * 16 + row < op.N);
+      const uint32_t off = in ? (o == 0 ? (uint32_t)row * (uint32_t)op.lda : (uint32_t)((o - 1) * 16 + row) * (uint32_t)op.ldb) + (uint32_t)k : RING_OOB;
+      dma16<true>(o == 0 ? rsA : rsB, lds + (uint32_t)((o * slices + slice) * R16_SLICE + (w & 1) * 1024), off);
     }
-    if (has) scale = op.sa[m0 + row];
-  } else {
-    constexpr int ES = SRC == BF16_SRC ? 2 : 4, NV = ES;               // 16-byte vectors of 16 elements
-    const __amdgpu_buffer_rsrc_t rsX = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)x + (int64_t)m0 * ldx * ES), 0, 0x7fffffffu, 0x00020000);
-    const uint32_t offX = has ? (uint32_t)row * (uint32_t)ldx * ES : OOB;
-    u32x4 b[R16_S][NT], v[R16_S][NV];
-#pragma unroll
-    for (int s = 0; s < R16_S; s++) {
-      const int k = (wave + s * R16_W) * 64 + kq;
-#pragma unroll
-      for (int i = 0; i < NV; i++) {
-        const uint32_t at = k + i * (16 / ES) < op.K ? (uint32_t)(k * ES + i * 16) : OOB;
-        v[s][i] = __builtin_amdgcn_raw_buffer_load_b128(rsX, (int)((offX | at) & OOB ? OOB : offX + at), 0, 0);
-      }
+  };
+  i32x4 acc[NT] = {};
+  const Tail tail(op.K);
+  auto multiply = [&](int k0) {
+    const int row = lane & 15, sw = (row >> 1) & 7;
+    for (int step = wave; step < 2 * slices; step += R16_W) {
+      const int at = (step >> 1) * R16_SLICE + row * 128 + ((((step & 1) * 4 + (lane >> 4)) ^ sw) << 4);
+      i32x4 fa = *reinterpret_cast<const i32x4*>(smem + at);
+      if constexpr (!OURS && TAIL) fa = tail.of(fa, (k0 + step * 64) / 16 + (lane >> 4));
 #pragma unroll
       for (int j = 0; j < NT; j++)
-        b[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rsB, (int)(((offB[j] | (k < kbytes ? 0u : OOB)) & OOB) ? OOB : offB[j] + (uint32_t)k), 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4*>(sB + j * slices * R16_SLICE + at), fa, acc[j], 0, 0, 0);
     }
-    auto values = [&](int s, float* f) {
-      if constexpr (SRC == BF16_SRC) {
-        unpack8(make_uint4(v[s][0][0], v[s][0][1], v[s][0][2], v[s][0][3]), f);
-        unpack8(make_uint4(v[s][1][0], v[s][1][1], v[s][1][2], v[s][1][3]), f + 8);
-      } else {
+  };
+  if constexpr (!OURS) {
+    for (int k0 = 0; k0 < kbytes; k0 += chunk) {
+      load(k0);
+      wait_vmcnt<0>();
+      __syncthreads();
+      multiply(k0);
+      __syncthreads();
+    }
+    if (tid < 16) row_scale[tid] = m0 + tid < op.M ? op.sa[m0 + tid] : 0.f;
+  } else {
+    f32x4 v[OURS];
+    const bool has = m0 + wave < op.M;
+    const float* px = x + (int64_t)(m0 + wave) * ldx;
 #pragma unroll
-        for (int e = 0; e < 16; e++) f[e] = __uint_as_float(v[s][e / 4][e % 4]);
-      }
-    };
+    for (int i = 0; i < OURS; i++) {
+      const int k = (i * 64 + lane) * 4;
+      v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (has && k < op.K) v[i] = *reinterpret_cast<const f32x4*>(px + k);
+    }
+    load(0);
     uint32_t most = 0;
 #pragma unroll
-    for (int s = 0; s < R16_S; s++) {
-      float f[16];
-      values(s, f);
+    for (int i = 0; i < OURS; i++)
 #pragma unroll
-      for (int e = 0; e < 16; e++) most = max(most, __float_as_uint(f[e]) & 0x7fffffffu);
+      for (int e = 0; e < 4; e++) most = max(most, __float_as_uint(v[i][e]) & 0x7fffffffu);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    const Scale<Rows::OURS> sc(most);
+    if (lane == 0) row_scale[wave] = sc.scale;
+    const int sw = (wave >> 1) & 7;
+#pragma unroll
+    for (int i = 0; i < OURS; i++) {
+      const int k = (i * 64 + lane) * 4;
+      const float f[4] = {v[i][0], v[i][1], v[i][2], v[i][3]};
+      // (of a row without a scale anything: it is multiplied with NaN)
+      if (k < chunk) *reinterpret_cast<uint32_t*>(smem + (k >> 7) * R16_SLICE + wave * 128 + ((((k >> 4) & 7) ^ sw) << 4) + (k & 15)) = sc.bytes(f);
     }
-    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
-    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-    if (lane < 16) row_most[wave][lane] = most;
+    wait_vmcnt<0>();
     __syncthreads();
-#pragma unroll
-    for (int w = 0; w < R16_W; w++) most = max(most, row_most[w][row]);
-    const Scale<SRC == BF16_SRC ? Rows::BF16 : SRC == F32_SRC ? Rows::F32 : Rows::OURS> sc(most);
-    scale = sc.scale;
-    // (opaque copies: otherwise all elements are kept as floats across the barrier, and spilled)
-#pragma unroll
-    for (int s = 0; s < R16_S; s++)
-#pragma unroll
-      for (int i = 0; i < NV; i++) asm volatile("" : "+v"(v[s][i]));
-#pragma unroll
-    for (int s = 0; s < R16_S; s++) {
-      if (wave + s * R16_W >= steps) break;
-      float f[16];
-      values(s, f);
-      i32x4 fa;
-#pragma unroll
-      for (int e = 0; e < 4; e++) fa[e] = (int)sc.four(f + 4 * e);
-#pragma unroll
-      for (int j = 0; j < NT; j++) acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, b[s][j]), fa, acc[j], 0, 0, 0);
-    }
+    multiply(0);
   }
   // operands exchanged: lane -> row lane % 16, columns 4 (lane / 16) + 0..3
 #pragma unroll
-  for (int j = 0; j < NT; j++) *reinterpret_cast<i32x4*>(&part[wave][j * 256 + lane * 4]) = acc[j];
-  if (wave == 0 && lane < 16) row_most[0][lane] = __float_as_uint(scale);
+  for (int j = 0; j < NT; j++) *reinterpret_cast<i32x4*>(part + wave * (NT * 256) + j * 256 + lane * 4) = acc[j];
   __syncthreads();
   for (int t = tid; t < NT * 256; t += R16_W * 64) {
     int sum = 0;
 #pragma unroll
-    for (int w = 0; w < R16_W; w++) sum += part[w][t];
+    for (int w = 0; w < R16_W; w++) sum += part[w * (NT * 256) + t];
     const int l = (t >> 2) & 63, m = l & 15, n = n0 + (t >> 8) * 16 + (l >> 4) * 4 + (t & 3);
     if (m0 + m < op.M && n < op.N) {
-      const float c = act_f((float)sum * __uint_as_float(row_most[0][m]) * op.sb[n], op.act);
+      const float c = act_f((float)sum * row_scale[m] * op.sb[n], op.act);
       if constexpr (OUT == LR_BF16) ((uint16_t*)op.C)[(int64_t)(m0 + m) * op.ldc + n] = (uint16_t)f32_to_bf16_bits(c);
       else ((float*)op.C)[(int64_t)(m0 + m) * op.ldc + n] = c;
     }
   }
 }
 
-template <int SRC, int OUT, bool TAIL>
-hipError_t launch_rows16_q8(const Q8Op& op, const void* x, int64_t ldx, hipStream_t st) {
-  const int cols = (op.N + 15) / 16;
-  int nt = cols <= 256 ? 1 : cols <= 512 ? 2 : 4;
-  if (SRC >= F32_SRC && nt > 2) nt = 2;      // (registers)
-  const dim3 grid((uint32_t)((cols + nt - 1) / nt), (uint32_t)((op.M + 15) / 16));
-  if (nt == 1) hipLaunchKernelGGL((q8_rows16_kernel<SRC, 1, OUT, TAIL>), grid, dim3(R16_W * 64), 0, st, op, x, ldx);
-  else if (nt == 2) hipLaunchKernelGGL((q8_rows16_kernel<SRC, 2, OUT, TAIL>), grid, dim3(R16_W * 64), 0, st, op, x, ldx);
-  else if constexpr (SRC < F32_SRC) hipLaunchKernelGGL((q8_rows16_kernel<SRC, 4, OUT, TAIL>), grid, dim3(R16_W * 64), 0, st, op, x, ldx);
+// 16-column pieces of a workgroup: one where every piece finds a CU, more where that saves rounds
+int rows16_nt(int64_t M, int64_t N) {
+  const int64_t pieces = ((N + 15) / 16) * ((M + 15) / 16);
+  return pieces <= 256 ? 1 : pieces <= 512 ? 2 : 4;
+}
+
+template <int OURS, int NT, int OUT, bool TAIL>
+hipError_t launch_rows16_nt(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
+  auto kern = q8_rows16_kernel<OURS, NT, OUT, TAIL>;
+  // one-time opt-in to more than 64 KB of dynamic LDS (thread-safe function-local static)
+  static const hipError_t attr_err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, R16_LDS - 256);
+  if (attr_err != hipSuccess) return attr_err;
+  const int whole = (op.K + 127) / 128 * 128;
+  int chunk = whole;
+  while (rows16_lds(chunk, NT) > R16_LDS - 256) chunk = (chunk / 2 + 127) / 128 * 128;      // (int8 alone: several turns of even length)
+  if (OURS && (chunk != whole || op.K > OURS * 256)) return hipErrorInvalidValue;
+  const dim3 grid((uint32_t)((op.N + NT * 16 - 1) / (NT * 16)), (uint32_t)((op.M + 15) / 16));
+  hipLaunchKernelGGL(kern, grid, dim3(R16_W * 64), rows16_lds(chunk, NT), st, op, x, ldx, chunk);
   return hipGetLastError();
+}
+template <int OURS, int OUT, bool TAIL>
+hipError_t launch_rows16_q8(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
+  switch (rows16_nt(op.M, op.N)) {
+    case 1: return launch_rows16_nt<OURS, 1, OUT, TAIL>(op, x, ldx, st);
+    case 2: return launch_rows16_nt<OURS, 2, OUT, TAIL>(op, x, ldx, st);
+    default: return launch_rows16_nt<OURS, 4, OUT, TAIL>(op, x, ldx, st);
+  }
 }
 
 using R64x128 = RingTile<64, 128, 2, 2, 1, 3>;      // two workgroups per CU
@@ -567,7 +566,7 @@ hipError_t launch_q8(const Q8Op& op, int tile, hipStream_t st) {
     case Q8_R128: return launch_q8_ring<R128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64X128: return launch_q8_ring<R64x128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64: return launch_q8_ring<R64, OUT, EDGE, TAIL>(op, st);
-    default: return launch_rows16_q8<Q8_SRC, OUT, TAIL>(op, nullptr, 0, st);
+    default: return launch_rows16_q8<0, OUT, TAIL>(op, nullptr, 0, st);
   }
 }
 
@@ -603,13 +602,14 @@ int q8_tile(const Q8Op& op) {
 
 }  // namespace
 
-bool gemm_q8_quantises(int64_t M, int64_t K, const void* x, int64_t ldx, int dt) {
-  return M <= 16 && K <= R16_K && (dt == LR_BF16 || (((uintptr_t)x & 15) == 0 && ldx % 4 == 0 && K % 4 == 0)) && ldx <= (1 << 22);
+bool gemm_q8_acts(const Q8Op& op) { return q8_tile(op) == Q8_ROWS16; }
+bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K) {
+  return M <= 16 && K <= 4096 && K % 4 == 0 && rows16_lds((int)(K + 127) / 128 * 128, rows16_nt(M, N)) <= R16_LDS - 256;
 }
-hipError_t gemm_q8_from(const Q8Op& op, const void* x, int64_t ldx, int src_dt, bool ours, hipStream_t st) {
-  if (src_dt == LR_BF16) return op.dt == LR_BF16 ? launch_rows16_q8<BF16_SRC, LR_BF16, false>(op, x, ldx, st) : launch_rows16_q8<BF16_SRC, LR_F32, false>(op, x, ldx, st);
-  if (ours) return op.dt == LR_BF16 ? launch_rows16_q8<OURS_SRC, LR_BF16, false>(op, x, ldx, st) : launch_rows16_q8<OURS_SRC, LR_F32, false>(op, x, ldx, st);
-  return op.dt == LR_BF16 ? hipErrorInvalidValue : launch_rows16_q8<F32_SRC, LR_F32, false>(op, x, ldx, st);
+hipError_t gemm_q8_from(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
+  const bool narrow = op.K <= 1024;
+  if (op.dt == LR_BF16) return narrow ? launch_rows16_q8<4, LR_BF16, false>(op, x, ldx, st) : launch_rows16_q8<16, LR_BF16, false>(op, x, ldx, st);
+  return narrow ? launch_rows16_q8<4, LR_F32, false>(op, x, ldx, st) : launch_rows16_q8<16, LR_F32, false>(op, x, ldx, st);
 }
 
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st) {

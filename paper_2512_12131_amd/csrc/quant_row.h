@@ -27,7 +27,7 @@ struct Scale {
     if (none) scale = __builtin_nanf("");
   }
   // Four elements as bytes.  Adding 1.5 * 2^23 leaves the nearest whole number in the low bits.
-  __device__ __forceinline__ uint32_t four(const float* x) const {
+  __device__ __forceinline__ uint32_t bytes(const float* x) const {
     constexpr float C = 12582912.f, NEAR = 0.5f - 0x1p-13f;
     uint32_t w[4];
 #pragma unroll
@@ -43,8 +43,10 @@ struct Scale {
       }
     }
     const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(w[3], w[2], 0x04000c0cu);
-    return none ? 0u : lo | hi;
+    return lo | hi;
   }
+  // ... of a row without a scale zeros
+  __device__ __forceinline__ uint32_t four(const float* x) const { return none ? 0u : bytes(x); }
   // An element next to k + 1/2: the sign of 127 |x| - (k + 1/2) max decides.  Both products have 32 bits at most; as a float and its error each they are
   // subtracted without rounding (the floats are neighbours, the errors have 8 bits and exponents within 8 of each other).
   __device__ __forceinline__ uint32_t settled(float x) const {

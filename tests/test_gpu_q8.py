@@ -98,7 +98,7 @@ def product(a, sa, b, sb, dtype):
 
 SHAPES = [(1, 1, 1), (1, 33, 15), (3, 7, 16), (33, 31, 17), (32, 64, 32), (5, 100, 129), (16, 1024, 4096), (16, 4096, 1024), (64, 2048, 512), (65, 129, 1000),
           (100, 777, 333), (128, 128, 128), (129, 257, 640), (256, 512, 255), (777, 2047, 546), (300, 4096, 64), (1031, 768, 256), (2048, 2048, 2048),
-          (64, 8200, 2050), (40, 33000, 515), (128, 33000, 523), (100, 4100, 4109), (17, 16500, 1024)]
+          (16, 1024, 11000), (50, 700, 9001), (64, 8200, 2050), (40, 33000, 515), (128, 33000, 523), (100, 4100, 4109), (17, 16500, 1024)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -145,7 +145,8 @@ def test_matmul_q8_largest_sums_and_scales_that_are_no_numbers():
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T,d,r,n,silu", [(1, 64, 16, 64, True), (16, 512, 128, 512, True), (7, 136, 40, 72, False), (133, 264, 72, 328, True), (300, 1024, 256, 768, True),
-                                          (777, 512, 64, 1368, False), (5, 4096, 1024, 4096, True)])
+                                          (777, 512, 64, 1368, False), (5, 4096, 1024, 4096, True), (16, 1024, 1024, 4200, True),
+                                          (9, 4000, 520, 8504, False)])
 def test_linear_q8(T, d, r, n, silu, dtype):
     """Bound, element by element.  z and a are within e = 2^-18 of their size (three roundings; the logistic's exponent is rounded by 2^-23 |z| and |z| is
     below 16 here), so the largest of a row and an element are off by 2 e together, and 127 a / max by 254 e: an element may fall to the other side of a half
