@@ -524,11 +524,8 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const fl
   }
 }
 
-// 16-column pieces of a workgroup: one where every piece finds a CU, more where that saves rounds
-int rows16_nt(int64_t M, int64_t N) {
-  const int64_t pieces = ((N + 15) / 16) * ((M + 15) / 16);
-  return pieces <= 256 ? 1 : pieces <= 512 ? 2 : 4;
-}
+// 16-column pieces of a workgroup that quantises its rows: as many as leave about a workgroup per CU
+int rows16_nt(int64_t N) { return N <= 256 * 16 ? 1 : N <= 512 * 16 ? 2 : 4; }
 
 template <int OURS, int NT, int OUT, bool TAIL>
 hipError_t launch_rows16_nt(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
@@ -544,12 +541,12 @@ hipError_t launch_rows16_nt(const Q8Op& op, const float* x, int64_t ldx, hipStre
   hipLaunchKernelGGL(kern, grid, dim3(R16_W * 64), rows16_lds(chunk, NT), st, op, x, ldx, chunk);
   return hipGetLastError();
 }
-template <int OURS, int OUT, bool TAIL>
-hipError_t launch_rows16_q8(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
-  switch (rows16_nt(op.M, op.N)) {
-    case 1: return launch_rows16_nt<OURS, 1, OUT, TAIL>(op, x, ldx, st);
-    case 2: return launch_rows16_nt<OURS, 2, OUT, TAIL>(op, x, ldx, st);
-    default: return launch_rows16_nt<OURS, 4, OUT, TAIL>(op, x, ldx, st);
+template <int OURS, int OUT>
+hipError_t launch_rows16_ours(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
+  switch (rows16_nt(op.N)) {
+    case 1: return launch_rows16_nt<OURS, 1, OUT, false>(op, x, ldx, st);
+    case 2: return launch_rows16_nt<OURS, 2, OUT, false>(op, x, ldx, st);
+    default: return launch_rows16_nt<OURS, 4, OUT, false>(op, x, ldx, st);
   }
 }
 
@@ -566,7 +563,7 @@ hipError_t launch_q8(const Q8Op& op, int tile, hipStream_t st) {
     case Q8_R128: return launch_q8_ring<R128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64X128: return launch_q8_ring<R64x128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64: return launch_q8_ring<R64, OUT, EDGE, TAIL>(op, st);
-    default: return launch_rows16_q8<0, OUT, TAIL>(op, nullptr, 0, st);
+    default: return launch_rows16_nt<0, 1, OUT, TAIL>(op, nullptr, 0, st);
   }
 }
 
@@ -575,11 +572,11 @@ hipError_t launch_q8(const Q8Op& op, int tile, hipStream_t st) {
 // estimates are off by 2 % in the median, 8 to 16 % at the 95th percentile); taking the shortest estimate loses 0.3 % on average and 28 % at most to the
 // fastest tile.  us, 256 x 256 / 128 x 128 / 64 x 128 / 64 x 64: 16384 x 4096 x 4096 225 / 328 / 361 / 555, 4096 x 2048 x 1024 18.5 / 16.6 / 16.8 / 32.7,
 // 1031 x 4096 x 256 9.5 / 10.0 / 8.4 / 15.1, 512 x 1024 x 4096 37.7 / 16.4 / 12.8 / 9.9.
-// Up to 64 rows whose pieces of 16 x 16 find a CU each run as those: 16 x 1024 x 4096 5.6 (9.4 on 64 x 64), 64 x 1024 x 1024 5.1 (5.6); with more pieces,
-// 64 x 4096 x 1024, 10.2 (5.5).
+// Up to 512 pieces of 16 x 16, two for each CU, run as those: 16 x 1024 x 4096 3.8 (9.4 on 64 x 64), 64 x 1024 x 1024 4.1 (5.5), 16 x 8192 x 4096 10.8 (13.1),
+// 128 x 1024 x 4096 7.9 (9.9); with 1024 of them, 128 x 2048 x 1024, 6.7 (5.5).
 int q8_tile(const Q8Op& op) {
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  if (op.M <= 64 && up(op.M, 16) * up(op.N, 16) <= 256) return Q8_ROWS16;
+  if (up(op.M, 16) * up(op.N, 16) <= 512) return Q8_ROWS16;
   struct Cost { int rows, cols, slots; double f, e, e1, s0, s1; };
   static constexpr Cost cost[] = {{256, 256, 256, 4.06, 2.35, 3.45, 0.935, 0.568}, {128, 128, 256, 2.53, 2.07, 0.95, 0.345, 0.186},
                                   {64, 128, 512, 3.00, 0.95, 1.40, 0.252, 0.353}, {64, 64, 256, 2.27, 2.00, 0.22, 0.159, 0.050}};
@@ -604,12 +601,12 @@ int q8_tile(const Q8Op& op) {
 
 bool gemm_q8_acts(const Q8Op& op) { return q8_tile(op) == Q8_ROWS16; }
 bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K) {
-  return M <= 16 && K <= 4096 && K % 4 == 0 && rows16_lds((int)(K + 127) / 128 * 128, rows16_nt(M, N)) <= R16_LDS - 256;
+  return M <= 16 && K <= 4096 && K % 4 == 0 && rows16_lds((int)(K + 127) / 128 * 128, rows16_nt(N)) <= R16_LDS - 256;
 }
 hipError_t gemm_q8_from(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
   const bool narrow = op.K <= 1024;
-  if (op.dt == LR_BF16) return narrow ? launch_rows16_q8<4, LR_BF16, false>(op, x, ldx, st) : launch_rows16_q8<16, LR_BF16, false>(op, x, ldx, st);
-  return narrow ? launch_rows16_q8<4, LR_F32, false>(op, x, ldx, st) : launch_rows16_q8<16, LR_F32, false>(op, x, ldx, st);
+  if (op.dt == LR_BF16) return narrow ? launch_rows16_ours<4, LR_BF16>(op, x, ldx, st) : launch_rows16_ours<16, LR_BF16>(op, x, ldx, st);
+  return narrow ? launch_rows16_ours<4, LR_F32>(op, x, ldx, st) : launch_rows16_ours<16, LR_F32>(op, x, ldx, st);
 }
 
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st) {
