@@ -279,7 +279,6 @@ struct KvCopy {
   FastDiv by_row, by_head;
   const int32_t *src, *dst, *rows;
   int64_t n;
-  int runs;
 };
 hipError_t k_kv_copy(KvCopy c, hipStream_t st);
 

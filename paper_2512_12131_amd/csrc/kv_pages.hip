@@ -301,34 +301,36 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(KvCompact c) {
 
 // The first rows[i] tokens (NULL: all) of page src[i] onto page dst[i], keys and values.
 //
-// Bound: HBM.  A workgroup takes 8 KB of keys or values of a pair at a time, two 16-byte vectors per lane, in the order token, head, column.
-constexpr int COPY_PER = 2, COPY_RUN = 256 * COPY_PER;
+// Bound: HBM.  A workgroup takes up to 256 * PER vectors of 16 bytes of a pair's keys or values at a time, PER per lane, in the order token, head, column.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int PER>
 __global__ __launch_bounds__(256) void kv_copy_kernel(KvCopy c) {
-  const int64_t items = c.n * 2 * c.runs;
-  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int64_t pair = it / (2 * c.runs);
-    const int part = (int)(it - pair * 2 * c.runs);
+  const int part = blockIdx.x, run = part >> 1;
+  uint16_t* const base = (part & 1) ? c.v : c.k;
+  int token[PER];
+  int64_t off[PER];                              // of this lane's vectors inside a page, in elements
+#pragma unroll
+  for (int j = 0; j < PER; j++) {
+    const int v = (run * PER + j) * 256 + threadIdx.x;
+    token[j] = (int)c.by_row.div((uint32_t)v);
+    const int w = v - token[j] * c.row_vecs, h = (int)c.by_head.div((uint32_t)w);
+    off[j] = token[j] * c.token_stride + h * c.head_stride + (w - h * c.head_vecs) * 8;
+  }
+  for (int64_t pair = blockIdx.y; pair < c.n; pair += gridDim.y) {
     const int src = c.src[pair], dst = c.dst[pair];
-    if ((uint32_t)src >= (uint32_t)c.n_pages || (uint32_t)dst >= (uint32_t)c.n_pages || src == dst) continue;
     const int rows = c.rows ? min(max(c.rows[pair], 0), c.page_size) : c.page_size;
-    const int end = rows * c.row_vecs;
-    const int run = part >> 1;
-    uint16_t* base = (part & 1) ? c.v : c.k;
+    if ((uint32_t)src >= (uint32_t)c.n_pages || (uint32_t)dst >= (uint32_t)c.n_pages || src == dst) continue;
     const uint16_t* from = base + (int64_t)src * c.page_stride;
     uint16_t* to = base + (int64_t)dst * c.page_stride;
-    uint4 q[COPY_PER];
-    int64_t off[COPY_PER];
+    u32x4 q[PER];
 #pragma unroll
-    for (int j = 0; j < COPY_PER; j++) {
-      const int v = run * COPY_RUN + j * 256 + threadIdx.x;
-      const int t = (int)c.by_row.div((uint32_t)v), w = v - t * c.row_vecs;
-      const int h = (int)c.by_head.div((uint32_t)w), d = w - h * c.head_vecs;
-      off[j] = v < end ? t * c.token_stride + h * c.head_stride + d * 8 : -1;
-      if (off[j] >= 0) q[j] = *reinterpret_cast<const uint4*>(from + off[j]);
+    for (int j = 0; j < PER; j++) {
+      q[j] = u32x4{0, 0, 0, 0};
+      if (token[j] < rows) q[j] = *reinterpret_cast<const u32x4*>(from + off[j]);
     }
 #pragma unroll
-    for (int j = 0; j < COPY_PER; j++)
-      if (off[j] >= 0) *reinterpret_cast<uint4*>(to + off[j]) = q[j];
+    for (int j = 0; j < PER; j++)
+      if (token[j] < rows) *reinterpret_cast<u32x4*>(to + off[j]) = q[j];
   }
 }
 
@@ -375,12 +377,13 @@ hipError_t k_kv_compact(KvCompact c, void* ws, hipStream_t st) {
 }
 
 hipError_t k_kv_copy(KvCopy c, hipStream_t st) {
-  if (c.n == 0) return hipSuccess;
   const int64_t vecs = (int64_t)c.page_size * c.row_vecs;
-  c.runs = (int)((vecs + COPY_RUN - 1) / COPY_RUN);
-  const int64_t items = c.n * 2 * c.runs;
-  hipLaunchKernelGGL(kv_copy_kernel, dim3((uint32_t)(items < (1 << 20) ? items : (1 << 20))), dim3(256), 0, st, c);
-  return hipGetLastError();
+  auto run = [&](auto kern, int per) {
+    const int64_t runs = (vecs + 256 * per - 1) / (256 * per), most = ((int64_t)1 << 22) / runs + 1;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)(2 * runs), (uint32_t)(c.n < most ? (c.n < 65535 ? c.n : 65535) : (most < 65535 ? most : 65535))), dim3(256), 0, st, c);
+    return hipGetLastError();
+  };
+  return vecs <= 512 ? run(kv_copy_kernel<2>, 2) : run(kv_copy_kernel<8>, 8);
 }
 
 }  // namespace lrb
