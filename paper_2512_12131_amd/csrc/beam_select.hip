@@ -73,178 +73,199 @@ __device__ __forceinline__ uint32_t nth_of_lanes(uint32_t v, int n) {
   return t;
 }
 
-// 16 bytes of logits
+// 16 bytes of logits; a row may start on any element
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
 template <class T> struct Vec;
 template <> struct Vec<uint16_t> {
   static constexpr int N = 8;
-  uint4 q;
-  __device__ __forceinline__ void load(const uint16_t* p) { q = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void load(const uint16_t* p, int from, int end) {      // those of the indices from .. end, -infinity elsewhere
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 8; j++) {
-      const uint32_t b = j >= from && j < end ? p[j] : 0xff80u;
-      w[j / 2] = j % 2 ? w[j / 2] | b << 16 : b;
-    }
-    q = make_uint4(w[0], w[1], w[2], w[3]);
+  static constexpr uint32_t NONE = 0xff80ff80u;        // two of -infinity
+  __device__ static __forceinline__ void floats(u32x4 q, float* f) { unpack8(make_uint4(q[0], q[1], q[2], q[3]), f); }
+  __device__ static __forceinline__ float one(const uint16_t* p) { return bf16_bits_to_f32(*p); }
+  __device__ static __forceinline__ float element(u32x4 q, int i) {      // (i < 8)
+    const uint32_t w = i & 4 ? (i & 2 ? q[3] : q[2]) : (i & 2 ? q[1] : q[0]);
+    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
   }
-  __device__ __forceinline__ void floats(float* f) const { unpack8(q, f); }
+  __device__ static __forceinline__ u32x4 less(u32x4 q, float by) {
+    float f[8];
+    floats(q, f);
+#pragma unroll
+    for (int j = 0; j < 4; j++) q[j] = pack_bf16x2(f[2 * j] - by, f[2 * j + 1] - by);
+    return q;
+  }
 };
 template <> struct Vec<float> {
   static constexpr int N = 4;
-  float4 q;
-  __device__ __forceinline__ void load(const float* p) { q = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void load(const float* p, int from, int end) {
-    float v[4];
+  static constexpr uint32_t NONE = 0xff800000u;
+  __device__ static __forceinline__ void floats(u32x4 q, float* f) {
 #pragma unroll
-    for (int j = 0; j < 4; j++) v[j] = j >= from && j < end ? p[j] : -INFINITY;
-    q = make_float4(v[0], v[1], v[2], v[3]);
+    for (int j = 0; j < 4; j++) f[j] = __uint_as_float(q[j]);
   }
-  __device__ __forceinline__ void floats(float* f) const { f[0] = q.x; f[1] = q.y; f[2] = q.z; f[3] = q.w; }
+  __device__ static __forceinline__ float one(const float* p) { return *p; }
+  __device__ static __forceinline__ float element(u32x4 q, int i) { return __uint_as_float(i & 2 ? (i & 1 ? q[3] : q[2]) : (i & 1 ? q[1] : q[0])); }
+  __device__ static __forceinline__ u32x4 less(u32x4 q, float by) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) q[j] = __float_as_uint(__uint_as_float(q[j]) - by);
+    return q;
+  }
 };
 
-// E: logits per lane and piece
+// A wavefront's n largest logits and its sum of exponentials.
+struct RunState {
+  Best best;
+  uint32_t last_hi = 0, last_lo = 0;                   // the n-th of them, 0: there are fewer
+  float ref = -INFINITY;                               // what the exponentials refer to
+  // Exponents are logit * log2(e) - ref2 with ref2 = ref * log2(e), whose rounding is below 2^-32 for |ref| < 2^20; `far` from there on, where logits are
+  // made differences to ref first (neighbours' differences are exact, and the others' exponentials 0) and ref2 is 0.
+  double sum = 0, ref2 = 0;
+  bool far = false;
+  bool bad = false;                                    // a NaN was there
+  // `most`: the lane's largest of what comes next.  The exponentials refer to the largest logit of the first piece that has any, or of one that is far above it.
+  __device__ __forceinline__ void refer(float most) {
+    if (__ballot(most > ref + 500.f || (ref == -INFINITY && most > ref)) == 0) return;
+    float top = most;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (ref > -INFINITY) sum *= pow2_64(((double)ref - top) * LOG2E);
+    ref = top;
+    far = __builtin_fabsf(ref) >= 1048576.f;
+    ref2 = far ? 0.0 : (double)ref * LOG2E;
+  }
+  // below it no lane's logit is among the n largest: at least n lanes have one that reaches it, or the list is full and ends with it
+  __device__ __forceinline__ float floor(float most, int n) const {
+    const uint32_t least = last_hi != 0 ? last_hi : nth_of_lanes(most > -INFINITY ? ordered(most + 0.f) : 0, n);
+    return least != 0 ? unordered(least) : -INFINITY;
+  }
+  // a logit per lane; at: its token
+  __device__ __forceinline__ void offer(float f, int at, float floor, int n, int lane) {
+    uint64_t m = __ballot(f >= floor && f > -INFINITY);
+    if (m == 0) return;
+    const uint32_t hi = ordered(f + 0.f), lo = ~(uint32_t)at;      // (-0 is 0)
+    m &= __ballot(hi > last_hi || (hi == last_hi && lo > last_lo));
+    while (m != 0) {
+      const int from = __builtin_ctzll(m);
+      best.insert(lane_value(hi, from), lane_value(lo, from), lane);
+      last_hi = lane_value(best.hi, n - 1);
+      last_lo = lane_value(best.lo, n - 1);
+      m &= ~(1ull << from) & __ballot(hi > last_hi || (hi == last_hi && lo > last_lo));
+    }
+  }
+};
+
+// E: logits per lane and piece.  Bound: 64-bit arithmetic, 15 instructions for an exponential.
+// Every piece asks for the same number of vectors, the next one's before this one is worked on, so that the compiler can count which have arrived:
+// behind the last vector it is that one once more.
 template <class T, int E>
 __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
-  constexpr int N = Vec<T>::N, NV = E / N, PIECE = 64 * E;
+  constexpr int N = Vec<T>::N, NV = E / N;
   const int lane = threadIdx.x & 63;
   const int item = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = item / s.parts, part = item - row * s.parts;
   if (row >= s.rows || (s.done && s.done[row] != 0)) return;
   const T* x = (const T*)s.logits + (int64_t)row * s.ld;
-  // vectors start on 16 bytes; the first may reach before the row
-  const int shift = (int)(((uintptr_t)x & 15) / sizeof(T));
-  const int begin = part * s.run - shift, end = min(begin + s.run, s.V);
-  auto load = [&](int p0, Vec<T> (&v)[NV]) {
+  // Runs, pieces and vectors are the same in every row, wherever it starts: rows of the same logits have the same sum, and equal candidates stay equal.
+  const int vecs = s.V / N, tail = s.V - vecs * N;
+  const int begin = part * s.run, end = min(begin + s.run, vecs);
+  RunState st;
+  if (part == 0 && tail > 0) {
+    const int at = vecs * N + lane;
+    const float f = lane < tail ? Vec<T>::one(x + at) : -INFINITY;
+    st.bad |= f != f;
+    st.refer(f);
+    if (st.ref > -INFINITY) st.sum += lane < tail ? pow2_64(((double)f - st.ref) * LOG2E) : 0.0;
+    st.offer(f, at, -INFINITY, s.n, lane);
+  }
+  const u32x4_anywhere* px = reinterpret_cast<const u32x4_anywhere*>(x);
+  u32x4 cur[NV], nxt[NV];
+  auto ask = [&](int v0, u32x4 (&v)[NV]) {
 #pragma unroll
-    for (int j = 0; j < NV; j++) {
-      const int i0 = p0 + (j * 64 + lane) * N;
-      if (p0 >= 0 && p0 + PIECE <= end) v[j].load(x + i0);
-      else v[j].load(x + i0, max(-i0, 0), end - i0);
-    }
+    for (int j = 0; j < NV; j++) v[j] = px[min(v0 + j * 64 + lane, vecs - 1)];
   };
-  Best best;
-  float ref = -INFINITY;
-  double sum = 0, ref2 = 0;                            // ref2: ref * log2(e)
-  bool bad = false;
-  Vec<T> cur[NV], nxt[NV];
-  load(begin, cur);
-  for (int p0 = begin; p0 < end; p0 += PIECE) {
-    if (p0 + PIECE < end) load(p0 + PIECE, nxt);
-    float most = -INFINITY;
+  if (begin < end) ask(begin, cur);
+  for (int v0 = begin; v0 < end; v0 += 64 * NV) {
+    ask(v0 + 64 * NV, nxt);
+    if (v0 + 64 * NV > end) {
+#pragma unroll
+      for (int j = 0; j < NV; j++)
+        if (v0 + j * 64 + lane >= end) cur[j] = u32x4{Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE};
+    }
+    // (a NaN comes through to `most`, and the comparisons below are false)
+    float top[NV], most = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; j++) {
       float f[N];
-      cur[j].floats(f);
+      Vec<T>::floats(cur[j], f);
+      top[j] = f[0];
 #pragma unroll
-      for (int e = 0; e < N; e += 2) {
-        bad |= __builtin_isunordered(f[e], f[e + 1]);
-        most = fmaxf(fmaxf(most, f[e]), f[e + 1]);
+      for (int e = 1; e < N; e++) top[j] = __builtin_elementwise_maximum(top[j], f[e]);
+      most = __builtin_elementwise_maximum(most, top[j]);
+    }
+    st.bad |= most != most;
+    st.refer(most);
+    const float floor = st.floor(most, s.n);
+    uint32_t which = 0;                                // vectors that hold candidates
+#pragma unroll
+    for (int j = 0; j < NV; j++) which |= __ballot(top[j] >= floor && top[j] > -INFINITY) != 0 ? 1u << j : 0u;
+    while (which != 0) {
+      const int j = __builtin_ctz(which);
+      which &= which - 1;
+      u32x4 v = cur[0];
+      float mine = top[0];
+#pragma unroll
+      for (int i = 1; i < NV; i++)
+        if (i == j) {
+          v = cur[i];
+          mine = top[i];
+        }
+      // one lane's vector at a time: a logit of it per lane
+      uint64_t m = __ballot(mine >= floor && mine > -INFINITY);
+      while (m != 0) {
+        const int from = __builtin_ctzll(m);
+        m &= m - 1;
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i] = lane_value(v[i], from);
+        const float f = Vec<T>::element(w, lane);
+        st.offer(lane < N ? f : -INFINITY, (v0 + j * 64 + from) * N + lane, floor, s.n, lane);
       }
     }
-    // the exponentials refer to the largest logit of the first piece that has any, or of one that is far above it
-    if (__ballot(most > ref + 500.f || (ref == -INFINITY && most > ref)) != 0) {
-      float top = most;
+    if (st.far) {
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      if (ref > -INFINITY) sum *= pow2_64(((double)ref - top) * LOG2E);
-      ref = top;
-      ref2 = (double)ref * LOG2E;
+      for (int j = 0; j < NV; j++) cur[j] = Vec<T>::less(cur[j], st.ref);
     }
-    if (ref > -INFINITY) {
+    if (st.ref > -INFINITY) {
 #pragma unroll
       for (int j = 0; j < NV; j++) {
         float f[N];
-        cur[j].floats(f);
+        Vec<T>::floats(cur[j], f);
 #pragma unroll
-        for (int e = 0; e < N; e++) sum += pow2_64(fma((double)f[e], LOG2E, -ref2));
-      }
-    }
-    // Candidates: at least n lanes have one that reaches `floor`, or the list is full and ends with it.
-    uint32_t last_hi = lane_value(best.hi, s.n - 1), last_lo = lane_value(best.lo, s.n - 1);
-    const uint32_t least = last_hi != 0 ? last_hi : nth_of_lanes(most > -INFINITY ? ordered(most + 0.f) : 0, s.n);
-    const float floor = least != 0 ? unordered(least) : -INFINITY;
-    if (__ballot(most >= floor && most > -INFINITY) != 0) {
-#pragma unroll 1
-      for (int j = 0; j < NV; j++) {
-        Vec<T> v = cur[0];
-#pragma unroll
-        for (int i = 1; i < NV; i++)
-          if (i == j) v = cur[i];
-        float f[N], top = -INFINITY;
-        v.floats(f);
-#pragma unroll
-        for (int e = 0; e < N; e += 2) top = fmaxf(fmaxf(top, f[e]), f[e + 1]);
-        if (__ballot(top >= floor) == 0) continue;
-#pragma unroll
-        for (int e = 0; e < N; e++) {
-          uint64_t m = __ballot(f[e] >= floor && f[e] > -INFINITY);
-          if (m == 0) continue;
-          const uint32_t hi = ordered(f[e] + 0.f);                              // (-0 is 0)
-          const uint32_t lo = ~(uint32_t)(p0 + (j * 64 + lane) * N + e);
-          m &= __ballot(hi > last_hi || (hi == last_hi && lo > last_lo));
-          while (m != 0) {
-            const int from = __builtin_ctzll(m);
-            best.insert(lane_value(hi, from), lane_value(lo, from), lane);
-            last_hi = lane_value(best.hi, s.n - 1);
-            last_lo = lane_value(best.lo, s.n - 1);
-            m &= ~(1ull << from) & __ballot(hi > last_hi || (hi == last_hi && lo > last_lo));
-          }
-        }
+        for (int e = 0; e < N; e++) st.sum += pow2_64(fma((double)f[e], LOG2E, -st.ref2));
       }
     }
 #pragma unroll
     for (int j = 0; j < NV; j++) cur[j] = nxt[j];
   }
+  double sum = st.sum;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-  if (__ballot(bad) != 0 || !(ref < INFINITY)) sum = __builtin_nan("");
+  if (__ballot(st.bad) != 0 || !(st.ref < INFINITY)) sum = __builtin_nan("");
   if (lane == 0) {
-    s.part_ref[item] = ref;
+    s.part_ref[item] = st.ref;
     s.part_sum[item] = sum;
   }
-  if (lane < s.n) s.part_key[(int64_t)item * s.n + lane] = make_uint2(best.hi, best.lo);
+  if (lane < s.n) s.part_key[(int64_t)item * s.n + lane] = make_uint2(st.best.hi, st.best.lo);
 }
 
-// Candidates by score, then by beam and token; one per lane, 0: none.
-struct Scored {
-  uint64_t score = 0;
-  uint32_t at = 0;                                     // ~(beam of the prompt * 2^20 + token)
-  __device__ __forceinline__ bool above(uint64_t s, uint32_t a) const { return score > s || (score == s && at > a); }
-  __device__ __forceinline__ void insert(uint64_t s, uint32_t a, int lane) {
-    const int to = lanes_in(__ballot(above(s, a)));
-    const uint32_t sh = from_lane_before((uint32_t)(score >> 32)), sl = from_lane_before((uint32_t)score), pa = from_lane_before(at);
-    if (lane == to) { score = s; at = a; }
-    if (lane > to) { score = (uint64_t)sh << 32 | sl; at = pa; }
-  }
-};
-__device__ __forceinline__ uint64_t lane_value64(uint64_t v, int lane) {
-  return (uint64_t)lane_value((uint32_t)(v >> 32), lane) << 32 | lane_value((uint32_t)v, lane);
-}
-
-// A wavefront's candidates (one per lane) into its list: was one added?
-__device__ __forceinline__ bool merge(Scored& best, uint64_t score, uint32_t at, int n, int lane) {
-  uint64_t last = lane_value64(best.score, n - 1);
-  uint32_t last_at = lane_value(best.at, n - 1);
-  const uint32_t floor = last == 0 ? nth_of_lanes((uint32_t)(score >> 32), n) : 0;      // (no full list yet)
-  uint64_t m = __ballot(score != 0 && (uint32_t)(score >> 32) >= floor && (score > last || (score == last && at > last_at)));
-  const bool added = m != 0;
-  while (m != 0) {
-    const int from = __builtin_ctzll(m);
-    best.insert(lane_value64(score, from), lane_value(at, from), lane);
-    last = lane_value64(best.score, n - 1);
-    last_at = lane_value(best.at, n - 1);
-    m &= ~(1ull << from) & __ballot(score > last || (score == last && at > last_at));
-  }
-  return added;
-}
-
+// One workgroup per prompt.  The n best candidates so far lie in LDS; with up to 256 more of them, a candidate's new place is the number of those
+// above it.  Bound: latency, of the first launch's results and of the steps that wait for each other.
 __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
   // a candidate's score is (logit - largest logit) - logarithm of the sum + score, in this order: the logits may be far from zero
   __shared__ double log_sum[BEAM_MOST];                // NaN: the beam offers nothing
   __shared__ float largest[BEAM_MOST], score_in[BEAM_MOST];
-  __shared__ uint64_t list_score[4 * 64];
-  __shared__ uint32_t list_at[4 * 64];
+  __shared__ uint64_t best_score[2][BEAM_MOST + 256 + 8];  // (double's order; 0: none)
+  __shared__ uint32_t best_at[2][BEAM_MOST + 256 + 8];     // ~(beam of the prompt * 2^20 + token): the larger, the earlier
+  __shared__ uint32_t floors[4];
+  __shared__ int added;
   constexpr int AHEAD = 4;                             // candidates of a list that are asked for at once
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int prompt = blockIdx.x, row0 = prompt * s.beams;
@@ -262,6 +283,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     const int w = w0 + (int)threadIdx.x / 16, sub = threadIdx.x & 15;
     const bool in = w < s.beams && !(s.done && s.done[row0 + w] != 0);      // (an ended beam's logits were not looked at)
     const int64_t item = (int64_t)(row0 + w) * s.parts;
+    const float score = w < s.beams ? s.score[row0 + w] : 0.f;
     float top = -INFINITY;
     double sum = 0;
     bool bad = false;
@@ -286,7 +308,6 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
       wrong |= __shfl_xor(wrong, d);
     }
     if (sub == 0 && w < s.beams) {
-      const float score = s.score[row0 + w];
       const bool none = !in || wrong || !(most > -INFINITY) || !(__builtin_fabsf(score) < INFINITY);
       log_sum[w] = none ? __builtin_nan("") : log(sum);
       largest[w] = most;
@@ -294,7 +315,58 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     }
   }
   __syncthreads();
-  Scored best;
+  int have = 0, side = 0;                              // candidates in best_*[side], the best first
+  // a candidate per thread: was one added?
+  auto offer = [&](uint64_t score, uint32_t at) {
+    bool in;
+    if (threadIdx.x == 0) added = 0;
+    if (have == s.n) {
+      const uint64_t last = best_score[side][s.n - 1];
+      in = score > last || (score == last && score != 0 && at > best_at[side][s.n - 1]);
+      __syncthreads();
+    } else {
+      // n of a wavefront's candidates reach its floor: those below the highest of the four are not among the best
+      const uint32_t floor = nth_of_lanes((uint32_t)(score >> 32), s.n);
+      if (lane == 0) floors[wave] = floor;
+      __syncthreads();
+      in = score != 0 && (uint32_t)(score >> 32) >= max(max(floors[0], floors[1]), max(floors[2], floors[3]));
+    }
+    const uint64_t m = __ballot(in);
+    int to = 0;
+    if (lane == 0 && m != 0) to = atomicAdd(&added, lanes_in(m));
+    to = have + __builtin_amdgcn_readfirstlane(to) + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+    if (in) {
+      best_score[side][to] = score;
+      best_at[side][to] = at;
+    }
+    __syncthreads();
+    const int more = added, all = have + more;
+    if (more == 0) return false;
+    for (int i = threadIdx.x; i < all; i += 256) {
+      const uint64_t mine = best_score[side][i];
+      const uint32_t mine_at = best_at[side][i];
+      int place = 0;
+      for (int j0 = 0; j0 < all; j0 += 8) {            // (eight at a time are on their way; what lies behind the last one is not looked at)
+        uint64_t other[8];
+        uint32_t other_at[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          other[j] = best_score[side][j0 + j];
+          other_at[j] = best_at[side][j0 + j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j++) place += j0 + j < all && (other[j] > mine || (other[j] == mine && other_at[j] > mine_at));
+      }
+      if (place < s.n) {
+        best_score[side ^ 1][place] = mine;
+        best_at[side ^ 1][place] = mine_at;
+      }
+    }
+    __syncthreads();
+    side ^= 1;
+    have = min(all, s.n);
+    return true;
+  };
   for (int l0 = 0; l0 < lists; l0 += 256) {
     const int l = l0 + lane * 4 + wave, w = min(l / s.parts, s.beams - 1);
     const double less = log_sum[w];
@@ -303,55 +375,39 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     auto step = [&](uint2 k) {
       uint64_t score = 0;
       if (some && k.x != 0) score = ordered(((double)unordered(k.x) - largest[w] - less) + score_in[w] + 0.0);
-      return merge(best, score, ~((uint32_t)w << 20 | ~k.y), s.n, lane);
+      return offer(score, ~((uint32_t)w << 20 | ~k.y));
     };
     bool more = true;
-#pragma unroll
-    for (int r = 0; r < AHEAD; r++)
-      if (more && r < s.n) more = step(key[r]);
-    for (int r = AHEAD; more && r < s.n; r++) more = step(l < lists ? keys[(int64_t)l * s.n + r] : make_uint2(0, 0));
+#pragma unroll 1
+    for (int r = 0; more && r < s.n; r++)
+      more = step(r == 0 ? key[0] : r == 1 ? key[1] : r == 2 ? key[2] : r == 3 ? key[3] : l < lists ? keys[(int64_t)l * s.n + r] : make_uint2(0, 0));
   }
-  if (s.done && wave == 0) {                           // an ended beam goes on with one token, at its score
-    const int w = lane;
+  if (s.done) {                                        // an ended beam goes on with one token, at its score
+    const int w = threadIdx.x;
     uint64_t score = 0;
-    if (w < s.beams && s.done[row0 + w] != 0 && __builtin_fabsf(s.score[row0 + w]) < INFINITY) score = ordered((double)s.score[row0 + w] + 0.0);
-    merge(best, score, ~((uint32_t)w << 20 | (uint32_t)s.done_token), s.n, lane);
+    if (w < s.beams && s.done[row0 + w] != 0 && __builtin_fabsf(score_in[w]) < INFINITY) score = ordered((double)score_in[w] + 0.0);
+    offer(score, ~((uint32_t)w << 20 | (uint32_t)s.done_token));
   }
-  list_score[wave * 64 + lane] = lane < s.n ? best.score : 0;
-  list_at[wave * 64 + lane] = best.at;
-  __syncthreads();
-  // A candidate's place is the number of those above it, in the four lists
-  const uint64_t mine = list_score[threadIdx.x];
-  const uint32_t at = list_at[threadIdx.x];
-  int place = 0, all = 0;
-  for (int l = 0; l < 4; l++)
-    for (int i = 0; i < s.n; i++) {
-      const uint64_t other = list_score[l * 64 + i];
-      place += other > mine || (other == mine && list_at[l * 64 + i] > at);
-      all += other != 0;
-    }
-  const int64_t o = (int64_t)prompt * s.n;
-  if (mine != 0 && place < s.n) {
-    s.parent[o + place] = row0 + (int)(~at >> 20);
-    s.token[o + place] = (int)(~at & 0xfffffu);
-    s.score_out[o + place] = (float)unordered(mine);
-  }
-  if ((int)threadIdx.x < s.n && (int)threadIdx.x >= all) {
-    s.parent[o + threadIdx.x] = s.token[o + threadIdx.x] = -1;
-    s.score_out[o + threadIdx.x] = -INFINITY;
+  if ((int)threadIdx.x < s.n) {
+    const int64_t o = (int64_t)prompt * s.n + threadIdx.x;
+    const bool some = (int)threadIdx.x < have;
+    const uint32_t at = some ? ~best_at[side][threadIdx.x] : 0;
+    s.parent[o] = some ? row0 + (int)(at >> 20) : -1;
+    s.token[o] = some ? (int)(at & 0xfffffu) : -1;
+    s.score_out[o] = some ? (float)unordered(best_score[side][threadIdx.x]) : -INFINITY;
   }
 }
 
 // A run for a wavefront: pieces of 512 logits where those of 2048 are too few for the chip, else as many as give every SIMD four wavefronts.
-struct Runs { int elems; int64_t run, parts; };
-Runs runs_of(int64_t rows, int64_t V) {
-  const int64_t span = V + 7;                          // (a row may start up to 7 logits behind 16 bytes)
-  const int elems = rows * ((span + 2047) / 2048) < 1024 ? 8 : 32;
-  const int64_t piece = 64 * elems, pieces = (span + piece - 1) / piece;
+struct Runs { int elems; int64_t run, parts; };        // run: in vectors of 16 bytes
+Runs runs_of(int64_t rows, int64_t V, int dt) {
+  const int64_t per_vec = dt == LR_BF16 ? 8 : 4;
+  const int elems = rows * ((V + 2047) / 2048) < 1024 ? 8 : 32;
+  const int64_t piece = 64 * elems, pieces = V >= piece ? (V + piece - 1) / piece : 1;
   int64_t parts = rows > 0 ? (4096 + rows - 1) / rows : 1;
   if (parts > pieces) parts = pieces;
   const int64_t per = (pieces + parts - 1) / parts;
-  return {elems, per * piece, (pieces + per - 1) / per};
+  return {elems, per * piece / per_vec, (pieces + per - 1) / per};
 }
 
 template <class T>
@@ -365,10 +421,11 @@ hipError_t launch_runs(const BeamSelect& s, int elems, int64_t items, hipStream_
 }  // namespace
 
 size_t beam_select_ws_bytes(int64_t rows, int64_t V, int64_t n) {
-  return (size_t)(rows * runs_of(rows, V).parts) * (sizeof(double) + (size_t)n * sizeof(uint2) + sizeof(float));
+  return (size_t)(rows * runs_of(rows, V, LR_BF16).parts)      // (the same for either type)
+         * (sizeof(double) + (size_t)n * sizeof(uint2) + sizeof(float));
 }
 hipError_t k_beam_select(BeamSelect s, int dt, void* ws, hipStream_t st) {
-  const Runs r = runs_of(s.rows, s.V);
+  const Runs r = runs_of(s.rows, s.V, dt);
   s.parts = (int)r.parts;
   s.run = (int)r.run;
   const int64_t items = (int64_t)s.rows * s.parts;
