@@ -11,13 +11,14 @@ namespace lrb {
 namespace {
 
 constexpr int UNIT = 16;                   // elements of a lane at a time: 16 bytes of output
+typedef float f32x4_anywhere __attribute__((ext_vector_type(4), aligned(4)));      // (fp32 rows may start at any element)
 
 // 16 elements as they are stored, and as floats
 template <class T> struct Unit;
 template <> struct Unit<uint16_t> {
   uint4 v[2];
   // n of them are there (a multiple of 8)
-  __device__ __forceinline__ void load(const uint16_t* p, int n, bool) {
+  __device__ __forceinline__ void load(const uint16_t* p, int n) {
     v[0] = *reinterpret_cast<const uint4*>(p);
     v[1] = make_uint4(0, 0, 0, 0);
     if (n > 8) v[1] = *reinterpret_cast<const uint4*>(p + 8);
@@ -39,10 +40,14 @@ template <> struct Unit<uint16_t> {
 };
 template <> struct Unit<float> {
   float v[UNIT];
-  __device__ __forceinline__ void load(const float* p, int n, bool vec) {
-    if (vec && n >= UNIT) {
+  __device__ __forceinline__ void load(const float* p, int n) {
+    if (n >= UNIT) {
 #pragma unroll
-      for (int j = 0; j < UNIT; j += 4) *reinterpret_cast<float4*>(v + j) = *reinterpret_cast<const float4*>(p + j);
+      for (int j = 0; j < UNIT; j += 4) {
+        const f32x4_anywhere w = *reinterpret_cast<const f32x4_anywhere*>(p + j);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[j + e] = w[e];
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < UNIT; j++) v[j] = j < n ? p[j] : 0.f;
@@ -62,7 +67,7 @@ template <> struct Unit<float> {
 
 // TPR threads per row, NU units of 16 elements in a thread's registers; longer rows are read twice.  ACT (fp32): silu first.
 template <class T, int TPR, int NU, bool ACT>
-__global__ __launch_bounds__(256) void quant_rows_kernel(const T* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t rows, int64_t n, int vec) {
+__global__ __launch_bounds__(256) void quant_rows_kernel(const T* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t rows, int64_t n) {
   constexpr int RPB = 256 / TPR;
   __shared__ uint32_t part[4];
   const int tid = threadIdx.x % TPR;
@@ -75,7 +80,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* x, int64_t ldx
     uint32_t most = 0;
     auto take = [&](int64_t u, Unit<T>& v) {
       const int64_t left = n - u * UNIT;
-      v.load(px + u * UNIT, (int)(left < UNIT ? left : UNIT), vec != 0);
+      v.load(px + u * UNIT, (int)(left < UNIT ? left : UNIT));
     };
     auto act = [&](Unit<T>& v) {
       if constexpr (ACT) {
@@ -136,10 +141,9 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* x, int64_t ldx
 
 template <class T, bool ACT>
 hipError_t launch(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t rows, int64_t n, hipStream_t st) {
-  const int vec = ((uintptr_t)x & 15) == 0 && ldx * sizeof(T) % 16 == 0;
   auto run = [&](auto kern, int64_t rpb) {
     const int64_t blocks = (rows + rpb - 1) / rpb;
-    hipLaunchKernelGGL(kern, dim3((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(256), 0, st, (const T*)x, ldx, q, ldq, scale, rows, n, vec);
+    hipLaunchKernelGGL(kern, dim3((uint32_t)(blocks < (1 << 20) ? blocks : 1 << 20)), dim3(256), 0, st, (const T*)x, ldx, q, ldq, scale, rows, n);
     return hipGetLastError();
   };
   // us, one wavefront a row / four: 16384 x 1024 fp32 14.1 / 22.4, 16 x 4096 6.3 / 3.5, 16384 x 4096 79 / 53
