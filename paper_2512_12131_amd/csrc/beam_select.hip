@@ -131,10 +131,11 @@ struct RunState {
     far = __builtin_fabsf(ref) >= 1048576.f;
     ref2 = far ? 0.0 : (double)ref * LOG2E;
   }
-  // below it no lane's logit is among the n largest: at least n lanes have one that reaches it, or the list is full and ends with it
-  __device__ __forceinline__ float floor(float most, int n) const {
-    const uint32_t least = last_hi != 0 ? last_hi : nth_of_lanes(most > -INFINITY ? ordered(most + 0.f) : 0, n);
-    return least != 0 ? unordered(least) : -INFINITY;
+  // below it no lane's logit is among the row's n largest: at least n lanes have one that reaches it, or the list is full and ends with it, or
+  // another run of the row says so (`known`, 0: none did)
+  __device__ __forceinline__ uint32_t floor(float most, uint32_t known, int n) const {
+    known = max(known, last_hi);
+    return known != 0 ? known : nth_of_lanes(most > -INFINITY ? ordered(most + 0.f) : 0, n);
   }
   // a logit per lane; at: its token
   __device__ __forceinline__ void offer(float f, int at, float floor, int n, int lane) {
@@ -161,6 +162,11 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
   const int lane = threadIdx.x & 63;
   const int item = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = item / s.parts, part = item - row * s.parts;
+  // the floors of the workgroup's rows: what falls below any run's cannot be among the row's n largest
+  __shared__ uint32_t floors[4];
+  if (threadIdx.x < 4) floors[threadIdx.x] = 0;
+  __syncthreads();
+  uint32_t* known = floors + (row - (int)blockIdx.x * 4 / s.parts);
   if (row >= s.rows || (s.done && s.done[row] != 0)) return;
   const T* x = (const T*)s.logits + (int64_t)row * s.ld;
   // Runs, pieces and vectors are the same in every row, wherever it starts: rows of the same logits have the same sum, and equal candidates stay equal.
@@ -202,7 +208,8 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
     }
     st.bad |= most != most;
     st.refer(most);
-    const float floor = st.floor(most, s.n);
+    const uint32_t least = st.floor(most, __hip_atomic_load(known, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP), s.n);
+    const float floor = least != 0 ? unordered(least) : -INFINITY;
     uint32_t which = 0;                                // vectors that hold candidates
 #pragma unroll
     for (int j = 0; j < NV; j++) which |= __ballot(top[j] >= floor && top[j] > -INFINITY) != 0 ? 1u << j : 0u;
@@ -229,6 +236,7 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
         st.offer(lane < N ? f : -INFINITY, (v0 + j * 64 + from) * N + lane, floor, s.n, lane);
       }
     }
+    if (lane == 0) __hip_atomic_fetch_max(known, max(least, st.last_hi), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     if (st.far) {
 #pragma unroll
       for (int j = 0; j < NV; j++) cur[j] = Vec<T>::less(cur[j], st.ref);
