@@ -112,7 +112,8 @@ def test_fork_writes_rows_of_wider_tables_and_reuses_results():
 
 
 @pytest.mark.parametrize("pages,live,batch,cols", [(1, 1.0, 1, 1), (1, 0.0, 0, 1), (2, 0.5, 1, 2), (7, 0.5, 2, 3), (1000, 0.5, 8, 70), (2048, 1.0, 3, 10), (4096, 0.5, 4, 2000),
-                                                   (4097, 0.02, 2, 50), (5000, 0.98, 2, 5000), (70001, 0.3, 64, 333)])
+                                                   (4097, 0.02, 2, 50), (5000, 0.98, 2, 5000), (16383, 0.6, 3, 900), (16384, 1.0, 2, 40), (16384, 0.4, 2, 2000), (16385, 0.5, 5, 700),
+                                                   (70001, 0.3, 64, 333)])
 def test_compact(pages, live, batch, cols):
     rng = np.random.default_rng(pages)
     refs = (rng.random(pages) < live) * rng.integers(1, 4, pages)
