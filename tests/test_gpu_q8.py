@@ -186,3 +186,49 @@ def test_linear_q8_rows_apart_and_workspace():
     with pytest.raises(B.LrError):
         B.lr_linear_q8_fwd(x, wd, sd, wu, su, ws=ws[:nb - 1])
     assert B.lr_linear_q8_fwd(x[:0], wd, sd, wu, su).shape == (0, n) and B.lr_quant_rows(x[:0])[0].shape == (0, d)
+
+
+@pytest.mark.parametrize("T", [1, 16, 130])
+def test_captured_layers_share_a_workspace(T):
+    """Two captured layers on one workspace, replayed in turn on other tokens with eager calls between; then one on another stream."""
+    g = gen(30 + T)
+    layers = []
+    for d, r, n, dtype in ((512, 128, 264, BF), (1000, 72, 512, F32)):
+        layers.append(((randn(g, T, d) * 2).to(dtype), *B.lr_quant_rows(randn(g, r, d)), *B.lr_quant_rows(randn(g, n, r))))
+    nb = max(B.lr_linear_q8_workspace_bytes(T, w[0].shape[1], w[1].shape[0]) for w in layers)
+    ws = torch.full((nb + 256,), 77, dtype=torch.uint8, device=DEV)
+    outs = [B.lr_linear_q8_fwd(*w, ws=ws[:nb]) for w in layers]
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in layers]
+    for graph, w, y in zip(graphs, layers, outs):
+        with torch.cuda.graph(graph):
+            B.lr_linear_q8_fwd(*w, y=y, ws=ws[:nb])
+    for turn in range(3):
+        for graph, w, y in zip(graphs, layers, outs):
+            w[0].copy_(randn(g, *w[0].shape) * (turn + 1))
+            graph.replay()
+            want = B.lr_linear_q8_fwd(*w)
+            torch.cuda.synchronize()
+            assert torch.equal(y, want), turn
+    assert bool((ws[nb:] == 77).all())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        q, s = B.lr_quant_rows(layers[0][0])
+        got = B.lr_linear_q8_fwd(*layers[0]), B.lr_matmul_q8(q, s, layers[0][1], layers[0][2])
+    side.synchronize()
+    q, s = B.lr_quant_rows(layers[0][0])
+    assert torch.equal(got[0], B.lr_linear_q8_fwd(*layers[0])) and torch.equal(got[1], B.lr_matmul_q8(q, s, layers[0][1], layers[0][2]))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [3, 90])
+def test_tokens_that_are_no_numbers_stay_alone(T, dtype):
+    """A token with an infinity or a NaN gives NaN, in every column of its own row; a token of zeros gives zeros."""
+    g = gen(T)
+    x = randn(g, T, 264).to(dtype)
+    w = (*B.lr_quant_rows(randn(g, 72, 264)), *B.lr_quant_rows(randn(g, 136, 72)))
+    want = B.lr_linear_q8_fwd(x, *w)
+    x[0, 100], x[1, 7], x[2] = float("inf"), float("nan"), 0
+    got = B.lr_linear_q8_fwd(x, *w)
+    assert got[:2].isnan().all() and not got[2].any() and torch.equal(got[3:], want[3:])
