@@ -411,7 +411,7 @@ int lr_kv_copy(const lr_kv_cache* cache, const int32_t* src, const int32_t* dst,
  * a beam with done != 0 has ended; its one candidate is done_token at its score, its logits are not read.  Logits of -infinity are no candidates; a beam whose
  * score is no finite number, or whose logits hold a NaN, +infinity or nothing above -infinity, has none.  Where there are fewer than n: parent and token
  * -1, score -infinity.  beams and n at most 64, V at most 2^20, batch * beams at most 2^20 (LR_EUNSUPPORTED).  Rows may start on any
- * element.                                                                                                                          */
+ * element.  No output overlaps an input or another one, but score_out may be score itself where n = beams.                           */
 size_t lr_beam_select_workspace_bytes(int64_t batch, int64_t beams, int64_t V, int64_t n);
 int lr_beam_select(const void* logits, int64_t ldl, const float* score, const int32_t* done, int64_t done_token, int32_t* parent, int32_t* token,
                    float* score_out, int64_t batch, int64_t beams, int64_t V, int64_t n, int dt, void* ws, size_t ws_bytes, void* stream);
@@ -424,7 +424,7 @@ int lr_beam_select(const void* logits, int64_t ldl, const float* score, const in
 int lr_quant_rows(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int64_t T, int64_t n, int dt, void* stream);
 /* c[m, n] = sa[m] * sb[n] * sum_k a[m, k] * b[n, k], the sum exact, the product in fp32 (the row's scale first), rounded to dt.  a [M, lda], b [N, ldb]: rows
  * start on 16 bytes (pointers and strides multiples of 16) and can be read up to the next multiple of 16 columns, whatever is there.  c [M, ldc]: rows start on 16
- * bytes; N is any.  K at most 133144 (2^31 / 127^2), lda and ldb at most 2^22, ldc 2^20 (LR_EUNSUPPORTED).                                       */
+ * bytes; N is any.  K at most 131071 (2^31 / 128^2), lda and ldb at most 2^22, ldc 2^20 (LR_EUNSUPPORTED).                                       */
 int lr_matmul_q8(const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb, void* c, int64_t ldc, int64_t M,
                  int64_t N, int64_t K, int dt, void* stream);
 /* The forward of one bottleneck layer with both weights in 8 bits: y = Q(act(Q(x) . W_down^T)) . W_up^T, Q = lr_quant_rows and back; z and act(z) are

@@ -1681,6 +1681,13 @@ int lr_beam_select(const void* logits, int64_t ldl, const float* score, const in
   if ((uintptr_t)logits & (dt == LR_BF16 ? 1 : 3)) return LR_EALIGN;
   TRY(check_lists({score, parent, token, score_out}));
   if ((uintptr_t)done & 3) return LR_EALIGN;
+  // (a prompt's scores are read before its new ones are written)
+  const auto list = [](const void* p, int64_t n) { return span_of(p, 1, n, n); };
+  const int64_t rows = batch * beams, es = dt == LR_BF16 ? 2 : 4;
+  const Span rows_in{(uintptr_t)logits, (uintptr_t)logits + (size_t)((rows - 1) * ldl + V) * es};
+  if (!apart({list(parent, batch * n), list(token, batch * n), list(score_out, batch * n)},
+             {rows_in, list(score, score_out == score && n == beams ? 0 : rows), list(done, done ? rows : 0)}))
+    return LR_EINVAL;
   TRY(check_ws(ws, ws_bytes, beam_select_ws_bytes(batch * beams, V, n)));
   BeamSelect s{};
   s.logits = logits; s.ld = ldl; s.score = score; s.done = done; s.done_token = (int)done_token;
@@ -1690,8 +1697,8 @@ int lr_beam_select(const void* logits, int64_t ldl, const float* score, const in
 }
 
 // ---- products of 8-bit integers --------------------------------------------------------------------
-// (offsets inside a tile of 256 rows are formed in 32 bits)
-constexpr int64_t Q8_K_MOST = 133144, Q8_LD_MOST = (int64_t)1 << 22, Q8_LDC_MOST = (int64_t)1 << 20;
+// (K products of -128 and -128 are below 2^31; offsets inside a tile of 256 rows are formed in 32 bits)
+constexpr int64_t Q8_K_MOST = 131071, Q8_LD_MOST = (int64_t)1 << 22, Q8_LDC_MOST = (int64_t)1 << 20;
 
 static int check_quant(const void* x, int64_t ldx, int64_t T, int64_t n, int dt) {
   TRY(check_dt(dt));

@@ -147,3 +147,14 @@ def test_shared_workspace_graphs_and_streams():
         got = B.lr_beam_select(a[0], a[1], 8)
     side.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(got, B.lr_beam_select(a[0], a[1], 8)))
+
+
+def test_scores_are_written_over_the_old_ones():
+    """score itself as the new scores, where each prompt has as many."""
+    logits, score = make(40, 6, 3001, BF, 31)
+    want = B.lr_beam_select(logits, score)
+    out = (torch.empty_like(want[0]), torch.empty_like(want[1]), score)
+    got = B.lr_beam_select(logits, score, out=out)
+    assert got[2].data_ptr() == score.data_ptr() and all(torch.equal(a, b) for a, b in zip(got, want))
+    with pytest.raises(B.LrError):
+        B.lr_beam_select(logits[:120], score[:20], out=tuple(t.view(40, 6)[10:30] for t in out))

@@ -127,13 +127,13 @@ def test_matmul_q8_writes_its_columns_alone(M, N):
 
 
 def test_matmul_q8_largest_sums_and_scales_that_are_no_numbers():
-    a = torch.full((40, 133136), 127, dtype=torch.int8, device=DEV)
-    b = a[:33].clone()
-    b[1] = -127
+    a = torch.full((40, 131072), -128, dtype=torch.int8, device=DEV)[:, :131071]
+    b = torch.full((33, 131072), -128, dtype=torch.int8, device=DEV)[:, :131071]
+    b[1] = 127
     one = torch.ones(40, device=DEV)
     got = B.lr_matmul_q8(a, one, b, one[:33], dtype=F32)
-    want = torch.full((33,), 133136.0 * 127 * 127, dtype=torch.float64, device=DEV)
-    want[1] *= -1
+    want = torch.full((33,), 131071.0 * 128 * 128, dtype=torch.float64, device=DEV)
+    want[1] *= -127 / 128
     assert bool(((got.double() - want).abs() <= 2.0 ** -24 * want.abs()).all())
     x = randn(gen(1), 4, 64)
     x[2, 3] = float("nan")

@@ -99,7 +99,7 @@ def test_matmul_q8_refuses():
         assert _matmul(**args) == EINVAL, args
     for args in (dict(lda=72), dict(ldb=72), dict(a=0x10008), dict(b=0x30004), dict(c=0x50008), dict(ldc=36), dict(sa=0x20001)):
         assert _matmul(**args) == EALIGN, args
-    for args in (dict(K=133145, lda=133152, ldb=133152), dict(lda=(1 << 22) + 16), dict(M=1 << 30, N=1 << 20, ldc=1 << 20)):
+    for args in (dict(K=133145, lda=133152, ldb=133152), dict(K=131072, lda=131072, ldb=131072), dict(lda=(1 << 22) + 16), dict(M=1 << 30, N=1 << 20, ldc=1 << 20)):
         assert _matmul(**args) == EUNSUPPORTED, args
     assert _matmul(M=0, a=None, c=None) == 0
 
@@ -129,14 +129,15 @@ def _select(logits=0x10000, ldl=100, score=0x20000, done=None, end=0, parent=0x3
 
 def test_beam_select_refuses():
     for args in (dict(batch=-1), dict(beams=0), dict(V=0), dict(n=0), dict(ldl=99), dict(dt=2), dict(logits=None), dict(score=None), dict(parent=None),
-                 dict(token=None), dict(best=None), dict(done=0x1000, end=100), dict(done=0x1000, end=-1)):
+                 dict(token=None), dict(best=None), dict(done=0x1000, end=100), dict(done=0x1000, end=-1), dict(parent=0x10000), dict(parent=0x1063c), dict(best=0x20004),
+                 dict(best=0x20000, n=3), dict(token=0x30010), dict(done=0x40004)):
         assert _select(**args) == EINVAL, args
     for args in (dict(logits=0x10001), dict(logits=0x10002, dt=F32), dict(done=0x1002), dict(score=0x20002), dict(ws=0x60010)):
         assert _select(**args) == EALIGN, args
     for args in (dict(beams=65), dict(n=65), dict(V=(1 << 20) + 1, ldl=1 << 21), dict(batch=(1 << 18) + 1)):
         assert _select(**args) == EUNSUPPORTED, args
     need = B.lr_beam_select_workspace_bytes(2, 4, 100, 4)
-    assert need > 0 and _select(nb=need - 1) == EWORKSPACE and _select(ws=None) == EWORKSPACE
+    assert need > 0 and _select(nb=need - 1) == EWORKSPACE and _select(ws=None) == EWORKSPACE and _select(best=0x20000, ws=None) == EWORKSPACE
     assert _select(batch=0, logits=None, ws=None) == 0 and B.lr_beam_select_workspace_bytes(2, 65, 100, 4) == 0
 
 
