@@ -1780,15 +1780,20 @@ int lr_linear_q8_fwd(const void* x, int64_t ldx, const int8_t* w_down, int64_t l
   const LinearQ8 p = linear_q8_parts(c, T, d_in, r);
   Q8Op down{p.qx, w_down, p.sx, s_down, p.z, p.ldx, ld_down, p.ldz, (int)T, (int)r, (int)d_in, LR_F32};
   Q8Op up{p.qa, w_up, p.sz, s_up, y, p.ldz, ld_up, ldy, (int)T, (int)d_out, (int)r, dt};
-  // few rows: the first product writes act(z), the second one quantises that itself
+  // few rows: the first product writes act(z), the second one quantises that itself, and the first one x where it has few elements
   const bool few = gemm_q8_acts(down) && gemm_q8_quantises(T, d_out, r);
-  LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));
   if (few) {
     down.act = act;
-    LAUNCH(c, gemm_q8(down, c.st));
-    LAUNCH(c, gemm_q8_from(up, p.z, p.ldz, c.st));
+    if (gemm_q8_quantises(T, r, d_in) && T * d_in <= Q8_FEW_ELEMENTS) {
+      LAUNCH(c, gemm_q8_from(down, x, ldx, dt, c.st));
+    } else {
+      LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));
+      LAUNCH(c, gemm_q8(down, c.st));
+    }
+    LAUNCH(c, gemm_q8_from_ours(up, p.z, p.ldz, c.st));
     return status_of(c);
   }
+  LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));
   LAUNCH(c, gemm_q8(down, c.st));
   LAUNCH(c, k_quant_rows(p.z, p.ldz, p.qa, p.ldz, p.sz, T, r, act, LR_F32, c.st));
   LAUNCH(c, gemm_q8(up, c.st));

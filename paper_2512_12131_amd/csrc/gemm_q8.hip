@@ -423,15 +423,30 @@ hipError_t launch_q8_big(const Q8Op& op, hipStream_t st) {
 // A workgroup takes 16 rows and NT * 16 columns over all of k: A and B lie in LDS as they are (up to `chunk` k at a time), its 16 wavefronts take every
 // 16th step of 64 k each (v_mfma_i32_16x16x64_i8) and the 16 sums are added up through LDS.
 //
-// OURS: A is fp32, the activations of a layer's first product, which every workgroup quantises for itself, a wavefront a row: it holds the row (of up to
-// 64 * 4 * OURS columns) in registers, whose largest element needs no other wavefront.  Bound: the way in and out of a launch, and what a CU takes in.
-// The layer 4096 -> 1024 -> 4096 of 16 tokens, us: 12.1 so, 13.0 with a launch for the quantisation between the products; with the bf16 rows
-// quantised by the first product too (128 KB for each of 64 workgroups) 12.9.
+// OURS: A comes as rows of type KIND, which every workgroup quantises for itself, a wavefront a row: it holds the row (of up to 64 * 4 * OURS columns) in
+// registers, whose largest element needs no other wavefront.  Bound: the way in and out of a launch, and what a CU takes in.
+// The layer 4096 -> 1024 -> 4096 of 16 tokens, us: 12.1 so in its second product, 13.0 with a launch for the quantisation between the products.  In the first
+// product, where every workgroup does the rows' whole work, up to 2^15 elements: of 1 / 8 / 16 tokens, with a launch before it, 10.6 / 11.4 / 12.1, without
+// 9.1 / 10.3 / 12.4; 1024 -> 256 -> 1024 7.8 / 8.1 / 8.5 and 5.6 / 6.0 / 6.7; 4096 -> 4096 -> 4096 in fp32 14.7 / 16.3 / 17.3 and 13.3 / 15.9 / 17.9.
 constexpr int R16_W = 16, R16_SLICE = 2048, R16_LDS = 160 * 1024;
 constexpr int rows16_lds(int chunk, int nt) { return chunk / 128 * R16_SLICE * (1 + nt) + R16_W * nt * 1024; }
 
-template <int OURS, int NT, int OUT, bool TAIL>
-__global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const float* x, int64_t ldx, int chunk) {
+// four elements of a row, as they are stored (fp32 rows may start anywhere) and as floats
+typedef float f32x4_anywhere __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <Rows KIND> struct Four { typedef f32x4_anywhere In; typedef f32x4 V; typedef float X; };
+template <> struct Four<Rows::BF16> { typedef u32x2_t In, V; typedef uint16_t X; };
+__device__ __forceinline__ void floats_of(const f32x4& v, float* f) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) f[e] = v[e];
+}
+__device__ __forceinline__ void floats_of(const u32x2_t& v, float* f) {
+#pragma unroll
+  for (int e = 0; e < 4; e++) f[e] = __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+}
+
+template <int OURS, Rows KIND, int NT, int OUT, bool TAIL>
+__global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const void* xs, int64_t ldx, int chunk) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float row_scale[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -476,32 +491,39 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const fl
     }
     if (tid < 16) row_scale[tid] = m0 + tid < op.M ? op.sa[m0 + tid] : 0.f;
   } else {
-    f32x4 v[OURS];
+    typename Four<KIND>::V v[OURS];
     const bool has = m0 + wave < op.M;
-    const float* px = x + (int64_t)(m0 + wave) * ldx;
+    using F = Four<KIND>;
+    const typename F::X* px = (const typename F::X*)xs + (int64_t)(m0 + wave) * ldx;
 #pragma unroll
     for (int i = 0; i < OURS; i++) {
       const int k = (i * 64 + lane) * 4;
-      v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (has && k < op.K) v[i] = *reinterpret_cast<const f32x4*>(px + k);
+      v[i] = typename F::V{};
+      if (has && k < op.K) v[i] = *reinterpret_cast<const typename F::In*>(px + k);
     }
     load(0);
-    uint32_t most = 0;
+    if (has) {                                         // (behind the last row anything: its products are not stored)
+      uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < OURS; i++)
+      for (int i = 0; i < OURS; i++) {
+        float f[4];
+        floats_of(v[i], f);
 #pragma unroll
-      for (int e = 0; e < 4; e++) most = max(most, __float_as_uint(v[i][e]) & 0x7fffffffu);
+        for (int e = 0; e < 4; e++) most = max(most, __float_as_uint(f[e]) & 0x7fffffffu);
+      }
 #pragma unroll
-    for (int d = 32; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    const Scale<Rows::OURS> sc(most);
-    if (lane == 0) row_scale[wave] = sc.scale;
-    const int sw = (wave >> 1) & 7;
+      for (int d = 32; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+      const Scale<KIND> sc(most);
+      if (lane == 0) row_scale[wave] = sc.scale;
+      const int sw = (wave >> 1) & 7;
 #pragma unroll
-    for (int i = 0; i < OURS; i++) {
-      const int k = (i * 64 + lane) * 4;
-      const float f[4] = {v[i][0], v[i][1], v[i][2], v[i][3]};
-      // (of a row without a scale anything: it is multiplied with NaN)
-      if (k < chunk) *reinterpret_cast<uint32_t*>(smem + (k >> 7) * R16_SLICE + wave * 128 + ((((k >> 4) & 7) ^ sw) << 4) + (k & 15)) = sc.bytes(f);
+      for (int i = 0; i < OURS; i++) {
+        const int k = (i * 64 + lane) * 4;
+        float f[4];
+        floats_of(v[i], f);
+        // (of a row without a scale anything: it is multiplied with NaN)
+        if (k < chunk) *reinterpret_cast<uint32_t*>(smem + (k >> 7) * R16_SLICE + wave * 128 + ((((k >> 4) & 7) ^ sw) << 4) + (k & 15)) = sc.bytes(f);
+      }
     }
     wait_vmcnt<0>();
     __syncthreads();
@@ -527,9 +549,9 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const fl
 // 16-column pieces of a workgroup that quantises its rows: as many as leave about a workgroup per CU
 int rows16_nt(int64_t N) { return N <= 256 * 16 ? 1 : N <= 512 * 16 ? 2 : 4; }
 
-template <int OURS, int NT, int OUT, bool TAIL>
-hipError_t launch_rows16_nt(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
-  auto kern = q8_rows16_kernel<OURS, NT, OUT, TAIL>;
+template <int OURS, Rows KIND, int NT, int OUT, bool TAIL>
+hipError_t launch_rows16_nt(const Q8Op& op, const void* x, int64_t ldx, hipStream_t st) {
+  auto kern = q8_rows16_kernel<OURS, KIND, NT, OUT, TAIL>;
   // one-time opt-in to more than 64 KB of dynamic LDS (thread-safe function-local static)
   static const hipError_t attr_err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, R16_LDS - 256);
   if (attr_err != hipSuccess) return attr_err;
@@ -541,13 +563,17 @@ hipError_t launch_rows16_nt(const Q8Op& op, const float* x, int64_t ldx, hipStre
   hipLaunchKernelGGL(kern, grid, dim3(R16_W * 64), rows16_lds(chunk, NT), st, op, x, ldx, chunk);
   return hipGetLastError();
 }
-template <int OURS, int OUT>
-hipError_t launch_rows16_ours(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
+template <int OURS, Rows KIND, int OUT>
+hipError_t launch_rows16_of(const Q8Op& op, const void* x, int64_t ldx, hipStream_t st) {
   switch (rows16_nt(op.N)) {
-    case 1: return launch_rows16_nt<OURS, 1, OUT, false>(op, x, ldx, st);
-    case 2: return launch_rows16_nt<OURS, 2, OUT, false>(op, x, ldx, st);
-    default: return launch_rows16_nt<OURS, 4, OUT, false>(op, x, ldx, st);
+    case 1: return launch_rows16_nt<OURS, KIND, 1, OUT, false>(op, x, ldx, st);
+    case 2: return launch_rows16_nt<OURS, KIND, 2, OUT, false>(op, x, ldx, st);
+    default: return launch_rows16_nt<OURS, KIND, 4, OUT, false>(op, x, ldx, st);
   }
+}
+template <Rows KIND, int OUT>
+hipError_t launch_rows16_from(const Q8Op& op, const void* x, int64_t ldx, hipStream_t st) {
+  return op.K <= 1024 ? launch_rows16_of<4, KIND, OUT>(op, x, ldx, st) : launch_rows16_of<16, KIND, OUT>(op, x, ldx, st);
 }
 
 using R64x128 = RingTile<64, 128, 2, 2, 1, 3>;      // two workgroups per CU
@@ -563,7 +589,7 @@ hipError_t launch_q8(const Q8Op& op, int tile, hipStream_t st) {
     case Q8_R128: return launch_q8_ring<R128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64X128: return launch_q8_ring<R64x128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64: return launch_q8_ring<R64, OUT, EDGE, TAIL>(op, st);
-    default: return launch_rows16_nt<0, 1, OUT, TAIL>(op, nullptr, 0, st);
+    default: return launch_rows16_nt<0, Rows::OURS, 1, OUT, TAIL>(op, nullptr, 0, st);
   }
 }
 
@@ -603,10 +629,11 @@ bool gemm_q8_acts(const Q8Op& op) { return q8_tile(op) == Q8_ROWS16; }
 bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K) {
   return M <= 16 && K <= 4096 && K % 4 == 0 && rows16_lds((int)(K + 127) / 128 * 128, rows16_nt(N)) <= R16_LDS - 256;
 }
-hipError_t gemm_q8_from(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
-  const bool narrow = op.K <= 1024;
-  if (op.dt == LR_BF16) return narrow ? launch_rows16_ours<4, LR_BF16>(op, x, ldx, st) : launch_rows16_ours<16, LR_BF16>(op, x, ldx, st);
-  return narrow ? launch_rows16_ours<4, LR_F32>(op, x, ldx, st) : launch_rows16_ours<16, LR_F32>(op, x, ldx, st);
+hipError_t gemm_q8_from_ours(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
+  return op.dt == LR_BF16 ? launch_rows16_from<Rows::OURS, LR_BF16>(op, x, ldx, st) : launch_rows16_from<Rows::OURS, LR_F32>(op, x, ldx, st);
+}
+hipError_t gemm_q8_from(const Q8Op& op, const void* x, int64_t ldx, int dt, hipStream_t st) {
+  return dt == LR_BF16 ? launch_rows16_from<Rows::BF16, LR_F32>(op, x, ldx, st) : launch_rows16_from<Rows::F32, LR_F32>(op, x, ldx, st);
 }
 
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st) {

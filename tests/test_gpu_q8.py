@@ -185,6 +185,9 @@ def test_linear_q8_rows_apart_and_workspace():
     assert torch.equal(B.lr_linear_q8_fwd(x[31:33].contiguous(), wd, sd, wu, su), want[31:33])
     with pytest.raises(B.LrError):
         B.lr_linear_q8_fwd(x, wd, sd, wu, su, ws=ws[:nb - 1])
+    for some in (x[31:32], x[3:19], x[:40]):              # (as many forms as there are for few tokens and many)
+        y = B.lr_linear_q8_fwd(some, wd, sd, wu, su)
+        assert torch.equal(y, B.lr_linear_q8_fwd(x, wd, sd, wu, su)[some.storage_offset() // x.stride(0):][:len(some)])
     assert B.lr_linear_q8_fwd(x[:0], wd, sd, wu, su).shape == (0, n) and B.lr_quant_rows(x[:0])[0].shape == (0, d)
 
 
@@ -232,3 +235,21 @@ def test_tokens_that_are_no_numbers_stay_alone(T, dtype):
     x[0, 100], x[1, 7], x[2] = float("inf"), float("nan"), 0
     got = B.lr_linear_q8_fwd(x, *w)
     assert got[:2].isnan().all() and not got[2].any() and torch.equal(got[3:], want[3:])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,r,n", [(1024, 256, 1024), (2048, 512, 264), (4096, 64, 136), (1000, 1000, 8), (104, 2048, 3000), (103, 72, 40)])
+def test_a_token_alone_and_among_others(d, r, n, dtype):
+    """Rows of a layer are the same bits, quantised by a launch of their own (17 tokens) or by the first product (a few), rows at any place in wider ones;
+    ties and numbers that are none among them."""
+    d += -d % 8 if dtype == BF else 0
+    g = gen(d + r)
+    wide = (randn(g, 17, d + 8) * 3).to(dtype)
+    x = wide[:, 8:] if dtype == BF else wide[:, 3:d + 3]
+    x[4, 9], x[5, 0], x[6] = float("nan"), -float("inf"), 0
+    x[2, d // 2] = x[2].abs().max() / 2
+    w = (*B.lr_quant_rows(randn(g, r, d)), *B.lr_quant_rows(randn(g, n, r)))
+    want = B.lr_linear_q8_fwd(x, *w)
+    bits = lambda t: t.contiguous().view(torch.int16 if dtype == BF else torch.int32)
+    for first, count in ((0, 1), (4, 1), (3, 2), (0, 8), (8, 5), (1, 16)):
+        assert torch.equal(bits(B.lr_linear_q8_fwd(x[first:first + count], *w)), bits(want[first:first + count])), (first, count)
