@@ -13,22 +13,38 @@ __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
 }
 
-// Sum of v over the workgroup's threads before this one, and over all of them.  scratch: one entry per wavefront, free again after the call.
+// v of the lane that a DPP control names, 0 where there is none
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t from_lane(int64_t v) {
+  return (int64_t)((uint64_t)(uint32_t)from_lane<CTRL, ROWS>((int)(v >> 32)) << 32 | (uint32_t)from_lane<CTRL, ROWS>((int)v));
+}
+// Sum of v over the lanes up to this one.
 template <class V>
-__device__ __forceinline__ V block_prefix(V v, V* scratch, V* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  V incl = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const V o = __shfl_up(incl, d);
-    if (lane >= d) incl += o;
-  }
+__device__ __forceinline__ V wave_prefix(V v) {
+  v += from_lane<0x111, 0xf>(v);      // row_shr:1, 2, 4, 8: within 16 lanes
+  v += from_lane<0x112, 0xf>(v);
+  v += from_lane<0x114, 0xf>(v);
+  v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v);      // row_bcast:15 into the second and fourth 16
+  v += from_lane<0x143, 0xc>(v);      // row_bcast:31 into the upper 32
+  return v;
+}
+
+// Sum of v over the workgroup's threads before this one, and over all of them.  scratch: one entry for each of its NW wavefronts, free again after the call.
+template <class V, int NW>
+__device__ __forceinline__ V block_prefix(V v, V (&scratch)[NW], V* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const V incl = wave_prefix(v);
   if (lane == 63) scratch[wave] = incl;
   __syncthreads();
   V before = 0, all = 0;
-  for (int w = 0; w < nw; w++) {
-    if (w < wave) before += scratch[w];
-    all += scratch[w];
+#pragma unroll
+  for (int w = 0; w < NW; w++) {
+    const V s = scratch[w];
+    before += w < wave ? s : 0;
+    all += s;
   }
   __syncthreads();
   *total = all;
@@ -69,6 +85,9 @@ __global__ __launch_bounds__(PLAN_T) void fork_plan_kernel(KvFork f) {
   }
   extern __shared__ int first[];          // [n_in] the first child of a parent, then [n_in] its children
   __shared__ int64_t scratch[PLAN_T / 64];
+  __shared__ int steps[PLAN_T / 64];
+  __shared__ unsigned long long beyond;   // pages that no column of the table is left for
+  if (tid == 0) beyond = 0;
   int* count = first + f.n_in;
   for (int p = tid; p < f.n_in; p += PLAN_T) {
     first[p] = 0x7fffffff;
@@ -83,7 +102,7 @@ __global__ __launch_bounds__(PLAN_T) void fork_plan_kernel(KvFork f) {
     }
   }
   __syncthreads();
-  int64_t want = 0, beyond = 0;           // fresh pages so far; pages that no column of the table is left for
+  int64_t want = 0;                       // fresh pages so far
   for (int i0 = 0; i0 < f.n_out; i0 += PLAN_T) {
     const int i = i0 + tid;
     int64_t need = 0, over = 0;
@@ -113,9 +132,9 @@ __global__ __launch_bounds__(PLAN_T) void fork_plan_kernel(KvFork f) {
     const int64_t at = want + block_prefix(need, scratch, &all);
     if (i < f.n_out) f.offset[i] = (int)min(at, (int64_t)f.n_pages);
     want += all;
-    block_prefix(over, scratch, &all);
-    beyond += all;
+    if (over > 0) atomicAdd(&beyond, (unsigned long long)over);
   }
+  __syncthreads();
   for (int p = tid; p < f.n_in; p += PLAN_T) {
     f.first[p] = first[p];
     f.count[p] = count[p];
@@ -132,17 +151,17 @@ __global__ __launch_bounds__(PLAN_T) void fork_plan_kernel(KvFork f) {
 #pragma unroll
       for (int j = 0; j < PLAN_PER; j++) r[j] = p + j < f.n_pages ? f.refs_in[p + j] : 1;
     }
-    int64_t mine = 0, all;
+    int mine = 0, all;
 #pragma unroll
     for (int j = 0; j < PLAN_PER; j++) mine += r[j] == 0;
-    int64_t at = found + block_prefix(mine, scratch, &all);
+    int64_t at = found + block_prefix(mine, steps, &all);
 #pragma unroll
     for (int j = 0; j < PLAN_PER; j++)
       if (r[j] == 0 && at < f.n_pages) f.fresh[at++] = (int)(p + j);
     found += all;
   }
   if (tid == 0) {
-    const int64_t lack = max(want - found, (int64_t)0) + beyond;
+    const int64_t lack = max(want - found, (int64_t)0) + (int64_t)beyond;
     *f.found = (int)min(found, (int64_t)f.n_pages);
     *f.missing = (int)min(lack, (int64_t)0x7fffffff);
   }
@@ -230,7 +249,7 @@ __device__ __forceinline__ int held_mask(const KvCompact& c, int64_t p) {      /
 __global__ __launch_bounds__(SPAN_T) void compact_count_kernel(KvCompact c) {
   __shared__ int scratch[SPAN_T / 64];
   int all;
-  block_prefix<int>(__popc(held_mask(c, (int64_t)blockIdx.x * SPAN + threadIdx.x * SPAN_PER)), scratch, &all);
+  block_prefix((int)__popc(held_mask(c, (int64_t)blockIdx.x * SPAN + threadIdx.x * SPAN_PER)), scratch, &all);
   if (threadIdx.x == 0) c.span_held[blockIdx.x] = all;
 }
 
@@ -250,7 +269,7 @@ __global__ __launch_bounds__(SPAN_T) void compact_lists_kernel(KvCompact c) {
     m = (int)(all >> shift) & ((1 << SPAN_PER) - 1);
     // three sums at once, of 20 bits each: of all, of the spans before this one, of this one
     int64_t total;
-    const int64_t below = block_prefix<int64_t>(__popcll(all) | (int64_t)__popcll(all & ((1ull << shift) - 1)) << 20 | (int64_t)__popc(m) << 40, sums, &total);
+    const int64_t below = block_prefix((int64_t)__popcll(all) | (int64_t)__popcll(all & ((1ull << shift) - 1)) << 20 | (int64_t)__popc(m) << 40, sums, &total);
     held = (int)(total & 0xfffff);
     rank = (int)(total >> 20 & 0xfffff) + (int)(below >> 40);
     int mine = 0;
@@ -280,7 +299,7 @@ __global__ __launch_bounds__(SPAN_T) void compact_lists_kernel(KvCompact c) {
     block_prefix(low, scratch, &all);
     low = all;
     m = held_mask(c, p);
-    rank = before + block_prefix<int>(__popc(m), scratch, &all);
+    rank = before + block_prefix((int)__popc(m), scratch, &all);
   }
   const int moves = held - low, room = (int)(c.n_pages / 2);
 #pragma unroll
