@@ -7,17 +7,14 @@
 // First launch: a wavefront takes a run of one beam's logits.  Within a beam the order of the scores is that of the logits, so it keeps the
 // n largest logits of the run, one per lane, and the sum of exponentials relative to the largest logit of its first piece.  Second launch:
 // a workgroup per prompt adds up the beams' sums and merges their lists by score.
-#include "common.h"
+#include "lanes.h"
 
 namespace lrb {
 namespace {
 
 __device__ __forceinline__ int lanes_in(uint64_t m) { return __popcll(m); }
-__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 // the value of the lane before (lane 0: its own)
-__device__ __forceinline__ uint32_t from_lane_before(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x138, 0xf, 0xf, false);      // wave_shr:1
-}
+__device__ __forceinline__ uint32_t from_lane_before(uint32_t v) { return from_lane<0x138, 0xf>(v, v); }      // wave_shr:1
 
 // Whole numbers in the order of floats (no NaN, no -0); all are above 0.
 __device__ __forceinline__ uint32_t ordered(float f) {
@@ -123,9 +120,7 @@ struct RunState {
   // `most`: the lane's largest of what comes next.  The exponentials refer to the largest logit of the first piece that has any, or of one that is far above it.
   __device__ __forceinline__ void refer(float most) {
     if (__ballot(most > ref + 500.f || (ref == -INFINITY && most > ref)) == 0) return;
-    float top = most;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float top = wave_max(most);
     if (ref > -INFINITY) sum *= pow2_64(((double)ref - top) * LOG2E);
     ref = top;
     far = __builtin_fabsf(ref) >= 1048576.f;
@@ -145,9 +140,9 @@ struct RunState {
     m &= __ballot(hi > last_hi || (hi == last_hi && lo > last_lo));
     while (m != 0) {
       const int from = __builtin_ctzll(m);
-      best.insert(lane_value(hi, from), lane_value(lo, from), lane);
-      last_hi = lane_value(best.hi, n - 1);
-      last_lo = lane_value(best.lo, n - 1);
+      best.insert(value_of_lane(hi, from), value_of_lane(lo, from), lane);
+      last_hi = value_of_lane(best.hi, n - 1);
+      last_lo = value_of_lane(best.lo, n - 1);
       m &= ~(1ull << from) & __ballot(hi > last_hi || (hi == last_hi && lo > last_lo));
     }
   }
@@ -231,7 +226,7 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
         m &= m - 1;
         u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; i++) w[i] = lane_value(v[i], from);
+        for (int i = 0; i < 4; i++) w[i] = value_of_lane(v[i], from);
         const float f = Vec<T>::element(w, lane);
         st.offer(lane < N ? f : -INFINITY, (v0 + j * 64 + from) * N + lane, floor, s.n, lane);
       }
@@ -253,9 +248,7 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
 #pragma unroll
     for (int j = 0; j < NV; j++) cur[j] = nxt[j];
   }
-  double sum = st.sum;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  double sum = wave_sum(st.sum);
   if (__ballot(st.bad) != 0 || !(st.ref < INFINITY)) sum = __builtin_nan("");
   if (lane == 0) {
     s.part_ref[item] = st.ref;
@@ -305,16 +298,10 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
       }
       if (ref > -INFINITY) sum += t * pow2_64(((double)ref - top) * LOG2E);
     }
-    float most = top;
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    const float most = row_all(top, [](float a, float b) { return fmaxf(a, b); });
     sum = top > -INFINITY ? sum * pow2_64(((double)top - most) * LOG2E) : 0;
-    int wrong = bad;
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) {
-      sum += __shfl_xor(sum, d);
-      wrong |= __shfl_xor(wrong, d);
-    }
+    sum = row_all(sum, [](double a, double b) { return a + b; });
+    const int wrong = row_all((int)bad, [](int a, int b) { return a | b; });
     if (sub == 0 && w < s.beams) {
       const bool none = !in || wrong || !(most > -INFINITY) || !(__builtin_fabsf(score) < INFINITY);
       log_sum[w] = none ? __builtin_nan("") : log(sum);

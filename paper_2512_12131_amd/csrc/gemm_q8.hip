@@ -511,8 +511,7 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
 #pragma unroll
         for (int e = 0; e < 4; e++) most = max(most, __float_as_uint(f[e]) & 0x7fffffffu);
       }
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+      most = wave_max(most);
       const Scale<KIND> sc(most);
       if (lane == 0) row_scale[wave] = sc.scale;
       const int sw = (wave >> 1) & 7;

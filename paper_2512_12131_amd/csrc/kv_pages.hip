@@ -3,7 +3,7 @@
 // A page's count says how many entries of page tables hold it (and whoever else does); pages of count 0 are free.  Fork and compact
 // read the old lists and write new ones, so that a step that finds too few pages can be taken back.  Fresh pages are the lowest free
 // ones, given to the sequences in order: sums of whole numbers and prefix counts, so the same lists give the same result.
-#include "common.h"
+#include "lanes.h"
 
 namespace lrb {
 namespace {
@@ -11,25 +11,6 @@ namespace {
 __device__ __forceinline__ int lane_id() { return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)); }
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
-}
-
-// v of the lane that a DPP control names, 0 where there is none
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int64_t from_lane(int64_t v) {
-  return (int64_t)((uint64_t)(uint32_t)from_lane<CTRL, ROWS>((int)(v >> 32)) << 32 | (uint32_t)from_lane<CTRL, ROWS>((int)v));
-}
-// Sum of v over the lanes up to this one.
-template <class V>
-__device__ __forceinline__ V wave_prefix(V v) {
-  v += from_lane<0x111, 0xf>(v);      // row_shr:1, 2, 4, 8: within 16 lanes
-  v += from_lane<0x112, 0xf>(v);
-  v += from_lane<0x114, 0xf>(v);
-  v += from_lane<0x118, 0xf>(v);
-  v += from_lane<0x142, 0xa>(v);      // row_bcast:15 into the second and fourth 16
-  v += from_lane<0x143, 0xc>(v);      // row_bcast:31 into the upper 32
-  return v;
 }
 
 // Sum of v over the workgroup's threads before this one, and over all of them.  scratch: one entry for each of its NW wavefronts, free again after the call.

@@ -106,8 +106,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* x, int64_t ldx
       act(v);
       most = max(most, v.most());
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
+    most = wave_max(most);
     if constexpr (TPR == 256) {
       if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
       __syncthreads();

@@ -1,6 +1,6 @@
 // One row's scale and the whole numbers of its elements (quant_q8.hip, gemm_q8.hip).
 #pragma once
-#include "common.h"
+#include "lanes.h"
 
 namespace lrb {
 namespace {
