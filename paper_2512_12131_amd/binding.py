@@ -535,7 +535,7 @@ def lr_kv_fork(refs, page_size, page_table, kv_len, parent, grow, out=None, ws=N
     """The page tables of the sequences `parent` [n] (rows of page_table [batch, columns], which has their kv_len keys; outside it: a new sequence)
     with room for `grow` [n] new tokens each.  refs [pages] counts every page's holders.  Returns new (refs, page_table, kv_len, (src, dst, rows),
     missing); src, dst and rows go to lr_kv_copy before new keys are appended, missing [1] counts pages that were not there.  All int32.
-    out: what an earlier call returned, to be written again."""
+    The lists of a result share one allocation.  out: what an earlier call returned, to be written again."""
     return _native().kv_fork(refs, page_size, page_table, kv_len, parent, grow, *_outs(out, 3, 3, 1), ws)
 
 
@@ -545,8 +545,8 @@ def lr_kv_fork_workspace_bytes(pages, n_in, n_out):
 
 def lr_kv_compact(refs, page_table, out=None, ws=None):
     """Moves the pages in use (refs [pages] above 0) to the front.  Returns new (refs, page_table, (src, dst), page_map, n_live): src and dst
-    [pages / 2] go to lr_kv_copy, page_map [pages] gives the new numbers (-1: free), n_live [1] their count.  All int32.  out: what an earlier call
-    returned, to be written again."""
+    [pages / 2] go to lr_kv_copy, page_map [pages] gives the new numbers (-1: free), n_live [1] their count.  All int32.  The lists of a result share one
+    allocation.  out: what an earlier call returned, to be written again."""
     return _native().kv_compact(refs, page_table, *_outs(out, 2, 2, 2), ws)
 
 

@@ -331,8 +331,9 @@ PyObject* swiglu_bwd(Args& a) {
 // ---- rotary positions, paged cache -----------------------------------------------------------
 // Launches go to the current stream, which is one of the current device's: operands are there too.
 void on_current_device(std::initializer_list<const at::Tensor*> ts) {
+  int here = -1;
   for (const at::Tensor* t : ts)
-    if (t->defined() && (!t->is_cuda() || t->get_device() != c10::hip::current_device())) fail(g_lr_error, "tensors on the current GPU expected");
+    if (t->defined() && (!t->is_cuda() || t->get_device() != (here >= 0 ? here : here = c10::hip::current_device()))) fail(g_lr_error, "tensors on the current GPU expected");
 }
 const int32_t* indices(const at::Tensor& t, int64_t n) {
   if (t.defined() && t.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
@@ -484,6 +485,26 @@ PyObject* attention_paged_fwd(Args& a) {
 
 // ---- pages of the cache ----------------------------------------------------------------------
 at::Tensor fresh32(at::IntArrayRef sizes, const at::Tensor& like) { return fresh(sizes, at::kInt, like); }
+// The int32 lists of a result in one allocation, each from 256 bytes on (one each takes the host 0.6 us a list).  A list that the caller passes stays.
+struct Wanted { at::Tensor* t; int64_t rows, cols; };      // cols 0: a list of rows
+void fresh_lists(std::initializer_list<Wanted> lists, const at::Tensor& like) {
+  const auto span = [](const Wanted& w) { return (w.rows * (w.cols > 0 ? w.cols : 1) + 63) / 64 * 64; };
+  int64_t total = 0;
+  for (const Wanted& w : lists) total += w.t->defined() ? 0 : span(w);
+  if (total == 0) total = 1;
+  at::Tensor all;
+  int64_t at = 0;
+  for (const Wanted& w : lists) {
+    if (w.t->defined()) continue;
+    if (!all.defined()) all = fresh32({total}, like);
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+    t.unsafeGetTensorImpl()->set_storage_offset(at);
+    const int64_t sizes[] = {w.rows, w.cols};
+    t.unsafeGetTensorImpl()->set_sizes_contiguous(at::IntArrayRef(sizes, w.cols > 0 ? 2 : 1));
+    at += span(w);
+    *w.t = std::move(t);
+  }
+}
 // a page table [rows, columns]: its row stride (of a single row any will do)
 int64_t table_stride(const at::Tensor& t) {
   if (t.scalar_type() != at::kInt) fail(g_lr_error, "int32 indices expected");
@@ -524,11 +545,8 @@ PyObject* kv_fork(Args& a) {
              missing = a.optional(), ws = a.optional();
   const int64_t pages = rows_of(refs, 1), ld = table_stride(table), n_in = table.size(0), cols = table.size(1), n = rows_of(parent, 1);
   const int32_t *pr = indices(refs, pages), *pl = indices(len, n_in), *pp = indices(parent, n), *pg = indices(grow, n), *pt = (const int32_t*)ptr(table);
-  if (!refs_out.defined()) refs_out = fresh32({pages}, refs);
-  if (!table_out.defined()) table_out = fresh32({n, cols}, refs);
-  for (at::Tensor* t : {&len_out, &src, &dst, &rows})
-    if (!t->defined()) *t = fresh32({n}, refs);
-  if (!missing.defined()) missing = fresh32({1}, refs);
+  if (cols == 0) fail(PyExc_ValueError, "a page table with columns expected");
+  fresh_lists({{&refs_out, pages, 0}, {&table_out, n, cols}, {&len_out, n, 0}, {&src, n, 0}, {&dst, n, 0}, {&rows, n, 0}, {&missing, 1, 0}}, refs);
   const int64_t ldo = table_stride(table_out);
   if (table_out.size(0) != n || table_out.size(1) != cols) fail(PyExc_ValueError, "unexpected shape of the new page table");
   int32_t *qr = written(refs_out, pages), *ql = written(len_out, n), *qs = written(src, n), *qd = written(dst, n), *qw = written(rows, n),
@@ -547,12 +565,8 @@ PyObject* kv_compact(Args& a) {
              ws = a.optional();
   const int64_t pages = rows_of(refs, 1), ld = table_stride(table), batch = table.size(0), cols = table.size(1);
   const int32_t *pr = indices(refs, pages), *pt = (const int32_t*)ptr(table);
-  if (!refs_out.defined()) refs_out = fresh32({pages}, refs);
-  if (!table_out.defined()) table_out = fresh32({batch, cols}, refs);
-  for (at::Tensor* t : {&src, &dst})
-    if (!t->defined()) *t = fresh32({pages / 2}, refs);
-  if (!map.defined()) map = fresh32({pages}, refs);
-  if (!live.defined()) live = fresh32({1}, refs);
+  if (cols == 0) fail(PyExc_ValueError, "a page table with columns expected");
+  fresh_lists({{&refs_out, pages, 0}, {&table_out, batch, cols}, {&src, pages / 2, 0}, {&dst, pages / 2, 0}, {&map, pages, 0}, {&live, 1, 0}}, refs);
   const int64_t ldo = table_stride(table_out);
   if (table_out.size(0) != batch || table_out.size(1) != cols) fail(PyExc_ValueError, "unexpected shape of the new page table");
   int32_t *qr = written(refs_out, pages), *qs = written(src, pages / 2), *qd = written(dst, pages / 2), *qp = written(map, pages), *ql = written(live, 1),
