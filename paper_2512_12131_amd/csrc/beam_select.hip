@@ -60,10 +60,11 @@ struct Best {
   }
 };
 
-// The largest value that at least n lanes reach (0: fewer have any).
+// The largest value that at least n lanes reach (0: fewer have any), without its lowest 12 bits.
 __device__ __forceinline__ uint32_t nth_of_lanes(uint32_t v, int n) {
   uint32_t t = 0;
-  for (int b = 31; b >= 0; b--) {
+#pragma unroll
+  for (int b = 31; b >= 12; b--) {
     const uint32_t u = t | (1u << b);
     if (lanes_in(__ballot(v >= u)) >= n) t = u;
   }
@@ -263,8 +264,8 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
   // a candidate's score is (logit - largest logit) - logarithm of the sum + score, in this order: the logits may be far from zero
   __shared__ double log_sum[BEAM_MOST];                // NaN: the beam offers nothing
   __shared__ float largest[BEAM_MOST], score_in[BEAM_MOST];
-  __shared__ uint64_t best_score[2][BEAM_MOST + 256 + 8];  // (double's order; 0: none)
-  __shared__ uint32_t best_at[2][BEAM_MOST + 256 + 8];     // ~(beam of the prompt * 2^20 + token): the larger, the earlier
+  __shared__ uint64_t best_score[2][BEAM_MOST + 256];  // (double's order; 0: none)
+  __shared__ uint32_t best_at[2][BEAM_MOST + 256];     // ~(beam of the prompt * 2^20 + token): the larger, the earlier
   __shared__ uint32_t floors[4];
   __shared__ int added;
   constexpr int AHEAD = 4;                             // candidates of a list that are asked for at once
@@ -288,15 +289,27 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     float top = -INFINITY;
     double sum = 0;
     bool bad = false;
-    for (int p = sub; in && p < s.parts; p += 16) {
-      const float ref = s.part_ref[item + p];
-      const double t = s.part_sum[item + p];
-      bad |= !(t == t);
-      if (ref > top) {                                 // (the sum so far refers to the larger one)
-        sum = top > -INFINITY ? sum * pow2_64(((double)top - ref) * LOG2E) : 0;
-        top = ref;
+    for (int p0 = 0; in && p0 < s.parts; p0 += 64) {   // four runs of a lane are on their way at once
+      float ref[4], high = top;
+      double t[4];
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        const int p = p0 + 16 * j + sub, q = min(p, s.parts - 1);
+        ref[j] = s.part_ref[item + q];
+        t[j] = s.part_sum[item + q];
+        if (p >= s.parts) ref[j] = -INFINITY, t[j] = 0;
       }
-      if (ref > -INFINITY) sum += t * pow2_64(((double)ref - top) * LOG2E);
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        bad |= !(t[j] == t[j]);
+        high = fmaxf(high, ref[j]);
+      }
+      if (high > -INFINITY) {                          // (the sum so far refers to the largest one; a run without any has 0)
+        sum *= pow2_64(((double)top - high) * LOG2E);
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum += t[j] * pow2_64(((double)ref[j] - high) * LOG2E);
+        top = high;
+      }
     }
     const float most = row_all(top, [](float a, float b) { return fmaxf(a, b); });
     sum = top > -INFINITY ? sum * pow2_64(((double)top - most) * LOG2E) : 0;
@@ -337,22 +350,19 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     __syncthreads();
     const int more = added, all = have + more;
     if (more == 0) return false;
-    for (int i = threadIdx.x; i < all; i += 256) {
+    // sixteen lanes per candidate
+    for (int i0 = 0; i0 < all; i0 += 16) {
+      const int i = min(i0 + (int)threadIdx.x / 16, all - 1);
       const uint64_t mine = best_score[side][i];
       const uint32_t mine_at = best_at[side][i];
       int place = 0;
-      for (int j0 = 0; j0 < all; j0 += 8) {            // (eight at a time are on their way; what lies behind the last one is not looked at)
-        uint64_t other[8];
-        uint32_t other_at[8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-          other[j] = best_score[side][j0 + j];
-          other_at[j] = best_at[side][j0 + j];
-        }
-#pragma unroll
-        for (int j = 0; j < 8; j++) place += j0 + j < all && (other[j] > mine || (other[j] == mine && other_at[j] > mine_at));
+      for (int j = threadIdx.x & 15; j < all; j += 16) {
+        const uint64_t other = best_score[side][j];
+        const uint32_t other_at = best_at[side][j];
+        place += other > mine || (other == mine && other_at > mine_at);
       }
-      if (place < s.n) {
+      place = row_all(place, [](int a, int b) { return a + b; });
+      if ((threadIdx.x & 15) == 0 && i0 + (int)threadIdx.x / 16 < all && place < s.n) {
         best_score[side ^ 1][place] = mine;
         best_at[side ^ 1][place] = mine_at;
       }
