@@ -163,36 +163,27 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
   if (threadIdx.x < 4) floors[threadIdx.x] = 0;
   __syncthreads();
   uint32_t* known = floors + (row - (int)blockIdx.x * 4 / s.parts);
-  if (row >= s.rows || (s.done && s.done[row] != 0)) return;
-  const T* x = (const T*)s.logits + (int64_t)row * s.ld;
+  const bool live = row < s.rows && !(s.done && s.done[row] != 0);
+  const T* x = (const T*)s.logits + (int64_t)(live ? row : 0) * s.ld;
   // Runs, pieces and vectors are the same in every row, wherever it starts: rows of the same logits have the same sum, and equal candidates stay equal.
   const int vecs = s.V / N, tail = s.V - vecs * N;
   const int begin = part * s.run, end = min(begin + s.run, vecs);
-  RunState st;
-  if (part == 0 && tail > 0) {
-    const int at = vecs * N + lane;
-    const float f = lane < tail ? Vec<T>::one(x + at) : -INFINITY;
-    st.bad |= f != f;
-    st.refer(f);
-    if (st.ref > -INFINITY) st.sum += lane < tail ? pow2_64(((double)f - st.ref) * LOG2E) : 0.0;
-    st.offer(f, at, -INFINITY, s.n, lane);
-  }
   const u32x4_anywhere* px = reinterpret_cast<const u32x4_anywhere*>(x);
   u32x4 cur[NV], nxt[NV];
   auto ask = [&](int v0, u32x4 (&v)[NV]) {
 #pragma unroll
     for (int j = 0; j < NV; j++) v[j] = px[min(v0 + j * 64 + lane, vecs - 1)];
   };
-  if (begin < end) ask(begin, cur);
-  for (int v0 = begin; v0 < end; v0 += 64 * NV) {
-    ask(v0 + 64 * NV, nxt);
+  auto cut = [&](int v0) {                             // what of `cur` lies behind the run
     if (v0 + 64 * NV > end) {
 #pragma unroll
       for (int j = 0; j < NV; j++)
         if (v0 + j * 64 + lane >= end) cur[j] = u32x4{Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE, Vec<T>::NONE};
     }
-    // (a NaN comes through to `most`, and the comparisons below are false)
-    float top[NV], most = -INFINITY;
+  };
+  // the largest logit of every vector, and of them all (a NaN comes through, and comparisons with it are false)
+  auto largest = [&](float (&top)[NV]) {
+    float most = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; j++) {
       float f[N];
@@ -202,6 +193,33 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
       for (int e = 1; e < N; e++) top[j] = __builtin_elementwise_maximum(top[j], f[e]);
       most = __builtin_elementwise_maximum(most, top[j]);
     }
+    return most;
+  };
+  // all first pieces' floors before any of them is searched
+  if (live && begin < end) {
+    ask(begin, cur);
+    cut(begin);
+    float top[NV];
+    const float most = largest(top);
+    const uint32_t least = nth_of_lanes(most > -INFINITY ? ordered(most + 0.f) : 0, s.n);
+    if (lane == 0) __hip_atomic_fetch_max(known, least, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+  }
+  __syncthreads();
+  if (!live) return;
+  RunState st;
+  if (part == 0 && tail > 0) {
+    const int at = vecs * N + lane;
+    const float f = lane < tail ? Vec<T>::one(x + at) : -INFINITY;
+    st.bad |= f != f;
+    st.refer(f);
+    if (st.ref > -INFINITY) st.sum += lane < tail ? pow2_64(((double)f - st.ref) * LOG2E) : 0.0;
+    st.offer(f, at, -INFINITY, s.n, lane);
+  }
+  for (int v0 = begin; v0 < end; v0 += 64 * NV) {
+    ask(v0 + 64 * NV, nxt);
+    cut(v0);
+    float top[NV];
+    const float most = largest(top);
     st.bad |= most != most;
     st.refer(most);
     const uint32_t least = st.floor(most, __hip_atomic_load(known, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP), s.n);
