@@ -4,7 +4,8 @@
 // The quotient is formed in 32 bits as a product with 127 / max, off by at most 127 * 2^-23 < 2^-16; fp32 elements for which that leaves the nearest whole
 // number open (within 2^-13 of a half) are settled by an exact comparison, of bf16 ones none needs it (quant_row.h).
 //
-// Bound: HBM, a row read once where it fits the registers of its lanes.
+// Bound: HBM, a row read once where it fits the registers of its lanes: 16384 x 4096 bf16 34 - 46 us (201 MB), 777 x 5461 fp32 in rows that start anywhere 7.9; few rows
+// the way in and out of a launch, 16 x 4096 bf16 3.0.
 #include "quant_row.h"
 
 namespace lrb {
