@@ -148,7 +148,9 @@ hipError_t launch(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* sca
   };
   // us, one wavefront a row / four: 16384 x 1024 fp32 14.1 / 22.4, 16 x 4096 6.3 / 3.5, 16384 x 4096 79 / 53
   if (n <= 1024) return run(quant_rows_kernel<T, 64, 1, ACT>, 4);
-  return run(quant_rows_kernel<T, 256, 1, ACT>, 1);
+  // us, 4096 / 12288 elements in registers: 16384 x 5460 fp32 81 / 87 (with 8192), 16384 x 11008 bf16 108 / 101, fp32 181 / 168, 4096 x 16384 bf16 48 / 39
+  if (n <= 8192) return run(quant_rows_kernel<T, 256, 1, ACT>, 1);
+  return run(quant_rows_kernel<T, 256, 3, ACT>, 1);
 }
 
 }  // namespace
