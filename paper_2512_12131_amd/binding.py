@@ -535,8 +535,8 @@ def lr_kv_fork(refs, page_size, page_table, kv_len, parent, grow, out=None, ws=N
     """The page tables of the sequences `parent` [n] (rows of page_table [batch, columns], which has their kv_len keys; outside it: a new sequence)
     with room for `grow` [n] new tokens each.  refs [pages] counts every page's holders.  Returns new (refs, page_table, kv_len, (src, dst, rows),
     missing); src, dst and rows go to lr_kv_copy before new keys are appended, missing [1] counts pages that were not there.  All int32.
-    The lists of a result share one allocation.  out: what an earlier call returned, to be written again."""
-    return _native().kv_fork(refs, page_size, page_table, kv_len, parent, grow, *_outs(out, 3, 3, 1), ws)
+    The lists of a result and the workspace share one allocation.  out: what an earlier call returned, to be written again."""
+    return _native().kv_fork(refs, page_size, page_table, kv_len, parent, grow, *(_outs(out, 3, 3, 1) if out is not None else (None,) * 7), ws)
 
 
 def lr_kv_fork_workspace_bytes(pages, n_in, n_out):
@@ -545,9 +545,9 @@ def lr_kv_fork_workspace_bytes(pages, n_in, n_out):
 
 def lr_kv_compact(refs, page_table, out=None, ws=None):
     """Moves the pages in use (refs [pages] above 0) to the front.  Returns new (refs, page_table, (src, dst), page_map, n_live): src and dst
-    [pages / 2] go to lr_kv_copy, page_map [pages] gives the new numbers (-1: free), n_live [1] their count.  All int32.  The lists of a result share one
-    allocation.  out: what an earlier call returned, to be written again."""
-    return _native().kv_compact(refs, page_table, *_outs(out, 2, 2, 2), ws)
+    [pages / 2] go to lr_kv_copy, page_map [pages] gives the new numbers (-1: free), n_live [1] their count.  All int32.  The lists of a result and the
+    workspace share one allocation.  out: what an earlier call returned, to be written again."""
+    return _native().kv_compact(refs, page_table, *(_outs(out, 2, 2, 2) if out is not None else (None,) * 6), ws)
 
 
 def lr_kv_compact_workspace_bytes(pages):
@@ -556,8 +556,6 @@ def lr_kv_compact_workspace_bytes(pages):
 
 def _outs(out, before, pair, behind):
     """The tensors of a result whose entry number `before` is a tuple of `pair` of them, in a row."""
-    if out is None:
-        return [None] * (before + pair + behind)
     if len(out) != before + 1 + behind or len(out[before]) != pair:
         raise LrError("out: the result of an earlier call expected")
     return [*out[:before], *out[before], *out[before + 1:]]

@@ -485,7 +485,7 @@ PyObject* attention_paged_fwd(Args& a) {
 
 // ---- pages of the cache ----------------------------------------------------------------------
 at::Tensor fresh32(at::IntArrayRef sizes, const at::Tensor& like) { return fresh(sizes, at::kInt, like); }
-// The int32 lists of a result in one allocation, each from 256 bytes on (one each takes the host 0.6 us a list).  A list that the caller passes stays.
+// The int32 lists of a result and the workspace in one allocation, each from 256 bytes on (one each takes the host 0.6 us a list).  What the caller passes stays.
 struct Wanted { at::Tensor* t; int64_t rows, cols; };      // cols 0: a list of rows
 void fresh_lists(std::initializer_list<Wanted> lists, const at::Tensor& like) {
   const auto span = [](const Wanted& w) { return (w.rows * (w.cols > 0 ? w.cols : 1) + 63) / 64 * 64; };
@@ -546,13 +546,13 @@ PyObject* kv_fork(Args& a) {
   const int64_t pages = rows_of(refs, 1), ld = table_stride(table), n_in = table.size(0), cols = table.size(1), n = rows_of(parent, 1);
   const int32_t *pr = indices(refs, pages), *pl = indices(len, n_in), *pp = indices(parent, n), *pg = indices(grow, n), *pt = (const int32_t*)ptr(table);
   if (cols == 0) fail(PyExc_ValueError, "a page table with columns expected");
-  fresh_lists({{&refs_out, pages, 0}, {&table_out, n, cols}, {&len_out, n, 0}, {&src, n, 0}, {&dst, n, 0}, {&rows, n, 0}, {&missing, 1, 0}}, refs);
+  fresh_lists({{&refs_out, pages, 0}, {&table_out, n, cols}, {&len_out, n, 0}, {&src, n, 0}, {&dst, n, 0}, {&rows, n, 0}, {&missing, 1, 0},
+               {&ws, (int64_t)(lr_kv_fork_workspace_bytes(pages, n_in, n) + 3) / 4, 0}}, refs);
   const int64_t ldo = table_stride(table_out);
   if (table_out.size(0) != n || table_out.size(1) != cols) fail(PyExc_ValueError, "unexpected shape of the new page table");
   int32_t *qr = written(refs_out, pages), *ql = written(len_out, n), *qs = written(src, n), *qd = written(dst, n), *qw = written(rows, n),
           *qm = written(missing, 1), *qt = (int32_t*)ptr(table_out);
   on_current_device({&refs, &table, &len, &parent, &grow, &refs_out, &table_out, &len_out, &src, &dst, &rows, &missing, &ws});
-  if (!ws.defined()) ws = workspace(lr_kv_fork_workspace_bytes(pages, n_in, n), refs);
   const size_t nb = ws.numel() * ws.element_size();
   void *pw = dense(ws), *st = stream();
   call("lr_kv_fork", [&] { return lr_kv_fork(pr, pages, page, pt, ld, pl, n_in, pp, pg, qr, qt, ldo, ql, n, cols, qs, qd, qw, qm, pw, nb, st); });
@@ -566,13 +566,13 @@ PyObject* kv_compact(Args& a) {
   const int64_t pages = rows_of(refs, 1), ld = table_stride(table), batch = table.size(0), cols = table.size(1);
   const int32_t *pr = indices(refs, pages), *pt = (const int32_t*)ptr(table);
   if (cols == 0) fail(PyExc_ValueError, "a page table with columns expected");
-  fresh_lists({{&refs_out, pages, 0}, {&table_out, batch, cols}, {&src, pages / 2, 0}, {&dst, pages / 2, 0}, {&map, pages, 0}, {&live, 1, 0}}, refs);
+  fresh_lists({{&refs_out, pages, 0}, {&table_out, batch, cols}, {&src, pages / 2, 0}, {&dst, pages / 2, 0}, {&map, pages, 0}, {&live, 1, 0},
+               {&ws, (int64_t)(lr_kv_compact_workspace_bytes(pages) + 3) / 4, 0}}, refs);
   const int64_t ldo = table_stride(table_out);
   if (table_out.size(0) != batch || table_out.size(1) != cols) fail(PyExc_ValueError, "unexpected shape of the new page table");
   int32_t *qr = written(refs_out, pages), *qs = written(src, pages / 2), *qd = written(dst, pages / 2), *qp = written(map, pages), *ql = written(live, 1),
           *qt = (int32_t*)ptr(table_out);
   on_current_device({&refs, &table, &refs_out, &table_out, &src, &dst, &map, &live, &ws});
-  if (!ws.defined()) ws = workspace(lr_kv_compact_workspace_bytes(pages), refs);
   const size_t nb = ws.numel() * ws.element_size();
   void *pw = dense(ws), *st = stream();
   call("lr_kv_compact", [&] { return lr_kv_compact(pr, pages, pt, ld, batch, cols, qr, qt, ldo, qs, qd, qp, ql, pw, nb, st); });

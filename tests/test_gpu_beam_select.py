@@ -158,3 +158,19 @@ def test_scores_are_written_over_the_old_ones():
     assert got[2].data_ptr() == score.data_ptr() and all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(B.LrError):
         B.lr_beam_select(logits[:120], score[:20], out=tuple(t.view(40, 6)[10:30] for t in out))
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 logits: the last prompts' choices are those of the prompts alone."""
+    batch, beams, V = 700, 4, 800000
+    g = torch.Generator(device=DEV).manual_seed(41)
+    logits = torch.randint(-20000, 20000, (batch * beams, V // 8), generator=g, device=DEV, dtype=torch.int16)
+    logits = (logits.to(BF) / 4096).repeat(1, 8)
+    logits[:, V // 2] = 9
+    assert logits.numel() > 2 ** 31
+    score = torch.randn((batch, beams), generator=g, device=DEV)
+    got = B.lr_beam_select(logits, score)
+    for p in (0, 350, batch - 1):
+        alone = B.lr_beam_select(logits[p * beams:(p + 1) * beams].clone(), score[p:p + 1])
+        assert torch.equal(got[0][p] - p * beams, alone[0][0]) and torch.equal(got[1][p], alone[1][0])
+        assert float((got[2][p] - alone[2][0]).abs().max()) <= 2.0 ** -23 * 64      # (other runs, another order of the sum: neighbouring roundings)

@@ -193,3 +193,13 @@ def test_captured_steps_take_what_the_lists_hold():
             B.lr_kv_copy(before[0], before[1], *moved)
             torch.cuda.synchronize()
             assert all(np.array_equal(a, b) for a, b in zip(flat(out), flat(want))) and torch.equal(cache, before), turn
+
+
+def test_copies_past_32_bits():
+    """A cache of more than 2^31 elements: pages at its two ends."""
+    pages = 2 ** 17 + 64
+    k, v = (torch.zeros((pages, 16, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    k[5], v[5], k[-1], v[-1] = 1, 2, 3, 4
+    B.lr_kv_copy(k, v, dev([5, pages - 1, pages]), dev([pages - 2, 6, 7]))
+    assert bool((k[-2] == 1).all()) and bool((v[-2] == 2).all()) and bool((k[6] == 3).all()) and bool((v[6] == 4).all())
+    assert not k[7].any() and not k[-3].any() and not v[-3].any() and not k[4].any()

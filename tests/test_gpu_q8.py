@@ -98,7 +98,7 @@ def product(a, sa, b, sb, dtype):
 
 SHAPES = [(1, 1, 1), (1, 33, 15), (3, 7, 16), (33, 31, 17), (32, 64, 32), (5, 100, 129), (16, 1024, 4096), (16, 4096, 1024), (64, 2048, 512), (65, 129, 1000),
           (100, 777, 333), (128, 128, 128), (129, 257, 640), (256, 512, 255), (777, 2047, 546), (300, 4096, 64), (1031, 768, 256), (2048, 2048, 2048),
-          (16, 1024, 11000), (50, 700, 9001), (64, 8200, 2050), (40, 33000, 515), (128, 33000, 523), (100, 4100, 4109), (17, 16500, 1024)]
+          (16, 1024, 11000), (50, 700, 9001), (64, 8200, 2050), (40, 33000, 515), (128, 33000, 523), (100, 4100, 4109), (17, 16500, 1024), (9000, 1, 40), (1, 9000, 40), (40000, 3, 7)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
@@ -253,3 +253,18 @@ def test_a_token_alone_and_among_others(d, r, n, dtype):
     bits = lambda t: t.contiguous().view(torch.int16 if dtype == BF else torch.int32)
     for first, count in ((0, 1), (4, 1), (3, 2), (0, 8), (8, 5), (1, 16)):
         assert torch.equal(bits(B.lr_linear_q8_fwd(x[first:first + count], *w)), bits(want[first:first + count])), (first, count)
+
+
+def test_offsets_past_32_bits():
+    """Rows of 8-bit integers and results with more than 2^31 elements: the last ones are those of the rows alone."""
+    g = gen(40)
+    M, N = 66000, 33000
+    a, b, sa, sb = ints(g, M, 16), ints(g, N, 16), scales(g, M), scales(g, N)
+    big = B.lr_matmul_q8(a, sa, b, sb)
+    assert big.numel() > 2 ** 31
+    for rows in (slice(0, 300), slice(M // 2, M // 2 + 300), slice(M - 300, M)):
+        assert torch.equal(big[rows], B.lr_matmul_q8(a[rows].contiguous(), sa[rows].contiguous(), b, sb))
+    q, s = B.lr_quant_rows(big)
+    for rows in (slice(0, 40), slice(M - 40, M)):
+        alone = B.lr_quant_rows(big[rows].clone())
+        assert torch.equal(q[rows], alone[0]) and torch.equal(s[rows], alone[1])
