@@ -581,7 +581,8 @@ def lr_beam_select_workspace_bytes(batch, beams, V, n):
 
 # ---- 8-bit integers ----------------------------------------------------------------------------
 def lr_quant_rows(x, q=None, scale=None):
-    """x [T, n] as integers of 8 bits and a scale for each row: returns (q [T, n] int8 in rows that start on 16 bytes, scale [T] fp32).  Activations by
+    """x [T, n] as integers of 8 bits and a scale for each row: returns (q [T, n] int8 in rows that start on 16 bytes, on 128
+    above 1024 elements, scale [T] fp32).  Activations by
     token, weights [out, in] by output channel."""
     return _native().quant_rows(x, q, scale)
 

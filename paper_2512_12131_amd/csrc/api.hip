@@ -1750,7 +1750,8 @@ struct LinearQ8 {
 };
 LinearQ8 linear_q8_parts(Ctx& c, int64_t T, int64_t d_in, int64_t r) {
   LinearQ8 p{};
-  p.ldx = rup(d_in, 16); p.ldz = rup(r, 16);
+  const auto ld = [](int64_t n) { return rup(n, n > 1024 ? 128 : 16); };      // (long rows on lines of 128 bytes, which the products read whole)
+  p.ldx = ld(d_in); p.ldz = ld(r);
   p.qx = (int8_t*)c.take((size_t)T * p.ldx);
   p.sx = (float*)c.take((size_t)T * sizeof(float));
   p.z = (float*)c.take((size_t)T * p.ldz * sizeof(float));

@@ -637,9 +637,9 @@ void scales_of(const at::Tensor& s, int64_t n) {
   if (s.scalar_type() != at::kFloat) fail(g_lr_error, "fp32 scales expected");
   if (s.dim() != 1 || s.size(0) != n) fail(PyExc_ValueError, "a scale for each row expected");
 }
-// [rows, width] in rows that start on 16 bytes
-at::Tensor padded(int64_t rows, int64_t width, at::ScalarType dt, const at::Tensor& like) {
-  const int64_t per = 16 / (int64_t)at::elementSize(dt), ld = (width + per - 1) / per * per;
+// [rows, width] in rows that start on `bytes`
+at::Tensor padded(int64_t rows, int64_t width, at::ScalarType dt, const at::Tensor& like, int64_t bytes = 16) {
+  const int64_t per = bytes / (int64_t)at::elementSize(dt), ld = (width + per - 1) / per * per;
   const at::Tensor t = fresh({rows, ld}, dt, like);
   return ld == width ? t : t.narrow(1, 0, width);
 }
@@ -650,7 +650,8 @@ PyObject* quant_rows(Args& a) {
   const int64_t T = rows_of(x), n = x.size(1);
   const int dt = dt_of(x);
   const int64_t ldx = rows_as_wide(x, T, n);
-  if (!q.defined()) q = padded(T, n, at::kChar, x);
+  // (long rows on 128 bytes: the product reads 128 of a row at a time, one line of a cache then instead of two)
+  if (!q.defined()) q = padded(T, n, at::kChar, x, n > 1024 ? 128 : 16);
   if (!scale.defined()) scale = fresh({T}, at::kFloat, x);
   const int64_t ldq = rows_q8(q, T, n);
   scales_of(scale, T);
