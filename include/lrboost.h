@@ -428,7 +428,7 @@ int lr_quant_rows(const void* x, int64_t ldx, int8_t* q, int64_t ldq, float* sca
 int lr_matmul_q8(const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb, void* c, int64_t ldc, int64_t M,
                  int64_t N, int64_t K, int dt, void* stream);
 /* The forward of one bottleneck layer with both weights in 8 bits: y = Q(act(Q(x) . W_down^T)) . W_up^T, Q = lr_quant_rows and back; z and act(z) are
- * fp32 and not rounded in between.  w_down [r, ld_down], s_down [r], w_up [d_out, ld_up], s_up [d_out] as lr_matmul_q8 takes b.  x, y: as lr_linear_fwd (y's rows start on 16
+ * fp32 and not rounded in between: a row of y has the bits that lr_quant_rows, lr_matmul_q8 and lr_act_fwd in fp32 give it, however many there are.  w_down [r, ld_down], s_down [r], w_up [d_out, ld_up], s_up [d_out] as lr_matmul_q8 takes b.  x, y: as lr_linear_fwd (y's rows start on 16
  * bytes in LR_F32 too).                                                                                                             */
 size_t lr_linear_q8_workspace_bytes(int64_t T, int64_t d_in, int64_t r);
 int lr_linear_q8_fwd(const void* x, int64_t ldx, const int8_t* w_down, int64_t ld_down, const float* s_down, const int8_t* w_up, int64_t ld_up,

@@ -1791,7 +1791,7 @@ int lr_linear_q8_fwd(const void* x, int64_t ldx, const int8_t* w_down, int64_t l
       LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));
       LAUNCH(c, gemm_q8(down, c.st));
     }
-    LAUNCH(c, gemm_q8_from_ours(up, p.z, p.ldz, c.st));
+    LAUNCH(c, gemm_q8_from(up, p.z, p.ldz, LR_F32, c.st));
     return status_of(c);
   }
   LAUNCH(c, k_quant_rows(x, ldx, p.qx, p.ldx, p.sx, T, d_in, LR_ACT_IDENTITY, dt, c.st));

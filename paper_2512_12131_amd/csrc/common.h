@@ -310,15 +310,14 @@ struct Q8Op {
   void* C;
   int64_t lda, ldb, ldc;
   int M, N, K, dt;
-  int act = LR_ACT_IDENTITY;               // of C, before it is stored (where gemm_q8_acts says so, and gemm_q8_from..)
+  int act = LR_ACT_IDENTITY;               // of C, before it is stored (where gemm_q8_acts says so, and gemm_q8_from)
 };
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st);
-// The same of few rows x [M, K] that are quantised on the way in (op.A and op.sa are not read): of type dt, for fp32 results, or fp32 rows of our own.
+// The same of few rows x [M, K] of type dt that are quantised on the way in (op.A and op.sa are not read); of bf16 rows only fp32 results.
 bool gemm_q8_acts(const Q8Op& op);
 constexpr int64_t Q8_FEW_ELEMENTS = 1 << 15;
 bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K);
 hipError_t gemm_q8_from(const Q8Op& op, const void* x, int64_t ldx, int dt, hipStream_t st);
-hipError_t gemm_q8_from_ours(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st);
 
 // ---- attention (attention.hip) ---------------------------------------------------------------
 hipError_t attention_fwd_bf16(const void* q, const void* k, const void* v, void* o, float* lse, int64_t ld,

@@ -433,7 +433,7 @@ hipError_t launch_q8_big(const Q8Op& op, hipStream_t st) {
 // A workgroup takes 16 rows and NT * 16 columns over all of k: A and B lie in LDS as they are (up to `chunk` k at a time), its 16 wavefronts take every
 // 16th step of 64 k each (v_mfma_i32_16x16x64_i8) and the 16 sums are added up through LDS.
 //
-// OURS: A comes as rows of type KIND, which every workgroup quantises for itself, a wavefront a row: it holds the row (of up to 64 * 4 * OURS columns) in
+// QUADS: A comes as rows of type KIND, which every workgroup quantises for itself, a wavefront a row: it holds the row (of up to 64 * 4 * QUADS columns) in
 // registers, whose largest element needs no other wavefront.  Bound: the way in and out of a launch, and what a CU takes in.
 // The layer 4096 -> 1024 -> 4096 of 16 tokens, us: 12.1 so in its second product, 13.0 with a launch for the quantisation between the products.  In the first
 // product, where every workgroup does the rows' whole work, up to 2^15 elements: of 1 / 8 / 16 tokens, with a launch before it, 10.6 / 11.4 / 12.1, without
@@ -455,7 +455,7 @@ __device__ __forceinline__ void floats_of(const u32x2_t& v, float* f) {
   for (int e = 0; e < 4; e++) f[e] = __uint_as_float(e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
 }
 
-template <int OURS, Rows KIND, int NT, int OUT, bool TAIL>
+template <int QUADS, Rows KIND, int NT, int OUT, bool TAIL>
 __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const void* xs, int64_t ldx, int chunk) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   __shared__ float row_scale[16];
@@ -465,9 +465,9 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
   unsigned char* sB = smem + slices * R16_SLICE;                 // then NT of these
   int* part = reinterpret_cast<int*>(sB + NT * slices * R16_SLICE);
   const uint32_t lds = (uint32_t)(uintptr_t)LRB_LDS_PTR(smem);
-  const rsrc_words rsB = operand_rsrc(op.B + (int64_t)n0 * op.ldb), rsA = operand_rsrc(OURS ? op.B : op.A + (int64_t)m0 * op.lda);
+  const rsrc_words rsB = operand_rsrc(op.B + (int64_t)n0 * op.ldb), rsA = operand_rsrc(QUADS ? op.B : op.A + (int64_t)m0 * op.lda);
   // Loads of 8 rows x 128 bytes: the rows of A (as int8), then those of B, slice by slice
-  constexpr int FIRST_OP = OURS ? 1 : 0, PER = 2 * (1 + NT - FIRST_OP);
+  constexpr int FIRST_OP = QUADS ? 1 : 0, PER = 2 * (1 + NT - FIRST_OP);
   auto load = [&](int k0) {
     for (int id = wave; id < slices * PER; id += R16_W) {
       const int slice = id / PER, w = id % PER + 2 * FIRST_OP, o = w >> 1;      // o: 0 A, then the 16 columns of B
@@ -485,13 +485,13 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
     for (int step = wave; step < 2 * slices; step += R16_W) {
       const int at = (step >> 1) * R16_SLICE + row * 128 + ((((step & 1) * 4 + (lane >> 4)) ^ sw) << 4);
       i32x4 fa = *reinterpret_cast<const i32x4*>(smem + at);
-      if constexpr (!OURS && TAIL) fa = tail.of(fa, (k0 + step * 64) / 16 + (lane >> 4));
+      if constexpr (!QUADS && TAIL) fa = tail.of(fa, (k0 + step * 64) / 16 + (lane >> 4));
 #pragma unroll
       for (int j = 0; j < NT; j++)
         acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(*reinterpret_cast<const i32x4*>(sB + j * slices * R16_SLICE + at), fa, acc[j], 0, 0, 0);
     }
   };
-  if constexpr (!OURS) {
+  if constexpr (!QUADS) {
     for (int k0 = 0; k0 < kbytes; k0 += chunk) {
       load(k0);
       wait_vmcnt<0>();
@@ -501,12 +501,12 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
     }
     if (tid < 16) row_scale[tid] = m0 + tid < op.M ? op.sa[m0 + tid] : 0.f;
   } else {
-    typename Four<KIND>::V v[OURS];
+    typename Four<KIND>::V v[QUADS];
     const bool has = m0 + wave < op.M;
     using F = Four<KIND>;
     const typename F::X* px = (const typename F::X*)xs + (int64_t)(m0 + wave) * ldx;
 #pragma unroll
-    for (int i = 0; i < OURS; i++) {
+    for (int i = 0; i < QUADS; i++) {
       const int k = (i * 64 + lane) * 4;
       v[i] = typename F::V{};
       if (has && k < op.K) v[i] = *reinterpret_cast<const typename F::In*>(px + k);
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
     if (has) {                                         // (behind the last row anything: its products are not stored)
       uint32_t most = 0;
 #pragma unroll
-      for (int i = 0; i < OURS; i++) {
+      for (int i = 0; i < QUADS; i++) {
         float f[4];
         floats_of(v[i], f);
 #pragma unroll
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
       if (lane == 0) row_scale[wave] = sc.scale;
       const int sw = (wave >> 1) & 7;
 #pragma unroll
-      for (int i = 0; i < OURS; i++) {
+      for (int i = 0; i < QUADS; i++) {
         const int k = (i * 64 + lane) * 4;
         float f[4];
         floats_of(v[i], f);
@@ -558,26 +558,26 @@ __global__ __launch_bounds__(R16_W * 64) void q8_rows16_kernel(Q8Op op, const vo
 // 16-column pieces of a workgroup that quantises its rows: as many as leave about a workgroup per CU
 int rows16_nt(int64_t N) { return N <= 256 * 16 ? 1 : N <= 512 * 16 ? 2 : 4; }
 
-template <int OURS, Rows KIND, int NT, int OUT, bool TAIL>
+template <int QUADS, Rows KIND, int NT, int OUT, bool TAIL>
 hipError_t launch_rows16_nt(const Q8Op& op, const void* x, int64_t ldx, hipStream_t st) {
-  auto kern = q8_rows16_kernel<OURS, KIND, NT, OUT, TAIL>;
+  auto kern = q8_rows16_kernel<QUADS, KIND, NT, OUT, TAIL>;
   // one-time opt-in to more than 64 KB of dynamic LDS (thread-safe function-local static)
   static const hipError_t attr_err = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, R16_LDS - 256);
   if (attr_err != hipSuccess) return attr_err;
   const int whole = (op.K + 127) / 128 * 128;
   int chunk = whole;
   while (rows16_lds(chunk, NT) > R16_LDS - 256) chunk = (chunk / 2 + 127) / 128 * 128;      // (int8 alone: several turns of even length)
-  if (OURS && (chunk != whole || op.K > OURS * 256)) return hipErrorInvalidValue;
+  if (QUADS && (chunk != whole || op.K > QUADS * 256)) return hipErrorInvalidValue;
   const dim3 grid((uint32_t)((op.N + NT * 16 - 1) / (NT * 16)), (uint32_t)((op.M + 15) / 16));
   hipLaunchKernelGGL(kern, grid, dim3(R16_W * 64), rows16_lds(chunk, NT), st, op, x, ldx, chunk);
   return hipGetLastError();
 }
-template <int OURS, Rows KIND, int OUT>
+template <int QUADS, Rows KIND, int OUT>
 hipError_t launch_rows16_of(const Q8Op& op, const void* x, int64_t ldx, hipStream_t st) {
   switch (rows16_nt(op.N)) {
-    case 1: return launch_rows16_nt<OURS, KIND, 1, OUT, false>(op, x, ldx, st);
-    case 2: return launch_rows16_nt<OURS, KIND, 2, OUT, false>(op, x, ldx, st);
-    default: return launch_rows16_nt<OURS, KIND, 4, OUT, false>(op, x, ldx, st);
+    case 1: return launch_rows16_nt<QUADS, KIND, 1, OUT, false>(op, x, ldx, st);
+    case 2: return launch_rows16_nt<QUADS, KIND, 2, OUT, false>(op, x, ldx, st);
+    default: return launch_rows16_nt<QUADS, KIND, 4, OUT, false>(op, x, ldx, st);
   }
 }
 template <Rows KIND, int OUT>
@@ -598,7 +598,7 @@ hipError_t launch_q8(const Q8Op& op, int tile, hipStream_t st) {
     case Q8_R128: return launch_q8_ring<R128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64X128: return launch_q8_ring<R64x128, OUT, EDGE, TAIL>(op, st);
     case Q8_R64: return launch_q8_ring<R64, OUT, EDGE, TAIL>(op, st);
-    default: return launch_rows16_nt<0, Rows::OURS, 1, OUT, TAIL>(op, nullptr, 0, st);
+    default: return launch_rows16_nt<0, Rows::F32, 1, OUT, TAIL>(op, nullptr, 0, st);
   }
 }
 
@@ -638,11 +638,9 @@ bool gemm_q8_acts(const Q8Op& op) { return q8_tile(op) == Q8_ROWS16; }
 bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K) {
   return M <= 16 && K <= 4096 && K % 4 == 0 && rows16_lds((int)(K + 127) / 128 * 128, rows16_nt(N)) <= R16_LDS - 256;
 }
-hipError_t gemm_q8_from_ours(const Q8Op& op, const float* x, int64_t ldx, hipStream_t st) {
-  return op.dt == LR_BF16 ? launch_rows16_from<Rows::OURS, LR_BF16>(op, x, ldx, st) : launch_rows16_from<Rows::OURS, LR_F32>(op, x, ldx, st);
-}
 hipError_t gemm_q8_from(const Q8Op& op, const void* x, int64_t ldx, int dt, hipStream_t st) {
-  return dt == LR_BF16 ? launch_rows16_from<Rows::BF16, LR_F32>(op, x, ldx, st) : launch_rows16_from<Rows::F32, LR_F32>(op, x, ldx, st);
+  if (dt == LR_BF16) return op.dt == LR_F32 ? launch_rows16_from<Rows::BF16, LR_F32>(op, x, ldx, st) : hipErrorInvalidValue;
+  return op.dt == LR_BF16 ? launch_rows16_from<Rows::F32, LR_BF16>(op, x, ldx, st) : launch_rows16_from<Rows::F32, LR_F32>(op, x, ldx, st);
 }
 
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st) {

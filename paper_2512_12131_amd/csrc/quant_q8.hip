@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* x, int64_t ldx
       __syncthreads();
     }
     if (!in) continue;
-    const Scale<sizeof(T) == 2 ? Rows::BF16 : ACT ? Rows::OURS : Rows::F32> s(most);
+    const Scale<sizeof(T) == 2 ? Rows::BF16 : Rows::F32> s(most);
     auto put = [&](int64_t u, const Unit<T>& v) {
       float e[UNIT];
       v.floats(e);

@@ -8,8 +8,9 @@ namespace {
 // What a row's elements are.  bf16: the one quotient 127 |x| / max that lies on a half without being formed exactly is that of |x| = max / 2, 63.5 (254 |x| is an
 // odd multiple of max only if that has the prime factor 127, where 127 / max is a power of two, or for this x), and every other one is off a half by at
 // least 1/510 of a unit in the last place of x against max, 65 times the error of the product below; so 127 / max is rounded up, and 63.5 becomes
-// 64, as it should.  fp32: quotients next to a half are settled.  Ours: fp32 results of our own, where the last bits mean nothing: as they come.
-enum class Rows { BF16, F32, OURS };
+// 64, as it should.  fp32, also the rows between a layer's two products: quotients next to a half are settled, so that a row
+// has the same integers whichever kernel quantises it.
+enum class Rows { BF16, F32 };
 
 template <Rows KIND>
 struct Scale {
