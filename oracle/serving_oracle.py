@@ -30,7 +30,8 @@ def linear_q8(x, w_down, s_down, w_up, s_up, silu):
 
 
 def beam_select(logits, score, n, done=None, done_token=0):
-    """logits [batch * beams, V], score [batch, beams] -> parent, token, score [batch, n]"""
+    """logits [batch * beams, V], score [batch, beams] -> parent, token, score [batch, n].  By score, then beam; a beam's by logit (logits closer than a last
+    place of the score have one score), then token."""
     batch, beams = score.shape
     parent, token, best = (np.full((batch, n), v, dtype=t) for v, t in ((-1, np.int64), (-1, np.int64), (-np.inf, np.float64)))
     for b in range(batch):
@@ -40,7 +41,7 @@ def beam_select(logits, score, n, done=None, done_token=0):
             if not np.isfinite(score[b, w]):
                 continue
             if done is not None and done[b, w]:
-                found.append((-score[b, w], w, done_token))
+                found.append((-score[b, w], w, 0.0, done_token))
                 continue
             most = row.max()
             if not np.isfinite(most):
@@ -48,10 +49,10 @@ def beam_select(logits, score, n, done=None, done_token=0):
             lse = most + np.log(np.sum(np.exp(row - most)))
             value = score[b, w] + (row - lse)
             # more than n of a beam are never wanted; equal ones in the order of their tokens
-            for v in np.argsort(-value, kind="stable")[:n]:
+            for v in np.argsort(-row, kind="stable")[:n]:
                 if np.isfinite(value[v]):
-                    found.append((-value[v], w, int(v)))
-        for i, (v, w, t) in enumerate(sorted(found)[:n]):
+                    found.append((-value[v], w, -row[v], int(v)))
+        for i, (v, w, _, t) in enumerate(sorted(found)[:n]):
             parent[b, i], token[b, i], best[b, i] = b * beams + w, t, -v
     return parent, token, best
 

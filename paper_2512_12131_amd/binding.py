@@ -570,7 +570,7 @@ def lr_kv_copy(k_cache, v_cache, src, dst, rows=None):
 # ---- beam search -------------------------------------------------------------------------------
 def lr_beam_select(logits, score, n=None, done=None, done_token=0, out=None, ws=None):
     """logits [batch * beams, V], score [batch, beams] fp32.  Returns (parent, token, score) [batch, n] (n: None = beams) of the candidates of
-    highest score, in falling order; parent is a row of logits, -1 where there is no candidate left.  done [batch, beams] int32: beams that have ended
+    highest score, in falling order (equal ones by beam, a beam's own by logit and then token); parent is a row of logits, -1 where there is no candidate left.  done [batch, beams] int32: beams that have ended
     go on with done_token, at their score.  out: what an earlier call returned, to be written again."""
     return _native().beam_select(logits, score, score.shape[-1] if n is None else n, done, done_token, *((None,) * 3 if out is None else out), ws)
 

@@ -1,8 +1,10 @@
 // The candidates of highest score over the beams of a prompt and the vocabulary: score[w] + logit[w, v] - log sum_u exp(logit[w, u]), the n
-// largest for each prompt, ties to the lower beam, then the lower token.
+// largest for each prompt, ties to the lower beam; within a beam the order is that of the logits, ties to the lower token.
 //
 // Scores are formed in 64 bits: candidates of different beams are compared through two such sums, and 32 bits would change the
-// order of those that lie next to each other.
+// order of those that lie next to each other.  Logits that differ by less than a last place of their scores have one score, and still an order: score, beam,
+// logit and token together order all candidates, in the runs (one beam: logit and token) and in the merge alike, so that the first ones are the same however many
+// are asked for.
 //
 // First launch: a wavefront takes a run of one beam's logits.  Within a beam the order of the scores is that of the logits, so it keeps the
 // n largest logits of the run, one per lane, and the sum of exponentials relative to the largest logit of its first piece.  Second launch:
@@ -285,13 +287,13 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
   __shared__ double log_sum[BEAM_MOST];                // NaN: the beam offers nothing
   __shared__ float largest[BEAM_MOST], score_in[BEAM_MOST];
   __shared__ uint64_t best_score[2][BEAM_MOST + 256];  // (double's order; 0: none)
-  __shared__ uint32_t best_at[2][BEAM_MOST + 256];     // ~(beam of the prompt * 2^20 + token): the larger, the earlier
+  __shared__ uint64_t best_at[2][BEAM_MOST + 256];     // order_of: of equal scores the larger is the earlier
   __shared__ uint32_t floors[4];
   __shared__ int added;
   constexpr int AHEAD = 4;                             // candidates of a list that are asked for at once
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int prompt = blockIdx.x, row0 = prompt * s.beams;
-  // The runs' lists fall from candidate to candidate: all first ones, then the second ones, until none is added
+  // The runs' lists fall from candidate to candidate, in the order that the merge has: all first ones, then the second ones, until none is added
   const int lists = s.beams * s.parts;
   const uint2* keys = s.part_key + (int64_t)row0 * s.parts * s.n;
   uint2 key[AHEAD];
@@ -343,9 +345,11 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     }
   }
   __syncthreads();
+  // the lower beam of the prompt, the larger logit (as `ordered` numbers it), the lower token
+  auto order_of = [](int w, uint32_t logit, uint32_t token) { return (uint64_t)(BEAM_MOST - 1 - w) << 52 | (uint64_t)logit << 20 | (0xfffffu - token); };
   int have = 0, side = 0;                              // candidates in best_*[side], the best first
   // a candidate per thread: was one added?
-  auto offer = [&](uint64_t score, uint32_t at) {
+  auto offer = [&](uint64_t score, uint64_t at) {
     bool in;
     if (threadIdx.x == 0) added = 0;
     if (have == s.n) {
@@ -374,11 +378,11 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     for (int i0 = 0; i0 < all; i0 += 16) {
       const int i = min(i0 + (int)threadIdx.x / 16, all - 1);
       const uint64_t mine = best_score[side][i];
-      const uint32_t mine_at = best_at[side][i];
+      const uint64_t mine_at = best_at[side][i];
       int place = 0;
       for (int j = threadIdx.x & 15; j < all; j += 16) {
         const uint64_t other = best_score[side][j];
-        const uint32_t other_at = best_at[side][j];
+        const uint64_t other_at = best_at[side][j];
         place += other > mine || (other == mine && other_at > mine_at);
       }
       place = row_all(place, [](int a, int b) { return a + b; });
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     auto step = [&](uint2 k) {
       uint64_t score = 0;
       if (some && k.x != 0) score = ordered(((double)unordered(k.x) - largest[w] - less) + score_in[w] + 0.0);
-      return offer(score, ~((uint32_t)w << 20 | ~k.y));
+      return offer(score, order_of(w, k.x, ~k.y & 0xfffffu));
     };
     bool more = true;
 #pragma unroll 1
@@ -411,14 +415,14 @@ __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
     const int w = threadIdx.x;
     uint64_t score = 0;
     if (w < s.beams && s.done[row0 + w] != 0 && __builtin_fabsf(score_in[w]) < INFINITY) score = ordered((double)score_in[w] + 0.0);
-    offer(score, ~((uint32_t)w << 20 | (uint32_t)s.done_token));
+    offer(score, order_of(w & (BEAM_MOST - 1), 0, (uint32_t)s.done_token));
   }
   if ((int)threadIdx.x < s.n) {
     const int64_t o = (int64_t)prompt * s.n + threadIdx.x;
     const bool some = (int)threadIdx.x < have;
-    const uint32_t at = some ? ~best_at[side][threadIdx.x] : 0;
-    s.parent[o] = some ? row0 + (int)(at >> 20) : -1;
-    s.token[o] = some ? (int)(at & 0xfffffu) : -1;
+    const uint64_t at = some ? best_at[side][threadIdx.x] : 0;
+    s.parent[o] = some ? row0 + BEAM_MOST - 1 - (int)(at >> 52) : -1;
+    s.token[o] = some ? (int)(0xfffffu - (uint32_t)(at & 0xfffffu)) : -1;
     s.score_out[o] = some ? (float)unordered(best_score[side][threadIdx.x]) : -INFINITY;
   }
 }
