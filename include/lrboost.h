@@ -465,6 +465,8 @@ int lr_launch_timer_end(lr_launch_record* records, int max_records, int* n_recor
  * operands k-contiguous (activation . weight^T), 1 the second one k-major (gradient . weight), 2 both k-major (weight
  * gradient, not accumulated, nothing folded in); tag: its epilogue class, as above.  Makes no GPU call.   */
 int lr_gemm_tile(int M, int N, int K, int batch, int form, int tag, int* rows, int* cols);
+/* The same of lr_matmul_q8's product of these sizes, and of lr_linear_q8_fwd's where it does not quantise rows on the way in.    */
+int lr_matmul_q8_tile(int64_t M, int64_t N, int64_t K, int* rows, int* cols);
 /* Sustained rate of the bf16 matrix pipes fed from registers alone (no LDS, no memory traffic):
  * 2048 wavefronts, 8 independent 32x32x16 accumulator tiles each, iters instructions per tile and
  * launch, `launches` timed launches after up to 4 untimed ones, on `stream`; *tflops (HOST pointer)

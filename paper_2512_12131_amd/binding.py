@@ -121,6 +121,7 @@ _SIGS = {
     "lr_linear_q8_fwd": (_int, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _int, _int, _vp, _sz, _vp]),
     "lr_launch_timer_begin": (_int, [_int]),
     "lr_launch_timer_end": (_int, [_vp, _int, C.POINTER(_int)]),
+    "lr_matmul_q8_tile": (_int, [_i64, _i64, _i64, C.POINTER(_int), C.POINTER(_int)]),
     "lr_gemm_tile": (_int, [_int, _int, _int, _int, _int, _int, C.POINTER(_int), C.POINTER(_int)]),
     "lr_mfma_probe": (_int, [_int, _int, _int, C.POINTER(C.c_double), _vp]),
     "lr_rms_stat": (_int, [_vp, _i64, _vp, _i64, _i64, _int, _vp]),
@@ -637,6 +638,13 @@ def lr_gemm_tile(M, N, K, batch=1, form=0, tag=0):
     2: weight gradient; tag: the epilogue class of its launch record."""
     rows, cols = _int(0), _int(0)
     _check(lib().lr_gemm_tile(M, N, K, batch, form, tag, C.byref(rows), C.byref(cols)), "lr_gemm_tile")
+    return rows.value, cols.value
+
+
+def lr_matmul_q8_tile(M, N, K):
+    """(rows, columns) of the output tile that a product of 8-bit integers runs on."""
+    rows, cols = _int(0), _int(0)
+    _check(lib().lr_matmul_q8_tile(M, N, K, C.byref(rows), C.byref(cols)), "lr_matmul_q8_tile")
     return rows.value, cols.value
 
 

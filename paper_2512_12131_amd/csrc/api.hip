@@ -1731,11 +1731,14 @@ static int check_q8_out(const void* c, int64_t ldc, int64_t N, int dt) {
   if (ldc > Q8_LDC_MOST) return LR_EUNSUPPORTED;
   return check_ptrs(LR_BF16, {c});
 }
+static int check_q8_sizes(int64_t M, int64_t N, int64_t K) {
+  if (M < 0 || M > 0x7fffffffLL - 255 || N <= 0 || N > 0x7fffffffLL - 255 || K <= 0) return LR_EINVAL;
+  return K > Q8_K_MOST || M * N > ((int64_t)1 << 40) ? LR_EUNSUPPORTED : LR_OK;
+}
 int lr_matmul_q8(const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb, const float* sb, void* c, int64_t ldc, int64_t M,
                  int64_t N, int64_t K, int dt, void* stream) {
   TRY(check_dt(dt));
-  if (M < 0 || M > 0x7fffffffLL - 255 || N <= 0 || N > 0x7fffffffLL - 255 || K <= 0) return LR_EINVAL;
-  if (K > Q8_K_MOST || M * N > ((int64_t)1 << 40)) return LR_EUNSUPPORTED;
+  TRY(check_q8_sizes(M, N, K));
   if (M == 0) return LR_OK;
   TRY(check_q8(a, lda, sa, K)); TRY(check_q8(b, ldb, sb, K)); TRY(check_q8_out(c, ldc, N, dt));
   const Q8Op op{a, b, sa, sb, c, lda, ldb, ldc, (int)M, (int)N, (int)K, dt};
@@ -1814,6 +1817,16 @@ int lr_gemm_tile(int M, int N, int K, int batch, int form, int tag, int* rows, i
   op.M = M; op.N = N; op.K = K; op.batch = batch; op.epi.kind = tag;
   if (form == 1) { op.transB = 1; op.ldb = N; }
   gemm_bf16_tile_size(form == 2 ? gemm_bf16_plan_wgrad(M, N, K, batch, true).tile : gemm_bf16_tile(op), rows, cols);
+  return LR_OK;
+}
+
+int lr_matmul_q8_tile(int64_t M, int64_t N, int64_t K, int* rows, int* cols) {
+  if (!rows || !cols) return LR_EINVAL;
+  TRY(check_q8_sizes(M, N, K));
+  if (M == 0) return LR_EINVAL;
+  Q8Op op{};
+  op.M = (int)M; op.N = (int)N; op.K = (int)K;
+  gemm_q8_tile_size(op, rows, cols);
   return LR_OK;
 }
 

@@ -313,6 +313,7 @@ struct Q8Op {
   int act = LR_ACT_IDENTITY;               // of C, before it is stored (where gemm_q8_acts says so, and gemm_q8_from)
 };
 hipError_t gemm_q8(const Q8Op& op, hipStream_t st);
+void gemm_q8_tile_size(const Q8Op& op, int* rows, int* cols);
 // The same of few rows x [M, K] of type dt that are quantised on the way in (op.A and op.sa are not read); of bf16 rows only fp32 results.
 bool gemm_q8_acts(const Q8Op& op);
 constexpr int64_t Q8_FEW_ELEMENTS = 1 << 15;

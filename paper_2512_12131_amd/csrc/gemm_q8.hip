@@ -612,15 +612,16 @@ hipError_t launch_q8(const Q8Op& op, int tile, hipStream_t st) {
 int q8_tile(const Q8Op& op) {
   auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
   if (up(op.M, 16) * up(op.N, 16) <= 512) return Q8_ROWS16;
-  struct Cost { int rows, cols, slots; double f, e, e1, s0, s1; };
-  static constexpr Cost cost[] = {{256, 256, 256, 4.06, 2.35, 3.45, 0.935, 0.568}, {128, 128, 256, 2.53, 2.07, 0.95, 0.345, 0.186},
-                                  {64, 128, 512, 3.00, 0.95, 1.40, 0.252, 0.353}, {64, 64, 256, 2.27, 2.00, 0.22, 0.159, 0.050}};
+  struct Cost { int rows, cols, slots, threads; double f, e, e1, s0, s1; };      // threads: of a workgroup per tile
+  static constexpr Cost cost[] = {{256, 256, 256, 0, 4.06, 2.35, 3.45, 0.935, 0.568}, {128, 128, 256, R128::NT, 2.53, 2.07, 0.95, 0.345, 0.186},
+                                  {64, 128, 512, R64x128::NT, 3.00, 0.95, 1.40, 0.252, 0.353}, {64, 64, 256, R64::NT, 2.27, 2.00, 0.22, 0.159, 0.050}};
   const double slices = (double)up(op.K, 128);
   int best = 0;
   double least = 0;
   for (int t = 0; t < 4; t++) {
     const Cost& c = cost[t];
     const int64_t tiles = up(op.M, c.rows) * up(op.N, c.cols);
+    if (tiles * c.threads >= (int64_t)1 << 32) continue;      // more than a launch may have (2^30 rows and a few columns); the stream of 256 x 256 tiles has 256 workgroups
     const double fill = (double)(tiles % c.slots) / c.slots;
     double us = c.f + (double)(tiles / c.slots) * (c.e + c.e1 + slices * (c.s0 + c.s1));
     if (fill > 0) us += c.e + c.e1 * fill + slices * (c.s0 + c.s1 * fill);
@@ -634,6 +635,12 @@ int q8_tile(const Q8Op& op) {
 
 }  // namespace
 
+void gemm_q8_tile_size(const Q8Op& op, int* rows, int* cols) {
+  static constexpr int size[][2] = {{256, 256}, {128, 128}, {64, 128}, {64, 64}, {16, 16}};
+  const int tile = q8_tile(op);
+  *rows = size[tile][0];
+  *cols = size[tile][1];
+}
 bool gemm_q8_acts(const Q8Op& op) { return q8_tile(op) == Q8_ROWS16; }
 bool gemm_q8_quantises(int64_t M, int64_t N, int64_t K) {
   return M <= 16 && K <= 4096 && K % 4 == 0 && rows16_lds((int)(K + 127) / 128 * 128, rows16_nt(N)) <= R16_LDS - 256;
