@@ -1,7 +1,9 @@
 """The rows between a layer's two products are those of lr_quant_rows, whatever the activation and however many tokens there are."""
+import numpy as np
 import pytest
 import torch
 
+from oracle import serving_oracle as so
 from paper_2512_12131_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -72,3 +74,21 @@ def test_a_layer_is_its_single_steps(d, r, n, act, dtype):
     for first, count in ((0, 130), (0, 1), (4, 1), (3, 2), (0, 8), (8, 5), (1, 16), (0, 17), (40, 64)):
         got = B.lr_linear_q8_fwd(x[first:first + count].contiguous(), wd, sd, wu, su, act=act)
         assert torch.equal(bits(got), bits(want[first:first + count])), (first, count)
+
+
+@pytest.mark.parametrize("n", [1016, 8 * 1016, 16 * 1016])
+def test_fp32_rows_next_to_a_half(n):
+    """Elements at (2 k + 1) max / 254 for every k and up to three last places beside it, and exact halves (max a multiple of 254), for the smallest and largest
+    rows there are: whole numbers are those of the quotient, which 64 bits hold exactly where it is a half and else decide (2^-33 off one at least)."""
+    rng = np.random.default_rng(n)
+    most = np.concatenate([2.0 ** np.array([-126.0, -119, -40, -1, 0, 1, 60, 127]) * (1 + rng.random(8)), 254.0 * 2.0 ** np.array([-120.0, -30, 0, 100]) * rng.integers(1, 2 ** 16, 4),
+                           127 * 2.0 ** -126 * np.array([1 - 2.0 ** -20, 1, 1 + 2.0 ** -20])]).astype(np.float32)
+    k = np.arange(n) % 127
+    x = ((2 * k + 1) * most.astype(np.float64)[:, None] / 254).astype(np.float32)
+    x = np.where(most[:, None] % 254 == 0, x, (x.view(np.int32) + rng.integers(-3, 4, x.shape).astype(np.int32)).view(np.float32))
+    x *= np.where(rng.random(x.shape) < 0.5, -1, 1).astype(np.float32)
+    x[:, n // 2] = most
+    want, scale = so.quant_rows(x.astype(np.float64))
+    q, s = B.lr_quant_rows(torch.from_numpy(x).to(DEV))
+    assert np.array_equal(q.cpu().numpy().astype(np.int64), want)
+    assert np.array_equal(s.cpu().numpy(), scale.astype(np.float32))
