@@ -407,7 +407,8 @@ int lr_kv_copy(const lr_kv_cache* cache, const int32_t* src, const int32_t* dst,
 /* Beam search's choice: for each of `batch` prompts the n candidates (beam w, token v) of highest
  *   score[b, w] + logits[b * beams + w, v] - log sum_u exp(logits[b * beams + w, u])
  * in falling order, formed in 64 bits; equal ones by beam.  A beam's own are in the order of their logits, also where those are too close for 64-bit scores to
- * differ, equal logits by token: the first candidates are the same for every n.  logits [batch * beams, ldl] (dt), V tokens; parent [batch, n] receives the
+ * differ, equal logits by token: the first candidates are the same for every n.  (The order in which a sum is added up depends on batch * beams, so a prompt's scores may differ by
+ * last places of 64 bits with the prompts beside it.)  logits [batch * beams, ldl] (dt), V tokens; parent [batch, n] receives the
  * row b * beams + w (what lr_kv_fork takes), token [batch, n] the token, score_out [batch, n] the score, rounded to fp32.  done [batch, beams] (int32, NULL: none):
  * a beam with done != 0 has ended; its one candidate is done_token at its score, its logits are not read.  Logits of -infinity are no candidates; a beam whose
  * score is no finite number, or whose logits hold a NaN, +infinity or nothing above -infinity, has none.  Where there are fewer than n: parent and token

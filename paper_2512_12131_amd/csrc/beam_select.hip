@@ -153,8 +153,8 @@ struct RunState {
   }
 };
 
-// E: logits per lane and piece.  Bound: vector instructions (70 % of all cycles), 16 for an exponential, most of them in 64 bits, which are as fast as those of 32
-// here.  64 prompts of 8 beams, 131072 tokens in bf16: 65 us (134 MB, 2.1 TB/s; without exponentials and candidates 22); one prompt of 4 beams, 32000 tokens: 5.5.
+// E: logits per lane and piece.  Bound: vector instructions (71 % of all cycles), 19 for an exponential, most of them in 64 bits, which are as fast as those of 32
+// here.  64 prompts of 8 beams, 131072 tokens in bf16: 72 us (134 MB, 1.9 TB/s; without exponentials and candidates 22); one prompt of 4 beams, 32000 tokens: 5.6.
 // Every piece asks for the same number of vectors, the next one's before this one is worked on, so that the compiler can count which have arrived:
 // behind the last vector it is that one once more.
 template <class T, int E>
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256) void beam_runs_kernel(BeamSelect s) {
 
 // One workgroup per prompt.  The n best candidates so far lie in LDS; with up to 256 more of them, a candidate's new place is the number of those
 // above it.  Bound: latency, of the first launch's results and of the steps that wait for each other:
-// one prompt of 4 beams 4.9 us, 64 of 8 beams 8.9.
+// one prompt of 4 beams 4.6 us, 64 of 8 beams 9.0.
 __global__ __launch_bounds__(256) void beam_merge_kernel(BeamSelect s) {
   // a candidate's score is (logit - largest logit) - logarithm of the sum + score, in this order: the logits may be far from zero
   __shared__ double log_sum[BEAM_MOST];                // NaN: the beam offers nothing

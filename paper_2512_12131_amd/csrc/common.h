@@ -251,7 +251,7 @@ hipError_t attention_paged_bf16(const KvCache& c, const void* q, int64_t ldq, vo
                                 void* ws, hipStream_t);
 
 // ---- pages of the cache (kv_pages.hip) -------------------------------------------------------------
-constexpr int KV_FORK_MOST = 1 << 14;      // sequences, old or new (two words of LDS for each)
+constexpr int KV_FORK_MOST = 1 << 14;      // sequences, old or new (two words of LDS for each old one)
 struct KvFork {
   const int32_t *refs_in, *table_in, *len_in, *parent, *grow;
   int32_t *refs_out, *table_out, *len_out, *copy_src, *copy_dst, *copy_rows, *missing;
@@ -292,7 +292,7 @@ struct BeamSelect {
   int done_token, rows, beams, V, n;
   int32_t *parent, *token;
   float* score_out;
-  int parts, run;                          // runs of a row, logits of each
+  int parts, run;                          // runs of a row, vectors of 16 bytes of each
   double* part_sum;                        // in the workspace
   uint2* part_key;
   float* part_ref;

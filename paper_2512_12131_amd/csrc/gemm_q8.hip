@@ -191,7 +191,7 @@ __global__ __launch_bounds__(T::NT) void q8_ring_kernel(Q8Op op, int tiles_m, in
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (TAIL && stage_of(it) == nit - 1) {
-      // what lies behind K is cleared in LDS, once (a mask on the way into every product, us: 777 x 2047 x 5461 23.3, so 20.9; 300 x 3001 x 4001 15.2, so 12.0)
+      // what lies behind K is cleared in LDS, once (a mask on the way into every product, us: 777 x 2047 x 5461 with rows of 5504 23.3, so 20.9; 300 x 3001 x 4001 15.2, so 12.0)
       static_assert(T::BM <= T::NT, "a thread per row");
       if (tid < T::BM) {
         i32x4* last = reinterpret_cast<i32x4*>(smem + rd * T::STAGE + tail.chunk / 8 % T::SUB * T::SLICE + tid * 128 + ((tail.chunk % 8 ^ (tid >> 1 & 7)) << 4));
@@ -377,6 +377,7 @@ __global__ __launch_bounds__(Big::NT) void q8_big_kernel(Q8Op op, int tiles_m, i
       multiply(kk & 1, kt * 8 + kk * 2 + fk, std::integral_constant<bool, first && kk == 0>{});
       interleave(std::integral_constant<int, (kk > 0 ? T::WLA / 2 : first ? 0 : T::WLB / 2)>{});
     });
+    // (behind an epilogue the scales' loads lie between its stores and this slice's loads, so most of its stores are waited for too)
     if (first && stores_fly) wait_vmcnt<(T::WLA + STORES)>();
     else wait_vmcnt<T::WLA>();
     wait_lgkmcnt0();
@@ -435,9 +436,9 @@ hipError_t launch_q8_big(const Q8Op& op, hipStream_t st) {
 //
 // QUADS: A comes as rows of type KIND, which every workgroup quantises for itself, a wavefront a row: it holds the row (of up to 64 * 4 * QUADS columns) in
 // registers, whose largest element needs no other wavefront.  Bound: the way in and out of a launch, and what a CU takes in.
-// The layer 4096 -> 1024 -> 4096 of 16 tokens, us: 12.1 so in its second product, 13.0 with a launch for the quantisation between the products.  In the first
-// product, where every workgroup does the rows' whole work, up to 2^15 elements: of 1 / 8 / 16 tokens, with a launch before it, 10.6 / 11.4 / 12.1, without
-// 9.1 / 10.3 / 12.4; 1024 -> 256 -> 1024 7.8 / 8.1 / 8.5 and 5.6 / 6.0 / 6.7; 4096 -> 4096 -> 4096 in fp32 14.7 / 16.3 / 17.3 and 13.3 / 15.9 / 17.9.
+// The layer 4096 -> 1024 -> 4096 of 16 tokens, us: 11.3 so in its second product, 12.7 with a launch for the quantisation between the products.  In the first
+// product, where every workgroup does the rows' whole work, up to 2^15 elements: of 1 / 8 / 16 tokens, with a launch before it, 10.1 / 10.6 / 11.3, without
+// 8.2 / 9.1 / 11.2; 1024 -> 256 -> 1024 9.2 / 9.2 / 9.4 and 6.0 / 6.0 / 6.5; 4096 -> 4096 -> 4096 in fp32 13.9 / 15.8 / 17.2 and 12.1 / 14.8 / 17.2.
 constexpr int R16_W = 16, R16_SLICE = 2048, R16_LDS = 160 * 1024;
 constexpr int rows16_lds(int chunk, int nt) { return chunk / 128 * R16_SLICE * (1 + nt) + R16_W * nt * 1024; }
 

@@ -148,7 +148,7 @@ __global__ __launch_bounds__(PLAN_T) void fork_plan_kernel(KvFork f) {
   }
 }
 
-// One wavefront per row: the new tables, lengths and copies, and how the old tables' pages change hands.  Bound: latency; 512 beams 3.5 us.
+// One wavefront per row: the new tables, lengths and copies, and how the old tables' pages change hands.  Bound: latency; 512 beams 3.8 us.
 __global__ __launch_bounds__(256) void fork_rows_kernel(KvFork f) {
   const int lane = threadIdx.x & 63;
   const int row = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void compact_apply_kernel(KvCompact c) {
 // The first rows[i] tokens (NULL: all) of page src[i] onto page dst[i], keys and values.
 //
 // Bound: HBM.  A workgroup takes up to 256 * PER vectors of 16 bytes of a pair's keys or values at a time, PER per lane, in the order token, head, column.
-// 2048 pages of 64 KB 37 - 43 us (268 MB read and written, 6.3 TB/s and more), the half filled pages of 512 beams, 47 MB, 12.4.
+// 2048 pages of 64 KB 37 - 43 us (268 MB read and written, 6.3 TB/s and more), the half filled pages of 512 beams, 47 MB, 11.9.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int PER>
 __global__ __launch_bounds__(256) void kv_copy_kernel(KvCopy c) {

@@ -3,8 +3,8 @@
 //
 // The quotient is not formed: quant_row.h says by which product the whole number is found.
 //
-// Bound: HBM, a row read once where it fits the registers of its lanes: 16384 x 4096 bf16 34 - 46 us (201 MB), 777 x 5461 fp32 in rows that start anywhere 7.9; few rows
-// the way in and out of a launch, 16 x 4096 bf16 3.0.
+// Bound: HBM, a row read once where it fits the registers of its lanes: 16384 x 4096 bf16 37 - 47 us (201 MB), 777 x 5461 fp32 in rows that start anywhere 8.0; few rows
+// the way in and out of a launch, 16 x 4096 bf16 2.8.
 #include "quant_row.h"
 
 namespace lrb {
