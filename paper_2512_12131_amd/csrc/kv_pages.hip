@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void fork_rows_kernel(KvFork f) {
       const bool take = col < f.max_pages && col >= c.full && !keep && (int64_t)col * f.page_size < c.now;
       const uint64_t takers = __ballot(take);
       const int slot = at + lanes_below(takers);
-      at += __popcll(takers);
+      at = min(at + __popcll(takers), f.n_pages);      // (no more than there are: a table may have 2^31 columns, and slots are counted in 32 bits)
       const int got = take && slot < found ? f.fresh[slot] : -1;
       if (col < f.max_pages) out[col] = keep ? e : got;
       if (got >= 0) f.refs_out[got] = 1;
